@@ -487,6 +487,126 @@ int mquant_w4g128_gemm(const void *x_dev, int64_t ldx, const uint8_t *w_prepacke
                        int64_t ldy, int32_t T, int32_t N, int32_t K, mquant_stream_t stream);
 
 /* -------------------------------------------------------------------------
+ * The serving step of a decoder layer: new rows of several sequences between the qkv linear and the o
+ * linear, over a paged cache, and low-rank adapters beside a linear.  The rows of a step lie behind one another,
+ * sequence by sequence: sequence s has rows row_start[s] .. row_start[s + 1] - 1 (in any order inside
+ * it, for instance AIFS order), possibly none.  row_start must not decrease; rows before row_start[0] or from
+ * row_start[n_seq] on belong to no sequence and are left alone.  pos[i] is the position row i had in its
+ * ORIGINAL sequence, as in mquant_aifs_attention and mquant_rope_apply.
+ * ---------------------------------------------------------------------- */
+
+/* A paged key/value cache (host descriptor, read during the call).  The token at original position p of
+ * sequence s is held in slot p: row p % page_size of page page_table[s][p / page_size].  Positions decide what a row
+ * sees, so the order in which a step's rows arrived leaves no trace in the cache.
+ *   k_pages_dev, v_pages_dev : fp16 [n_pages, n_kv_heads, page_size, head_dim], contiguous, 16-byte aligned
+ *   page_table_dev           : int32 [n_seq, table_pages], contiguous; entries of pages that no position reaches
+ *                              may hold anything
+ *   page_size : a power of two, 16 .. 4096 (ERR_UNSUPPORTED otherwise); head_dim must be 128 */
+typedef struct {
+    void *k_pages_dev;
+    void *v_pages_dev;
+    const int32_t *page_table_dev;
+    int32_t n_seq;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t table_pages;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+} mquant_paged_cache_t;
+
+/*
+ * DEVICE.  Root-mean-square norm of every query and key head and its rotary embedding in one pass:
+ *     u = x * (mean(x^2) + eps)^(-1/2) * w      over the head's channels; u = x where the weight is NULL
+ *     y[2j] = u[2j] cos a - u[2j+1] sin a,  y[2j+1] = u[2j] sin a + u[2j+1] cos a,  a = pos[i] * base^(-2j/head_dim)
+ * in fp32 (angles in double), rounded to fp16 once.  mquant_rope_apply is the same without the norm, in place.
+ *   q_dev, k_dev         : fp16 [T, n_heads * head_dim], leading dimensions multiples of 8, 16-byte aligned
+ *   q_out_dev, k_out_dev : the same layout (written); q_out_dev == q_dev with the same leading dimension
+ *                          works in place, likewise k; no other overlap of an output with an input or output
+ *   q_weight_dev, k_weight_dev : fp16 [head_dim], 16-byte aligned, or NULL: no norm
+ *   eps                  : finite, >= 0
+ *   n_q_heads, n_kv_heads: >= 0, not both 0; the pointers of a side without heads are not read
+ * Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED (head_dim != 128), ERR_ALIGNMENT.
+ */
+int mquant_qk_norm_rope(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ldqo, const void *k_dev, int64_t ldk,
+                        void *k_out_dev, int64_t ldko, const void *q_weight_dev, const void *k_weight_dev, float eps,
+                        const int32_t *pos_dev, int32_t T, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                        double base, mquant_stream_t stream);
+
+/*
+ * DEVICE.  mquant_qk_norm_rope of a serving step's rows with the write to the cache in the same pass: q goes to
+ * q_out_dev, the normalised and rotated key and the value (as it is) of row i to slot pos[i] of the row's sequence.
+ *   q_dev, k_dev, v_dev : fp16 rows as above (n_q_heads, cache->n_kv_heads heads); k and v are read only
+ *   rope_pos_dev        : NULL: the rotation takes pos; else int32 [T], the rotary position ids (models whose
+ *                         ids differ from the token's place)
+ * A row whose position is negative or beyond the table, or whose page id is outside [0, n_pages), gets no slot:
+ * nothing of it is cached (its q is written all the same).  Rows of one sequence with equal positions leave one of them,
+ * unspecified which.  q_out_dev may be q_dev as above; the pages must not overlap the rows.
+ * n_q_heads may be 0 (q and q_out are then not touched).
+ * Errors: as mquant_qk_norm_rope; ERR_NULL (cache or one of its pointers), ERR_BAD_SHAPE (a negative count, n_pages or
+ *         table_pages < 1 where there are sequences).
+ */
+int mquant_kv_append(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ldqo, const void *k_dev, int64_t ldk,
+                     const void *v_dev, int64_t ldv, const void *q_weight_dev, const void *k_weight_dev, float eps,
+                     const int32_t *row_start_dev, const int32_t *pos_dev, const int32_t *rope_pos_dev, int32_t T,
+                     int32_t n_q_heads, double base, const mquant_paged_cache_t *cache, mquant_stream_t stream);
+
+/* Workspace of mquant_paged_attention for the same sizes and bounds (max_kv: table_pages * page_size where the call
+ * passes 0): 0 where no sequence's keys are split. */
+int64_t mquant_paged_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
+                                               int32_t head_dim, int32_t max_rows, int32_t max_kv);
+
+/*
+ * DEVICE.  Attention of a step's rows over the cache, for one new row per sequence (decode), a few (drafted
+ * tokens) or a whole chunk of a prompt, mixed in one call as they come:
+ *     o[i] = softmax(q[i] k[j]^T / sqrt(head_dim)) v[j] over the slots j <= pos[i] of row i's sequence
+ * per head (query head h reads key/value head h / (n_q_heads / n_kv_heads)); fp32 softmax statistics, fp16
+ * MFMA operands.  The rows' own keys and values are in the cache already (mquant_kv_append).  A row that
+ * sees no slot (pos[i] < 0) gets zeros.  Positions beyond the table count as its last slot.
+ *   q_dev, o_dev   : fp16 [T, n_q_heads * head_dim]; ldq a multiple of 8, ldo of 4; q 16-byte aligned, o 8-byte
+ *   max_rows       : most rows a sequence has in this call, max_kv: largest pos + 1.  They choose the kernel and how keys
+ *                    are split over work-groups, so that host values are enough to capture the call;
+ *                    data beyond them still get right results.  0: not known (T, and the table's slots).
+ *   workspace_dev  : mquant_paged_attention_workspace_bytes(...) bytes, 256-byte aligned; scratch, concurrent
+ *                    calls must not share it.  NULL where that is 0.
+ * Slots up to the largest position of a sequence's rows must hold finite values; slots behind it are not
+ * looked at.  A page id outside [0, n_pages) reads page 0.  o must not overlap q or the pages.
+ * Errors: ERR_NULL, ERR_BAD_SHAPE (n_q_heads not a multiple of n_kv_heads, ...), ERR_UNSUPPORTED (head_dim,
+ *         page_size, sizes beyond the grid), ERR_WORKSPACE, ERR_ALIGNMENT.
+ */
+int mquant_paged_attention(const void *q_dev, int64_t ldq, const mquant_paged_cache_t *cache,
+                           const int32_t *row_start_dev, const int32_t *pos_dev, void *o_dev, int64_t ldo, int32_t T,
+                           int32_t n_q_heads, int32_t max_rows, int32_t max_kv, void *workspace_dev,
+                           int64_t workspace_bytes, mquant_stream_t stream);
+
+/* Workspace of mquant_lora_apply (the rank-sized intermediate in fp32).  Negative status on a bad shape or rank. */
+int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t rank);
+
+/*
+ * DEVICE.  Low-rank adapters of many requests beside a shared linear: with base the linear's output (of
+ * mquant_w4a8_gemm, mquant_w4g128_gemm ... on the same x) and a = adapter[i],
+ *     h[i] = x[perm[i]] A_a^T,   y[i, n] = fp16( base[i, n] + scale[a] * sum_r h[i, r] B_a[n, r] )
+ * sums and h in fp32 or better.  Rows with adapter[i] outside [0, n_adapters) have none: y = base.
+ *   x_dev       : fp16 [T, K], leading dimension ldx (multiple of 8), 16-byte aligned: the linear's input BEFORE
+ *                 rotation and quantization
+ *   perm_dev    : NULL, or int32 [T]: row i of y belongs to row perm[i] of x (an entry outside [0, T) reads row 0)
+ *   adapter_dev : int32 [T], for row i of y
+ *   a_dev       : fp16 [n_adapters, rank, K]; b_dev: fp16 [n_adapters, N, rank], contiguous, 16-byte aligned;
+ *                 adapters of lower rank are padded with zeros
+ *   scale_dev   : fp32 [n_adapters]
+ *   base_dev, y_dev : fp16 [T, N], ldb, ldy >= N; y_dev == base_dev with ldy == ldb adds in place, no other
+ *                 overlap; 16-byte accesses where N, ldb and ldy are multiples of 8 and both are 16-byte aligned
+ *   workspace_dev : mquant_lora_workspace_bytes(T, K, rank) bytes, 256-byte aligned; scratch, concurrent
+ *                 calls must not share it
+ * rank: a multiple of 8 up to 128, K a multiple of 8 (ERR_UNSUPPORTED otherwise).  Rows of one adapter next to each
+ * other are the fast case; any order is right.
+ * T == 0 or N == 0 is a no-op.  Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_ALIGNMENT.
+ */
+int mquant_lora_apply(const void *x_dev, int64_t ldx, const int32_t *perm_dev, const int32_t *adapter_dev,
+                      const void *a_dev, const void *b_dev, const float *scale_dev, const void *base_dev, int64_t ldb,
+                      void *y_dev, int64_t ldy, int32_t T, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                      void *workspace_dev, int64_t workspace_bytes, mquant_stream_t stream);
+
+/* -------------------------------------------------------------------------
  * Tuning hook (tests and tuning runs; not needed for normal use).
  * ---------------------------------------------------------------------- */
 

@@ -544,3 +544,86 @@ def w4a8_linear(x: np.ndarray, vis_spans: Sequence[Tuple[int, int]], w_packed: n
         y = ref.astype(np.float16)
     out.update({"acc": acc, "ref": ref, "y": y})
     return out
+
+
+# --------------------------------------------------------------------------
+# The serving step: norm and rotation per head, paged cache, attention over it, adapters
+# --------------------------------------------------------------------------
+
+def qk_norm_rope_f64(x, weight, pos, n_heads: int, eps: float = 1e-6, base: float = 10000.0) -> np.ndarray:
+    """Root-mean-square norm of every head's channels (skipped where weight is None), then the rotation
+    of `rope_apply_f64`.  x is [T, n_heads*D]; fp64."""
+    x = np.asarray(x, dtype=np.float64)
+    if weight is not None:
+        h = x.reshape(x.shape[0], n_heads, -1)
+        h = h / np.sqrt((h * h).mean(axis=2, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)
+        x = h.reshape(x.shape)
+    return rope_apply_f64(x, pos, n_heads, base)
+
+
+def sequence_rows(row_start, T: int):
+    """(sequence, rows) pairs of a step: rows row_start[s] .. row_start[s+1]-1 of T."""
+    return [(s, np.arange(row_start[s], row_start[s + 1])) for s in range(len(row_start) - 1)]
+
+
+def cache_slot(page_table, page_size: int, seq: int, pos: int, n_pages: int):
+    """(page, row in it) of a sequence's token at position pos; None where it has no slot."""
+    if pos < 0 or pos // page_size >= page_table.shape[1]:
+        return None
+    page = int(page_table[seq, pos // page_size])
+    return (page, int(pos) % page_size) if 0 <= page < n_pages else None
+
+
+def kv_append(k_pages, v_pages, page_table, row_start, pos, k_new, v_new) -> None:
+    """Writes the rows of k_new, v_new [T, Hkv*D] to the pages [n_pages, Hkv, page size, D] in place."""
+    n_pages, hkv, page_size, D = k_pages.shape
+    for s, rows in sequence_rows(row_start, len(pos)):
+        for i in rows:
+            at = cache_slot(page_table, page_size, s, int(pos[i]), n_pages)
+            if at is not None:
+                k_pages[at[0], :, at[1]] = k_new[i].reshape(hkv, D)
+                v_pages[at[0], :, at[1]] = v_new[i].reshape(hkv, D)
+
+
+def paged_attention_f64(q, k_pages, v_pages, page_table, row_start, pos, n_q_heads: int, rows=None):
+    """softmax(q k^T / sqrt(D)) v over the slots 0 .. pos[i] of row i's sequence, per head; zeros for a row that
+    sees none, NaN for a row of no sequence; a page id out of range is page 0, a position beyond the table
+    its last slot.  `rows` restricts the rows computed."""
+    n_pages, hkv, page_size, D = k_pages.shape
+    T, group = len(pos), n_q_heads // hkv
+    out = np.full((T, n_q_heads * D), np.nan)
+    slots = np.arange(page_table.shape[1] * page_size)
+    wanted = set(range(T) if rows is None else (int(r) for r in rows))
+    for s, seq_rows in sequence_rows(row_start, T):
+        mine = [int(i) for i in seq_rows if int(i) in wanted]
+        if not mine:
+            continue
+        n = min(len(slots), max(0, max(int(pos[i]) for i in mine) + 1))
+        ids = page_table[s, slots[:n] // page_size]
+        ids = np.where((ids >= 0) & (ids < n_pages), ids, 0)
+        keys = np.asarray(k_pages[ids, :, slots[:n] % page_size], dtype=np.float64)        # [n, Hkv, D]
+        vals = np.asarray(v_pages[ids, :, slots[:n] % page_size], dtype=np.float64)
+        for i in mine:
+            m = min(n, int(pos[i]) + 1)
+            if m <= 0:
+                out[i] = 0.0
+                continue
+            qi = np.asarray(q[i], dtype=np.float64).reshape(n_q_heads, D)
+            for h in range(n_q_heads):
+                z = keys[:m, h // group] @ qi[h] / math.sqrt(D)
+                e = np.exp(z - z.max())
+                out[i, h * D:(h + 1) * D] = (e / e.sum()) @ vals[:m, h // group]
+    return out
+
+
+def lora_f64(x, perm, adapter, a, b, scale, base) -> np.ndarray:
+    """base[i] + scale[id] * (x[perm[i]] A_id^T) B_id^T, id = adapter[i]; base[i] where id is no adapter's.  fp64."""
+    y = np.array(base, dtype=np.float64)
+    T = y.shape[0]
+    for i in range(T):
+        r, at = int(adapter[i]), i if perm is None else int(perm[i])
+        if 0 <= r < len(scale):
+            at = at if 0 <= at < T else 0
+            h = np.asarray(a[r], dtype=np.float64) @ np.asarray(x[at], dtype=np.float64)
+            y[i] += float(scale[r]) * (np.asarray(b[r], dtype=np.float64) @ h)
+    return y

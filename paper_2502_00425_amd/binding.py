@@ -40,6 +40,8 @@ EXPORTS = (
     "mquant_w4a8_linear_decode", "mquant_w4a8_linear_prefill_static", "mquant_w4a8_gemv_grouped",
     "mquant_w4a8_linear_decode_grouped",
     "mquant_w4g128_prepacked_bytes", "mquant_w4g128_prepack", "mquant_w4g128_gemm",
+    "mquant_qk_norm_rope", "mquant_kv_append", "mquant_paged_attention_workspace_bytes", "mquant_paged_attention",
+    "mquant_lora_workspace_bytes", "mquant_lora_apply",
 )
 
 OK, ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_ALIGNMENT = 0, -1, -2, -3, -4, -5, -6
@@ -53,6 +55,12 @@ class MQuantError(RuntimeError):
 
 class Span(ctypes.Structure):
     _fields_ = [("start", ctypes.c_int32), ("len", ctypes.c_int32)]
+
+
+class PagedCacheStruct(ctypes.Structure):
+    _fields_ = [("k_pages_dev", ctypes.c_void_p), ("v_pages_dev", ctypes.c_void_p), ("page_table_dev", ctypes.c_void_p),
+                ("n_seq", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("table_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class Linear(ctypes.Structure):
@@ -107,9 +115,19 @@ def _load() -> ctypes.CDLL:
     lib.mquant_w4g128_prepacked_bytes.argtypes = [i32, i32]
     lib.mquant_w4g128_prepack.argtypes = [p, p, p, i32, i32, p]
     lib.mquant_w4g128_gemm.argtypes = [p, i64, p, p, i64, i32, i32, i32, p]
+    f64 = ctypes.c_double
+    lib.mquant_qk_norm_rope.argtypes = [p, i64, p, i64, p, i64, p, i64, p, p, f32, p, i32, i32, i32, i32, f64, p]
+    lib.mquant_kv_append.argtypes = [p, i64, p, i64, p, i64, p, i64, p, p, f32, p, p, p, i32, i32, f64, p, p]
+    lib.mquant_paged_attention_workspace_bytes.restype = i64
+    lib.mquant_paged_attention_workspace_bytes.argtypes = [i32] * 7
+    lib.mquant_paged_attention.argtypes = [p, i64, p, p, p, p, i64, i32, i32, i32, i32, p, i64, p]
+    lib.mquant_lora_workspace_bytes.restype = i64
+    lib.mquant_lora_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.mquant_lora_apply.argtypes = [p, i64, p, p, p, p, p, p, i64, p, i64, i32, i32, i32, i32, i32, p, i64, p]
     for name in EXPORTS:
         if name not in ("mquant_status_string", "mquant_w4_prepacked_bytes", "mquant_aifs_attention_workspace_bytes",
                         "mquant_build_id", "mquant_w4g128_prepacked_bytes",
+                        "mquant_paged_attention_workspace_bytes", "mquant_lora_workspace_bytes",
                         "mquant_w4a8_workspace_bytes", "mquant_w4a8_linear_prefill_workspace_bytes",
                         "mquant_version"):
             getattr(lib, name).restype = ctypes.c_int
@@ -558,4 +576,152 @@ def w4g128_gemm(x, w_prepacked, N: int, out=None):
         return out
     _check(lib.mquant_w4g128_gemm(_dp(x), x.stride(0) if T > 0 else K, _dp(w_prepacked), _dp(out),
                                   out.stride(0) if T > 0 else N, T, N, K, _stream()), "mquant_w4g128_gemm")
+    return out
+
+
+# ----------------------------------------------------------- serving step
+
+def _operand(t, dtype, what: str, shape=None):
+    """A device operand of the serving entries: on the current device, of this type, and of `shape` (contiguous) or
+    2-D with unit column stride, whose leading dimension is returned."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected a tensor on the current device")
+    if t.dtype is not dtype:
+        raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected {dtype}, got {t.dtype}")
+    if shape is None:
+        ld = _rows(t, what)
+        return ld if t.shape[0] > 1 else t.shape[1] + -t.shape[1] % 8       # the stride of a single row says nothing
+    if tuple(t.shape) != shape:
+        raise MQuantError(ERR_BAD_SHAPE, f"{what}: expected shape {shape}, got {tuple(t.shape)}")
+    _dense(t, what)
+    return 0
+
+
+def _heads(t, n: int, head_dim: int, rows: int, what: str) -> int:
+    ld = _operand(t, torch.float16, what)
+    if t.shape[0] != rows or t.shape[1] < n * head_dim:
+        raise MQuantError(ERR_BAD_SHAPE, f"{what}: expected [{rows}, >= {n * head_dim}], got {tuple(t.shape)}")
+    return ld
+
+
+class PagedCache:
+    """A paged key/value cache (mquant_paged_cache_t) over the caller's tensors: k_pages, v_pages fp16 [n_pages,
+    n_kv_heads, page_size, head_dim] and page_table int32 [n_seq, table_pages]."""
+
+    def __init__(self, k_pages, v_pages, page_table):
+        if k_pages.dim() != 4 or page_table.dim() != 2:
+            raise MQuantError(ERR_BAD_SHAPE, "PagedCache: expected k_pages [pages, heads, page size, head dim], page_table [sequences, pages]")
+        _operand(k_pages, torch.float16, "k_pages", tuple(k_pages.shape))
+        _operand(v_pages, torch.float16, "v_pages", tuple(k_pages.shape))
+        _operand(page_table, torch.int32, "page_table", tuple(page_table.shape))
+        self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
+        (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim), (self.n_seq, self.table_pages) = k_pages.shape, page_table.shape
+        self.device_index = k_pages.device.index
+        self.struct = PagedCacheStruct(_dp(k_pages), _dp(v_pages), _dp(page_table), self.n_seq, self.n_pages, self.page_size,
+                                       self.table_pages, self.n_kv_heads, self.head_dim)
+        self.address = ctypes.addressof(self.struct)
+
+
+def _step(cache, row_start_dev, pos_dev, T: int) -> None:
+    if cache.device_index != torch.cuda.current_device():
+        raise MQuantError(ERR_UNSUPPORTED, "cache: expected tensors on the current device")
+    _operand(row_start_dev, torch.int32, "row_start", (cache.n_seq + 1,))
+    _operand(pos_dev, torch.int32, "pos", (T,))
+
+
+def _weight(w, head_dim: int, what: str) -> None:
+    if w is not None:
+        _operand(w, torch.float16, what, (head_dim,))
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, pos_dev, n_q_heads: int, n_kv_heads: int, head_dim: int = 128, eps: float = 1e-6,
+                 base: float = 10000.0, q_out=None, k_out=None):
+    """q [T, >= Hq*D], k [T, >= Hkv*D] fp16 views -> (q_out, k_out); pass q_out=q, k_out=k to work in place."""
+    T = q.shape[0]
+    if q_out is None:
+        q_out = torch.empty((T, n_q_heads * head_dim), dtype=torch.float16, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((T, n_kv_heads * head_dim), dtype=torch.float16, device=q.device)
+    lds = [_heads(t, n, head_dim, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
+                                                               (k, n_kv_heads, "k"), (k_out, n_kv_heads, "k_out"))]
+    _weight(q_weight, head_dim, "q_weight"), _weight(k_weight, head_dim, "k_weight")
+    _operand(pos_dev, torch.int32, "pos", (T,))
+    _check(lib.mquant_qk_norm_rope(_dp(q), lds[0], _dp(q_out), lds[1], _dp(k), lds[2], _dp(k_out), lds[3], _dp(q_weight),
+                                   _dp(k_weight), eps, _dp(pos_dev), T, n_q_heads, n_kv_heads, head_dim, base, _stream()),
+           "mquant_qk_norm_rope")
+    return q_out, k_out
+
+
+def kv_append(q, k, v, cache: PagedCache, row_start_dev, pos_dev, n_q_heads: int, q_weight=None, k_weight=None,
+              eps: float = 1e-6, base: float = 10000.0, rope_pos_dev=None, q_out=None):
+    """Norm and rotation of q and k [T, heads * D] and the write of k and v to the cache's slots -> q_out."""
+    T, D = q.shape[0], cache.head_dim
+    if q_out is None:
+        q_out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
+    lds = [_heads(t, n, D, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
+                                                        (k, cache.n_kv_heads, "k"), (v, cache.n_kv_heads, "v"))]
+    _weight(q_weight, D, "q_weight"), _weight(k_weight, D, "k_weight")
+    _step(cache, row_start_dev, pos_dev, T)
+    if rope_pos_dev is not None:
+        _operand(rope_pos_dev, torch.int32, "rope_pos", (T,))
+    _check(lib.mquant_kv_append(_dp(q), lds[0], _dp(q_out), lds[1], _dp(k), lds[2], _dp(v), lds[3], _dp(q_weight), _dp(k_weight),
+                                eps, _dp(row_start_dev), _dp(pos_dev), _dp(rope_pos_dev), T, n_q_heads, base, cache.address,
+                                _stream()), "mquant_kv_append")
+    return q_out
+
+
+def paged_attention_workspace_bytes(T: int, cache: PagedCache, n_q_heads: int, max_rows: int = 0, max_kv: int = 0) -> int:
+    n = int(lib.mquant_paged_attention_workspace_bytes(T, cache.n_seq, n_q_heads, cache.n_kv_heads, cache.head_dim, max_rows,
+                                                       max_kv or cache.table_pages * cache.page_size))
+    if n < 0:
+        raise MQuantError(n, "mquant_paged_attention_workspace_bytes")
+    return n
+
+
+def paged_attention(q, cache: PagedCache, row_start_dev, pos_dev, n_q_heads: int, max_rows: int = 0, max_kv: int = 0,
+                    out=None, workspace=None):
+    """q [T, >= Hq*D] fp16 of the step's rows -> o [T, Hq*D]; max_rows, max_kv: host bounds (0: not known)."""
+    T, D = q.shape[0], cache.head_dim
+    if out is None:
+        out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
+    ldq, ldo = _heads(q, n_q_heads, D, T, "q"), _heads(out, n_q_heads, D, T, "out")
+    _step(cache, row_start_dev, pos_dev, T)
+    if workspace is None:
+        need = paged_attention_workspace_bytes(T, cache, n_q_heads, max_rows, max_kv)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.mquant_paged_attention(_dp(q), ldq, cache.address, _dp(row_start_dev), _dp(pos_dev), _dp(out), ldo, T, n_q_heads,
+                                      max_rows, max_kv, _dp(workspace), ws_bytes, _stream()), "mquant_paged_attention")
+    return out
+
+
+def lora_workspace_bytes(T: int, K: int, rank: int) -> int:
+    n = int(lib.mquant_lora_workspace_bytes(T, K, rank))
+    if n < 0:
+        raise MQuantError(n, "mquant_lora_workspace_bytes")
+    return n
+
+
+def lora_apply(x, adapter_dev, a, b, scale, base, perm_dev=None, out=None, workspace=None):
+    """y = base + scale[id] * (x A_id^T) B_id^T per row, id = adapter[row] (outside the adapters: y = base); x [T, K], base
+    [T, N], a [adapters, rank, K], b [adapters, N, rank]; pass out=base to add in place."""
+    T, K = x.shape
+    N, (n_adapters, rank) = base.shape[1], a.shape[:2]
+    if out is None:
+        out = torch.empty((T, N), dtype=torch.float16, device=x.device)
+    ldx, ldb, ldy = (_operand(t, torch.float16, what) for t, what in ((x, "x"), (base, "base"), (out, "out")))
+    if base.shape[0] != T or tuple(out.shape) != (T, N):
+        raise MQuantError(ERR_BAD_SHAPE, f"lora_apply: base and out must be [{T}, {N}]")
+    _operand(adapter_dev, torch.int32, "adapter", (T,))
+    _operand(a, torch.float16, "a", (n_adapters, rank, K)), _operand(b, torch.float16, "b", (n_adapters, N, rank))
+    _operand(scale, torch.float32, "scale", (n_adapters,))
+    if perm_dev is not None:
+        _operand(perm_dev, torch.int32, "perm", (T,))
+    if workspace is None:
+        workspace = torch.empty(max(lora_workspace_bytes(T, K, rank), 256), dtype=torch.uint8, device=x.device)
+    ws_bytes = workspace.numel() * workspace.element_size()
+    _check(lib.mquant_lora_apply(_dp(x), ldx, _dp(perm_dev), _dp(adapter_dev), _dp(a), _dp(b), _dp(scale), _dp(base), ldb,
+                                 _dp(out), ldy, T, N, K, rank, n_adapters, _dp(workspace), ws_bytes, _stream()),
+           "mquant_lora_apply")
     return out

@@ -18,7 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libmquant.so")
 SOURCES = ["aifs.hip", "hadamard_quant.hip", "w4a8_gemm.hip", "w4a8_gemv.hip", "w4a8_sliced.hip", "w4a8_wide.hip", "w4a8_small.hip", "w4a8_walk.hip", "attention.hip",
-           "w4g128_gemm.hip", "w4g128_walk.hip"]
+           "w4g128_gemm.hip", "w4g128_walk.hip", "qk_norm.hip", "paged_attention.hip", "lora.hip"]
 # The benchmark's measurement probes: their own shared object, outside the product's ABI.
 PROBES_LIB = os.path.join(LIB_DIR, "libmquant_probes.so")
 PROBES_SOURCES = ["probes.hip"]
@@ -26,7 +26,7 @@ PROBES_SOURCES = ["probes.hip"]
 # this interpreter's ABI gives its modules.  Calls go through ctypes where it is not built.
 CALL_LIB = os.path.join(LIB_DIR, "mquant_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALL_SOURCES = ["fastcall.c"]
-HEADERS = ["mquant_internal.h", "hadamard_segment.h", "w4a8_common.h", "w4g128_common.h", "lds_dma.h", "probes.h"]
+HEADERS = ["mquant_internal.h", "hadamard_segment.h", "w4a8_common.h", "w4g128_common.h", "lds_dma.h", "serving_common.h", "probes.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,140 @@
+"""Adapters of many requests beside a shared linear against the fp64 oracle.
+
+Tolerance per element: the fp16 result is off by half a step, 2^-11 |y| and 2^-25 among subnormals.  The intermediate is an
+fp32 sum of K exact products whose accumulator takes at least 8 of them an addition, (K / 8 + 16) * 2^-24 of the
+sum of their magnitudes; carried into the second product as two fp16 parts it loses another 2^-21; that product's sum adds
+(rank + 4) * 2^-24 of its magnitudes."""
+import numpy as np
+import pytest
+
+from oracle import mquant_oracle as orc
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mq():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2502_00425_amd import binding
+    return binding
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def make(rng, T, K, N, rank, n, ids=None, gain=1.0):
+    return {"x": (rng.standard_normal((T, K)) * gain).astype(np.float16),
+            "a": (rng.standard_normal((n, rank, K)) / np.sqrt(K)).astype(np.float16),
+            "b": (rng.standard_normal((n, N, rank)) / np.sqrt(rank)).astype(np.float16),
+            "scale": rng.uniform(-2, 2, n).astype(np.float32), "base": rng.standard_normal((T, N)).astype(np.float16),
+            "ids": (rng.integers(-1, n + 1, T) if ids is None else np.asarray(ids)).astype(np.int32), "perm": None}
+
+
+def check(c, got, what=""):
+    ref = orc.lora_f64(c["x"], c["perm"], c["ids"], c["a"], c["b"], c["scale"], c["base"])
+    a, b, x = (np.abs(c[k].astype(np.float64)) for k in "abx")
+    K, rank = a.shape[2], a.shape[1]
+    size = orc.lora_f64(x, c["perm"], c["ids"], a, b, np.abs(c["scale"].astype(np.float64)), np.zeros_like(c["base"], dtype=np.float64))
+    tol = 2.0 ** -11 * np.abs(ref) + 2.0 ** -25 + ((K / 8 + 16 + rank + 4) * 2.0 ** -24 + 2.0 ** -21) * size
+    got = got.cpu().numpy().astype(np.float64)
+    assert np.isfinite(got).all(), what
+    err = np.abs(got - ref) - tol
+    worst = np.unravel_index(err.argmax(), err.shape)
+    assert (err <= 0).all(), f"{what}: {np.abs(got - ref)[worst]:.3e} > {tol[worst]:.3e} at {worst}"
+    none = (c["ids"] < 0) | (c["ids"] >= len(c["scale"]))
+    assert np.array_equal(got[none], c["base"].astype(np.float64)[none])
+
+
+def call(mq, c, **kw):
+    return mq.lora_apply(dev(c["x"]), dev(c["ids"]), dev(c["a"]), dev(c["b"]), dev(c["scale"]), dev(c["base"]),
+                         perm_dev=None if c["perm"] is None else dev(c["perm"]), **kw)
+
+
+@pytest.mark.parametrize("T,K,N,rank,n", [
+    (1, 8, 1, 8, 1), (1, 64, 16, 16, 1), (1, 3584, 4608, 16, 3), (2, 72, 100, 24, 2), (4, 3584, 512, 8, 4), (5, 520, 333, 40, 3),
+    (16, 512, 640, 16, 16), (17, 512, 640, 64, 4), (33, 1000, 130, 128, 5), (48, 4096, 264, 16, 12), (64, 640, 31, 32, 2),
+    (100, 264, 257, 56, 7), (150, 2048, 512, 64, 3), (257, 136, 72, 16, 40), (300, 512, 1032, 128, 2)])
+def test_sizes(mq, T, K, N, rank, n):
+    c = make(np.random.default_rng(T + K + N), T, K, N, rank, n)
+    check(c, call(mq, c), what=f"{T} {K} {N} r{rank}")
+
+
+@pytest.mark.parametrize("ids", ["one", "none", "runs", "each its own", "alternating", "last row only"])
+def test_who_has_which_adapter(mq, ids):
+    T, n = 133, 20
+    rows = {"one": np.full(T, 3), "none": np.where(np.arange(T) % 2, -1, n), "runs": np.arange(T) // 50, "each its own": np.arange(T) % n,
+            "alternating": np.where(np.arange(T) % 2, 0, 19), "last row only": np.where(np.arange(T) == T - 1, 5, -5)}[ids]
+    c = make(np.random.default_rng(1), T, 384, 272, 16, n, ids=rows)
+    check(c, call(mq, c), what=ids)
+
+
+@pytest.mark.parametrize("T", [6, 140])
+def test_reordered_rows(mq, T):
+    """x in original order, y in AIFS order; an index out of range reads row 0."""
+    rng = np.random.default_rng(2)
+    c = make(rng, T, 256, 320, 16, 3)
+    c["perm"] = orc.aifs_build_perm(T, [(1, T // 2)])[0].copy()
+    c["perm"][2], c["perm"][T - 1] = -1, T
+    check(c, call(mq, c), what="perm")
+
+
+def test_in_place_strides_and_streams(mq):
+    rng = np.random.default_rng(3)
+    for T, N in ((3, 96), (70, 96), (70, 91)):
+        c = make(rng, T, 128, N, 16, 4)
+        xw = torch.zeros((T, 200), dtype=torch.float16, device="cuda")
+        xw[:, 8:136] = dev(c["x"])
+        y = torch.full((T, N + 21), 2.0, dtype=torch.float16, device="cuda")
+        y[:, 5:5 + N] = dev(c["base"])
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            mq.lora_apply(xw[:, 8:136], dev(c["ids"]), dev(c["a"]), dev(c["b"]), dev(c["scale"]), y[:, 5:5 + N], out=y[:, 5:5 + N])
+        s.synchronize()
+        check(c, y[:, 5:5 + N], what="in place")
+        assert bool((y[:, :5] == 2).all()) and bool((y[:, 5 + N:] == 2).all())
+
+
+def test_wide_ranges(mq):
+    """Visual activations with outlier channels, an intermediate beyond fp16's range, tiny ones, no adapters at all."""
+    rng = np.random.default_rng(4)
+    c = make(rng, 40, 1024, 144, 16, 2, gain=20.0)
+    c["x"][:, [3, 97, 200]] *= np.float16(50)
+    check(c, call(mq, c), what="outliers")
+    c = make(rng, 20, 1024, 144, 16, 2)
+    c["x"][:] = 60000.0
+    c["a"][:] = np.abs(c["a"]) * np.float16(8)
+    c["b"][:] = (c["b"].astype(np.float32) * 1e-6).astype(np.float16)
+    check(c, call(mq, c), what="large intermediate")
+    c = make(rng, 20, 1024, 144, 16, 2, gain=1e-6)
+    check(c, call(mq, c), what="small")
+    c = make(rng, 20, 1024, 144, 16, 0, ids=np.zeros(20))
+    check(c, call(mq, c), what="no adapters")
+
+
+def test_stale_workspace_and_replays(mq):
+    """A captured call replayed with other ids and inputs, its workspace full of NaN patterns before each replay."""
+    rng = np.random.default_rng(5)
+    c = make(rng, 37, 2048, 264, 32, 5)
+    x, ids, base = dev(c["x"]), dev(c["ids"]), dev(c["base"])
+    rest = dev(c["a"]), dev(c["b"]), dev(c["scale"])
+    ws = torch.empty(mq.lora_workspace_bytes(37, 2048, 32), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(base)
+    run = lambda: mq.lora_apply(x, ids, *rest, base, out=out, workspace=ws)
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for rep in range(4):
+        c["ids"] = rng.integers(-1, 6, 37).astype(np.int32)
+        c["x"] = rng.standard_normal((37, 2048)).astype(np.float16)
+        ids.copy_(dev(c["ids"])), x.copy_(dev(c["x"]))
+        ws.fill_(0xff)
+        g.replay()
+        torch.cuda.synchronize()
+        check(c, out, what=f"replay {rep}")
+        assert torch.equal(mq.lora_apply(x, ids, *rest, base), out)

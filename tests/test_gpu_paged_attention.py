@@ -1,0 +1,215 @@
+"""Attention of a step's rows over a paged cache against the fp64 oracle.  Slots that no row may look at hold NaN and
+infinity, table entries behind a sequence's last page are out of range.  Tolerance: serving.attention_bound."""
+import numpy as np
+import pytest
+
+from oracle import mquant_oracle as orc
+from serving import D, attention_bound, make_step
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mq():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2502_00425_amd import binding
+    return binding
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def device_step(mq, st):
+    return (dev(st["q"]), mq.PagedCache(dev(st["kp"]), dev(st["vp"]), dev(st["table"])), dev(st["start"]), dev(st["pos"]), st["hq"])
+
+
+def check(st, got, rows=None, what=""):
+    ref = orc.paged_attention_f64(st["q"], st["kp"], st["vp"], st["table"], st["start"], st["pos"], st["hq"], rows=rows)
+    tol = attention_bound(st, ref, rows=rows)
+    mine = ~np.isnan(ref[:, 0])
+    got = got.cpu().numpy().astype(np.float64)
+    assert np.isfinite(got[mine]).all(), what
+    err = np.abs(got[mine] - ref[mine]) - tol[mine]
+    worst = np.unravel_index(err.argmax(), err.shape)
+    assert (err <= 0).all(), f"{what}: {np.abs(got[mine] - ref[mine])[worst]:.3e} > {tol[mine][worst]:.3e} at {worst}"
+    return mine
+
+
+def bounds_of(st):
+    return int(np.diff(st["start"]).max(initial=0)), int(st["pos"].max(initial=0)) + 1
+
+
+STEPS = {
+    "one token": ([(1, 1)], 28, 4, 16),
+    "two tokens": ([(1, 2)], 4, 4, 16),
+    "page borders": ([(1, n) for n in (15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129)], 8, 2, 16),
+    "one long": ([(1, 2500)], 28, 4, 16),
+    "mixed lengths": ([(1, 700), (1, 3), (1, 1500), (1, 64), (1, 65)], 16, 2, 64),
+    "large pages": ([(1, 300), (1, 1000)], 64, 8, 256),
+    "every head its own": ([(1, 333), (2, 90)], 5, 5, 32),
+    "one kv head": ([(1, 200), (1, 77)], 71, 1, 16),
+    "drafts": ([(5, 300), (3, 90), (1, 17), (9, 9)], 28, 4, 16),
+    "drafts, long": ([(5, 2100), (4, 1111)], 7, 1, 64),
+    "a prompt": ([(130, 130)], 4, 2, 16),
+    "a ragged prompt": ([(77, 77)], 28, 4, 64),
+    "a chunk": ([(100, 700)], 8, 2, 16),
+    "a chunk on a long cache": ([(65, 3000)], 7, 1, 32),
+    "chunks": ([(33, 500), (200, 201), (17, 1000)], 12, 4, 128),
+    "chunks and tokens": ([(1, 900), (150, 400), (1, 1), (0, 0), (3, 650), (64, 64)], 14, 2, 16),
+    "many short": ([(1, 1 + 7 * i % 90) for i in range(150)], 4, 1, 16),
+    "empty ones": ([(0, 0), (0, 40), (1, 9), (0, 0)], 4, 2, 16),
+}
+
+
+@pytest.mark.parametrize("name", list(STEPS))
+@pytest.mark.parametrize("known", [True, False])
+def test_steps(mq, name, known):
+    seqs, hq, hkv, page = STEPS[name]
+    rng = np.random.default_rng(sum(map(ord, name)))
+    st = make_step(rng, seqs, hq, hkv, page, before=1, behind=2, spans=[(3, 20), (40, 9)] if "prompt" in name or "chunk" in name else ())
+    out = torch.full((st["T"], hq * D), 7.0, dtype=torch.float16, device="cuda")
+    mq.paged_attention(*device_step(mq, st), *(bounds_of(st) if known else (0, 0)), out=out)
+    mine = check(st, out, what=name)
+    assert (out.cpu().numpy()[~mine] == 7).all()            # rows of no sequence stay as they were
+
+
+def test_seeded_sweep(mq):
+    """Random steps: rows, lengths, heads, page sizes, right, low and missing bounds."""
+    rng = np.random.default_rng(77)
+    heads = [(1, 1), (28, 4), (8, 8), (12, 2), (9, 3), (40, 1), (16, 8), (33, 11)]
+    for case in range(24):
+        hq, hkv = heads[case % len(heads)]
+        page = int(rng.choice([16, 32, 64, 128]))
+        seqs = []
+        for _ in range(int(rng.integers(1, 6))):
+            n = int(rng.choice([1, 1, 2, 7, int(rng.integers(10, 160))]))
+            seqs.append((n, n + int(rng.choice([0, 1, int(rng.integers(0, 60)), int(rng.integers(0, 900))]))))
+        st = make_step(rng, seqs, hq, hkv, page, before=int(rng.integers(0, 3)), behind=int(rng.integers(0, 3)),
+                       spans=[(1, int(rng.integers(1, 7)))])
+        bounds = [bounds_of(st), (0, 0), (1, 1), (3, 200)][int(rng.integers(0, 4))]
+        check(st, mq.paged_attention(*device_step(mq, st), *bounds), what=f"{case}: {seqs} {hq}/{hkv} page {page} bounds {bounds}")
+
+
+def test_rows_that_see_nothing(mq):
+    """Negative positions, alone and among others, with every slot of the cache NaN."""
+    rng = np.random.default_rng(4)
+    for rows, length in ((1, 200), (6, 200), (150, 400)):
+        st = make_step(rng, [(rows, length), (rows, length)], 8, 2, 16)
+        st["pos"][:rows] = -1 - np.arange(rows)
+        st["pos"][rows] = -2 ** 31
+        st["kp"][st["table"][0, :-1]] = np.nan                         # the first sequence's pages
+        st["vp"][st["table"][0, :-1]] = np.nan
+        for bounds in ((rows, length), (0, 0)):
+            got = mq.paged_attention(*device_step(mq, st), *bounds)
+            check(st, got, what=f"{rows} rows")
+            assert (got[:rows + 1] == 0).all()
+
+
+def test_positions_in_any_order_and_holes(mq):
+    """Rows of a chunk in random order, some far back, equal ones among them."""
+    rng = np.random.default_rng(5)
+    for rows in (4, 40, 200):
+        st = make_step(rng, [(rows, 600)], 7, 1, 32, poison=False)
+        st["pos"][:] = rng.integers(-3, 600, rows)
+        check(st, mq.paged_attention(*device_step(mq, st), rows, 600), what=f"{rows}")
+
+
+def test_positions_beyond_the_table_and_pages_out_of_range(mq):
+    rng = np.random.default_rng(6)
+    for rows in (1, 90):
+        st = make_step(rng, [(rows, 100)], 4, 2, 16, poison=False)
+        st["table"] = st["table"][:, :7].copy()                         # 112 slots; the tokens take all seven pages
+        st["table"][0, 2], st["table"][0, 4] = -1, 1 << 30              # page 0 is read in their place
+        st["pos"][0] = 5000
+        st["pos"][-1] = 2 ** 31 - 1
+        check(st, mq.paged_attention(*device_step(mq, st), rows, 112), what=f"{rows} rows")
+
+
+@pytest.mark.parametrize("rows", [1, 4, 130])
+def test_peaked_and_flat(mq, rows):
+    """Large logits of both signs (one slot takes all), equal logits, maxima that come late and early."""
+    rng = np.random.default_rng(7)
+    st = make_step(rng, [(rows, 1000)], 4, 2, 64, poison=False)
+    for gain in (0.0, 5.0, 30.0):
+        st2 = {**st, "q": (st["q"] * gain).astype(np.float16)}
+        check(st2, mq.paged_attention(*device_step(mq, st2), rows, 1000), what=f"gain {gain}")
+    up = st["kp"].copy()
+    for s in range(1000):                                               # logits that rise along the cache
+        page, r = orc.cache_slot(st["table"], 64, 0, s, len(up))
+        up[page, :, r] = 0.004 * s
+    st3 = {**st, "kp": up, "q": np.ones_like(st["q"])}
+    check(st3, mq.paged_attention(*device_step(mq, st3), rows, 1000), what="rising")
+
+
+def test_every_slot_counts(mq):
+    """Values one-hot in the slot's number: output channel c is the mass of the slots c, c + 128, ..., and a slot
+    skipped or taken twice shows, for single rows, drafts and chunks."""
+    rng = np.random.default_rng(8)
+    for rows, length, page in ((1, 128, 16), (1, 4000, 16), (6, 1500, 64), (140, 1200, 32)):
+        st = make_step(rng, [(rows, length)], 8, 2, page, poison=False)
+        st["q"] *= np.float16(0.2)
+        for s in range(length):
+            pg, r = orc.cache_slot(st["table"], page, 0, s, len(st["vp"]))
+            st["vp"][pg, :, r] = np.eye(D, dtype=np.float16)[s % D]
+        check(st, mq.paged_attention(*device_step(mq, st), rows, length), what=f"{rows} {length}")
+
+
+def test_strides_and_streams(mq):
+    """q and o as column slices with other strides, on a stream of its own."""
+    rng = np.random.default_rng(9)
+    for seqs in ([(1, 700), (1, 90)], [(70, 300)]):
+        st = make_step(rng, seqs, 6, 2, 16)
+        q, cache, start, pos, hq = device_step(mq, st)
+        wide = torch.full((st["T"], 6 * D + 40), 3.0, dtype=torch.float16, device="cuda")
+        wide[:, 16:16 + 6 * D] = q
+        out = torch.full((st["T"], 6 * D + 20), 3.0, dtype=torch.float16, device="cuda")
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            mq.paged_attention(wide[:, 16:16 + 6 * D], cache, start, pos, hq, out=out[:, 4:4 + 6 * D])
+        s.synchronize()
+        check(st, out[:, 4:4 + 6 * D], what="strides")
+        assert bool((out[:, :4] == 3).all()) and bool((out[:, 4 + 6 * D:] == 3).all())
+
+
+def test_long_cache_sampled(mq):
+    """A batch over caches of up to 12000 tokens on the 7B-class heads; every row."""
+    rng = np.random.default_rng(10)
+    st = make_step(rng, [(1, 12000), (1, 5), (2, 7001)], 28, 4, 64)
+    check(st, mq.paged_attention(*device_step(mq, st), 2, 12000), what="long")
+    st = make_step(rng, [(300, 9000)], 28, 4, 64, spans=[(20, 200)])
+    rows = [0, 1, 127, 128, 199, 200, 201, 298, 299]
+    check(st, mq.paged_attention(*device_step(mq, st), 300, 9000), rows=rows, what="long chunk")
+
+
+def test_captured_step_follows_its_lengths(mq):
+    """A captured call replayed while positions, rows per sequence and pages change under it: bounds that hold for all of
+    them are enough.  Eager work runs between the replays."""
+    rng = np.random.default_rng(11)
+    hq, hkv, page, S, T = 14, 2, 16, 3, 3
+    first = make_step(rng, [(1, 600), (1, 600), (1, 600)], hq, hkv, page, poison=False)
+    q, cache, start, pos, _ = device_step(mq, first)
+    ws = torch.empty(max(256, mq.paged_attention_workspace_bytes(T, cache, hq, 3, 600)), dtype=torch.uint8, device="cuda")
+    out = torch.zeros((T, hq * D), dtype=torch.float16, device="cuda")
+    call = lambda: mq.paged_attention(q, cache, start, pos, hq, 3, 600, out=out, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for starts, positions in (([0, 1, 2, 3], [599, 10, 300]), ([0, 3, 3, 3], [0, 1, 2]), ([0, 0, 1, 3], [64, 500, 501]),
+                              ([0, 1, 1, 2], [599, 15, 7])):
+        st = {**first, "start": np.array(starts, dtype=np.int32), "pos": np.array(positions, dtype=np.int32)}
+        start.copy_(dev(st["start"])), pos.copy_(dev(st["pos"]))
+        ws.fill_(0xff)
+        out.fill_(5.0)
+        g.replay()
+        torch.cuda.synchronize()
+        mine = check(st, out, what=f"{starts} {positions}")
+        assert (out.cpu().numpy()[~mine] == 5).all()
+        eager = torch.full_like(out, 5.0)
+        mq.paged_attention(q, cache, start, pos, hq, 3, 600, out=eager)
+        assert torch.equal(eager, out)

@@ -1,0 +1,79 @@
+"""One decoder layer's serving step as a program runs it: qkv linear, adapters on it, norm and rotation with the write
+to the pages, attention over them, o linear, for a prompt in chunks and for generated tokens, against the step in
+fp64 from the fp16 outputs of the linears."""
+import numpy as np
+import pytest
+
+from oracle import mquant_oracle as orc
+from serving import D
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def test_prompt_in_chunks_then_tokens():
+    """Two sequences, one with a visual span, prefilled in chunks of unequal lengths and continued token by token.
+    Tolerance of the attention: 2^-9 of the largest value in the sequence: keys and queries carry the fp16 rounding of the norm's result
+    (2^-11 relative each, a logit of size |q||k| / sqrt(128) <= 12 for unit weights moves by 12 * 2^-10, the output by twice that of the
+    values it averages), probabilities and output theirs."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2502_00425_amd import binding as mq
+    rng = np.random.default_rng(0)
+    hq, hkv, K, page, S = 4, 2, 512, 16, 2
+    N = (hq + 2 * hkv) * D
+    wp = mq.w4_prepack(dev(rng.integers(0, 256, (N, K // 2), dtype=np.uint8)))
+    wscale = dev((0.001 * rng.uniform(0.5, 1.5, N)).astype(np.float16))
+    a, b = (dev((rng.standard_normal(s) * 0.05).astype(np.float16)) for s in ((3, 16, K), (3, N, 16)))
+    a64, b64, lscale = a.cpu().numpy(), b.cpu().numpy(), np.array([0.5, 1.0, 2.0], dtype=np.float32)
+    wq, wk = (rng.uniform(0.5, 1.0, D).astype(np.float16) for _ in range(2))
+    table = np.stack([np.arange(12)[::-1], 12 + np.arange(12)]).astype(np.int32)
+    kp = torch.full((24, hkv, page, D), float("nan"), dtype=torch.float16, device="cuda")
+    vp = torch.full_like(kp, float("inf"))
+    cache = mq.PagedCache(kp, vp, dev(table))
+    keys = [[], []]                                     # per sequence (position, k, v) in fp64
+    steps = [([(70, [(10, 40)]), (33, [])], [2, -1]), ([(41, []), (50, [(0, 30)])], [2, 1]), ([(1, []), (1, [])], [2, 1]),
+             ([(1, []), (0, [])], [0, 1]), ([(3, []), (1, [])], [0, 1])]
+    have = [0, 0]
+    for counts, seq_adapter in steps:
+        T = sum(n for n, _ in counts)
+        x = rng.standard_normal((T, K)).astype(np.float16)
+        start = np.concatenate([[0], np.cumsum([n for n, _ in counts])]).astype(np.int32)
+        perm = np.concatenate([start[s] + orc.aifs_build_perm(n, spans)[0] for s, (n, spans) in enumerate(counts)]).astype(np.int32)
+        pos = np.concatenate([have[s] + orc.aifs_build_perm(n, spans)[0] for s, (n, spans) in enumerate(counts)]).astype(np.int32)
+        ids = np.concatenate([np.full(n, seq_adapter[s]) for s, (n, _) in enumerate(counts)]).astype(np.int32)
+        xq = mq.hadamard_quant_act(dev(x), 0, 0.05, 0.05, 128, perm_dev=dev(perm))
+        qkv = mq.w4a8_gemm(xq, wp, wscale, N, 0, 0.05, 0.05)
+        plain = qkv.cpu().numpy()
+        mq.lora_apply(dev(x), dev(ids), a, b, dev(lscale), qkv, perm_dev=dev(perm), out=qkv)
+        want = orc.lora_f64(x, perm, ids, a64, b64, lscale, plain)
+        got = qkv.cpu().numpy().astype(np.float64)
+        assert (np.abs(got - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -11 * 1e-2).all()
+        q, k, v = qkv[:, :hq * D], qkv[:, hq * D:(hq + hkv) * D], qkv[:, (hq + hkv) * D:]
+        mq.kv_append(q, k, v, cache, dev(start), dev(pos), hq, dev(wq), dev(wk), q_out=q)
+        o = mq.paged_attention(q, cache, dev(start), dev(pos), hq, max(n for n, _ in counts), int(pos.max()) + 1)
+        q64 = orc.qk_norm_rope_f64(got[:, :hq * D], wq, pos, hq)
+        k64 = orc.qk_norm_rope_f64(got[:, hq * D:(hq + hkv) * D], wk, pos, hkv)
+        res = o.cpu().numpy().astype(np.float64)
+        for s, (n, _) in enumerate(counts):
+            rows = np.arange(start[s], start[s + 1])
+            keys[s] += [(int(pos[i]), k64[i], got[i, (hq + hkv) * D:]) for i in rows]
+            if n == 0:
+                continue
+            ps = np.array([p for p, _, _ in keys[s]])
+            kk, vv = np.stack([e for _, e, _ in keys[s]]), np.stack([e for _, _, e in keys[s]])
+            for i in rows:
+                seen = ps <= pos[i]
+                for h in range(hq):
+                    g = h // (hq // hkv)
+                    ref = orc.causal_attention_f64(q64[i:i + 1, h * D:(h + 1) * D], kk[:, g * D:(g + 1) * D], vv[:, g * D:(g + 1) * D],
+                                                   seen[None, :])[0]
+                    assert (np.abs(res[i, h * D:(h + 1) * D] - ref) <= 2.0 ** -9 * 12 * np.abs(vv).max()).all()
+            have[s] += n
+    wo = mq.w4_prepack(dev(rng.integers(0, 256, (K, hq * D // 2), dtype=np.uint8)))
+    oq = mq.hadamard_quant_act(o, 0, 0.05, 0.05, 128)
+    assert torch.isfinite(mq.w4a8_gemm(oq, wo, wscale[:K].contiguous(), K, 0, 0.05, 0.05)).all()
