@@ -27,6 +27,7 @@ static inline int check_cache(const mquant_paged_cache_t *c)
     if (c->n_seq == 0) return MQUANT_OK;
     if (c->n_pages < 1 || c->table_pages < 1) return MQUANT_ERR_BAD_SHAPE;
     if (static_cast<int64_t>(c->table_pages) * c->page_size > 0x7fffffc0ll) return MQUANT_ERR_UNSUPPORTED;     // slots in 32 bits
+    if (static_cast<int64_t>(c->n_pages) * c->n_kv_heads > 0xffffffffll / (c->page_size / 16)) return MQUANT_ERR_UNSUPPORTED;
     if (!c->k_pages_dev || !c->v_pages_dev || !c->page_table_dev) return MQUANT_ERR_NULL;
     if (!aligned_to(c->k_pages_dev, 16) || !aligned_to(c->v_pages_dev, 16) || !aligned_to(c->page_table_dev, 4))
         return MQUANT_ERR_ALIGNMENT;
