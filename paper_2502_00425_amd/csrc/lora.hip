@@ -181,6 +181,8 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
 {
     constexpr int TR = RT * 16;
     __shared__ int32_t list[TR];
+    __shared__ float factors[TR];
+    __shared__ __attribute__((aligned(16))) v8h parts[RT][KS][2][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
     int32_t n = 0;
     const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.x, list, n);
@@ -189,55 +191,67 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
     if (none && p.y == p.base) return;
     __syncthreads();
 
+    // Wave w adds the slices of the rows w, w + 4, ... (16 each), lane's eight ranks at a time, and puts the parts where all waves read them
     const int nsub = (n + 15) / 16;
-    int32_t row[RT];
-    v8h hi[RT][KS], lo[RT][KS];
-    float factor[RT];
     const float scale = none ? 0.0f : p.scale[id];
+    if (!none)
+        for (int t = wave; t < nsub; t += kExpandWaves) {
+            const int j = t * 16 + l16;
+            const float *h = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank + g * 8;
+            const int64_t slice = static_cast<int64_t>(p.T) * p.rank;
+            float f[KS][8], top = 0.0f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
+            for (int32_t c = 0; c < p.slices; ++c, h += slice)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    if (s * 32 + g * 8 < p.rank) {
+                        const v4f h0 = *reinterpret_cast<const v4f *>(h + s * 32), h1 = *reinterpret_cast<const v4f *>(h + s * 32 + 4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            f[s][e] += h0[e];
+                            f[s][4 + e] += h1[e];
+                        }
+                    }
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            int e2 = static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14;   // the largest value below 2^15
+            e2 = e2 < -100 ? -100 : e2;
+            const float down = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
+            if (g == 0) factors[j] = scale * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                v8h hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = f[s][e] * down;
+                    hi[e] = static_cast<_Float16>(v);
+                    lo[e] = static_cast<_Float16>(v - static_cast<float>(hi[e]));
+                }
+                parts[t][s][0][lane] = hi;
+                parts[t][s][1][lane] = lo;
+            }
+        }
+    __syncthreads();
+
+    int32_t row[RT];
+    float factor[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         const int j = t * 16 + l16;
         row[t] = list[j < n ? j : n - 1];
-        if (none || t >= nsub) continue;
-        float f[KS][8], top = 0.0f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int r = s * 32 + g * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
-            if (r < p.rank) {
-                const float *h = p.h + static_cast<int64_t>(row[t]) * p.rank + r;
-                for (int32_t c = 0; c < p.slices; ++c, h += static_cast<int64_t>(p.T) * p.rank) {
-                    const v4f h0 = reinterpret_cast<const v4f *>(h)[0], h1 = reinterpret_cast<const v4f *>(h)[1];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        f[s][e] += h0[e];
-                        f[s][4 + e] += h1[e];
-                    }
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
-        }
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        int e2 = static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14;       // the largest value below 2^15
-        e2 = e2 < -100 ? -100 : e2;
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
-        factor[t] = scale * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = f[s][e] * down;
-                hi[t][s][e] = static_cast<_Float16>(v);
-                lo[t][s][e] = static_cast<_Float16>(v - static_cast<float>(hi[t][s][e]));
-            }
+        factor[t] = factors[j];
     }
     const v8h zero = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int32_t end = p.N < static_cast<int64_t>(blockIdx.z + 1) * p.cols ? p.N : (blockIdx.z + 1) * p.cols;
-    for (int32_t c0 = blockIdx.z * p.cols + wave * kCols; c0 < end; c0 += kExpandWaves * kCols) {
-        v8h bv[4][KS];
+    const int32_t first = blockIdx.z * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols;
+    for (int32_t c0 = first + wave * kCols; c0 < end; c0 += kExpandWaves * kCols) {
+        v8h bv[4][KS], bs[RT][2];
         if (!none)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -247,50 +261,49 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
                 for (int k = 0; k < KS; ++k) bv[s][k] = k * 32 + g * 8 < p.rank ? *reinterpret_cast<const v8h *>(br + k * 32) : zero;
             }
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (t >= nsub) break;
-            const bool mine = t * 16 + l16 < n;
-            const __half *base = p.base + row[t] * p.ldb;
-            __half *out = p.y + row[t] * p.ldy;
-            v8h bs[2] = {zero, zero};
+        for (int t = 0; t < RT; ++t)                           // rows and columns behind the last repeat it, so that no load is a branch
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const int32_t col = c0 + w * 32 + g * 8;
-                if (!mine) continue;
+                const __half *base = p.base + row[t] * p.ldb;
                 if constexpr (VEC) {
-                    if (col < p.N) bs[w] = *reinterpret_cast<const v8h *>(base + col);
+                    bs[t][w] = *reinterpret_cast<const v8h *>(base + (col < p.N ? col : p.N - 8));
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < p.N) bs[w][e] = *reinterpret_cast<const _Float16 *>(base + col + e);
+                    for (int e = 0; e < 8; ++e) bs[t][w][e] = *reinterpret_cast<const _Float16 *>(base + (col + e < p.N ? col + e : p.N - 1));
                 }
             }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            if (t >= nsub) break;
             v4f acc[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
             if (!none)
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
+                for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[s][k], lo[t][k], acc[s], 0, 0, 0);
+                    for (int part = 1; part >= 0; --part) {
+                        const v8h hv = parts[t][k][part][lane];
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[s][k], hi[t][k], acc[s], 0, 0, 0);
-                }
-            if (!mine) continue;
+                        for (int s = 0; s < 4; ++s) acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[s][k], hv, acc[s], 0, 0, 0);
+                    }
+            __half *out = p.y + row[t] * p.ldy;
+            const bool mine = t * 16 + l16 < n;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const int32_t col = c0 + w * 32 + g * 8;
-                v8h r = bs[w];
+                v8h r = bs[t][w];
                 if (!none)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        r[e] = static_cast<_Float16>(__builtin_fmaf(factor[t], acc[w * 2 + (e >> 2)][e & 3], static_cast<float>(bs[w][e])));
+                        r[e] = static_cast<_Float16>(__builtin_fmaf(factor[t], acc[w * 2 + (e >> 2)][e & 3], static_cast<float>(r[e])));
                 if constexpr (VEC) {
-                    if (col < p.N) *reinterpret_cast<v8h *>(out + col) = r;
+                    if (mine && col < p.N) *reinterpret_cast<v8h *>(out + col) = r;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (col + e < p.N) *reinterpret_cast<_Float16 *>(out + col + e) = r[e];
+                        if (mine && col + e < p.N) *reinterpret_cast<_Float16 *>(out + col + e) = r[e];
                 }
             }
         }
@@ -365,7 +378,7 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     const Plan p = make_plan(T, K, rank);
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
-                 n_adapters, p.slices, T <= 64 ? kExpandWaves * kCols : 2 * kExpandWaves * kCols};
+                 n_adapters, p.slices, T <= 64 ? kExpandWaves * kCols : 4 * kExpandWaves * kCols};
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
     const int32_t in_block = T < kBlock ? T : kBlock;
     // tiles of a block: full ones, and a last one of every adapter (and of the rows without)
