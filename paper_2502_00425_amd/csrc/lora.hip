@@ -20,7 +20,7 @@ constexpr int kShrinkWaves = 8;
 constexpr int kUnit = 64;                  // channels of K that a wave takes at a time: a 128-byte line of every row
 constexpr int kExpandWaves = 4;
 constexpr int kCols = 64;                  // columns of y that a wave takes at a time
-constexpr int kMaxSlices = 32;
+constexpr int kMaxSlices = 16;
 
 struct Lora {
     const __half *x;
@@ -97,7 +97,6 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void lora_shrink_kernel(Lora p)
     if (id < 0 || id == p.n_adapters) return;
     __syncthreads();
 
-    const int nsub = (n + 15) / 16;
     int32_t row[RT];                                           // of y, lane l: row l % 16 of each 16
     const __half *xr[RT], *ar[RB];
 #pragma unroll
@@ -106,41 +105,48 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void lora_shrink_kernel(Lora p)
         row[t] = list[j < n ? j : n - 1];
         int32_t src = p.perm ? p.perm[row[t]] : row[t];
         src = src >= 0 && src < p.T ? src : 0;
-        xr[t] = p.x + src * p.ldx + g * 8;
+        xr[t] = p.x + src * p.ldx;
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int r = b * 16 + l16;
-        ar[b] = p.a + (static_cast<int64_t>(id) * p.rank + (r < p.rank ? r : p.rank - 1)) * p.K + g * 8;
+        ar[b] = p.a + (static_cast<int64_t>(id) * p.rank + (r < p.rank ? r : p.rank - 1)) * p.K;
     }
     v4f acc[RT][RB];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int b = 0; b < RB; ++b) acc[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
-    const v8h zero = {0, 0, 0, 0, 0, 0, 0, 0};
     const int32_t units = (p.K + kUnit - 1) / kUnit, slice = blockIdx.z;
     const int32_t u0 = static_cast<int32_t>(static_cast<int64_t>(units) * slice / p.slices);
     const int32_t u1 = static_cast<int32_t>(static_cast<int64_t>(units) * (slice + 1) / p.slices);
-    for (int32_t u = u0 + wave; u < u1; u += kShrinkWaves) {
-        v8h xv[RT][2], av[RB][2];
+    v8h xv[RT][2], av[RB][2];
+    // K is a multiple of 8; what lies behind it in the last unit is read from the row's last 8 channels and multiplied by zero
+    auto load = [&](int32_t u) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int32_t k = u * kUnit + s * 32;
-            const bool in = k + g * 8 < p.K;                   // K is a multiple of 8
+            const int32_t k = u * kUnit + s * 32 + g * 8, at = k < p.K ? k : p.K - 8;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) av[b][s] = in ? *reinterpret_cast<const v8h *>(ar[b] + k) : zero;
+            for (int b = 0; b < RB; ++b) av[b][s] = *reinterpret_cast<const v8h *>(ar[b] + at);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-                if (t < nsub) xv[t][s] = in ? *reinterpret_cast<const v8h *>(xr[t] + k) : zero;
+            for (int t = 0; t < RT; ++t) xv[t][s] = *reinterpret_cast<const v8h *>(xr[t] + at);
         }
+    };
+    auto multiply = [&](int32_t u) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s) {
+            if ((u + 1) * kUnit > p.K && u * kUnit + s * 32 + g * 8 >= p.K)
+#pragma unroll
+                for (int b = 0; b < RB; ++b) av[b][s] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-                if (t < nsub)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[t][s], av[b][s], acc[t][b], 0, 0, 0);
+                for (int b = 0; b < RB; ++b) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[t][s], av[b][s], acc[t][b], 0, 0, 0);
+        }
+    };
+    for (int32_t u = u0 + wave; u < u1; u += kShrinkWaves) {
+        load(u);
+        multiply(u);
     }
     __syncthreads();
 #pragma unroll
@@ -191,77 +197,22 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
     if (none && p.y == p.base) return;
     __syncthreads();
 
-    // Wave w adds the slices of the rows w, w + 4, ... (16 each), lane's eight ranks at a time, and puts the parts where all waves read them
-    const int nsub = (n + 15) / 16;
-    const float scale = none ? 0.0f : p.scale[id];
-    if (!none)
-        for (int t = wave; t < nsub; t += kExpandWaves) {
-            const int j = t * 16 + l16;
-            const float *h = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank + g * 8;
-            const int64_t slice = static_cast<int64_t>(p.T) * p.rank;
-            float f[KS][8], top = 0.0f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
-            for (int32_t c = 0; c < p.slices; ++c, h += slice)
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-                    if (s * 32 + g * 8 < p.rank) {
-                        const v4f h0 = *reinterpret_cast<const v4f *>(h + s * 32), h1 = *reinterpret_cast<const v4f *>(h + s * 32 + 4);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            f[s][e] += h0[e];
-                            f[s][4 + e] += h1[e];
-                        }
-                    }
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            int e2 = static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14;   // the largest value below 2^15
-            e2 = e2 < -100 ? -100 : e2;
-            const float down = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
-            if (g == 0) factors[j] = scale * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                v8h hi, lo;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = f[s][e] * down;
-                    hi[e] = static_cast<_Float16>(v);
-                    lo[e] = static_cast<_Float16>(v - static_cast<float>(hi[e]));
-                }
-                parts[t][s][0][lane] = hi;
-                parts[t][s][1][lane] = lo;
-            }
-        }
-    __syncthreads();
-
     int32_t row[RT];
-    float factor[RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int j = t * 16 + l16;
-        row[t] = list[j < n ? j : n - 1];
-        factor[t] = factors[j];
-    }
-    const v8h zero = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int32_t first = blockIdx.z * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols;
-    for (int32_t c0 = first + wave * kCols; c0 < end; c0 += kExpandWaves * kCols) {
-        v8h bv[4][KS], bs[RT][2];
+    for (int t = 0; t < RT; ++t) row[t] = list[t * 16 + l16 < n ? t * 16 + l16 : n - 1];
+    v8h bv[4][KS], bs[RT][2];
+    // Rows, columns and ranks behind the last repeat it, so that no load is a branch; what they give is multiplied by zero or not stored
+    auto load = [&](int32_t c0) {
         if (!none)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int32_t col = c0 + (s >> 1) * 32 + (l16 >> 2) * 8 + (s & 1) * 4 + (l16 & 3);
-                const __half *br = p.b + (static_cast<int64_t>(id) * p.N + (col < p.N ? col : p.N - 1)) * p.rank + g * 8;
+                const __half *br = p.b + (static_cast<int64_t>(id) * p.N + (col < p.N ? col : p.N - 1)) * p.rank;
 #pragma unroll
-                for (int k = 0; k < KS; ++k) bv[s][k] = k * 32 + g * 8 < p.rank ? *reinterpret_cast<const v8h *>(br + k * 32) : zero;
+                for (int k = 0; k < KS; ++k) bv[s][k] = *reinterpret_cast<const v8h *>(br + (k * 32 + g * 8 < p.rank ? k * 32 + g * 8 : p.rank - 8));
             }
 #pragma unroll
-        for (int t = 0; t < RT; ++t)                           // rows and columns behind the last repeat it, so that no load is a branch
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const int32_t col = c0 + w * 32 + g * 8;
@@ -273,6 +224,94 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
                     for (int e = 0; e < 8; ++e) bs[t][w][e] = *reinterpret_cast<const _Float16 *>(base + (col + e < p.N ? col + e : p.N - 1));
                 }
             }
+    };
+    const int32_t first = blockIdx.z * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols;
+    load(first + wave * kCols);                                // on its way while the rows' parts are prepared
+
+    // The slices of h are added by all waves: wave w takes 16 rows and every SG-th slice; the groups' sums meet in LDS, and one of
+    // them leaves the rows' parts where all waves read them.
+    constexpr int SG = kExpandWaves / RT;
+    const int nsub = (n + 15) / 16;
+    const float scale = none ? 0.0f : p.scale[id];
+    const int t_h = wave / SG, part_h = wave % SG;
+    float f[KS][8];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
+    if (!none && t_h < nsub) {
+        const int j = t_h * 16 + l16;
+        const int64_t slice = static_cast<int64_t>(p.T) * p.rank;
+        const float *h = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank;
+        constexpr int kAtOnce = KS <= 2 ? 4 : 2;
+        for (int32_t c = part_h; c < p.slices; c += kAtOnce * SG) {
+            v4f v[kAtOnce][KS][2];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {                 // ranks and slices behind the last repeat it
+                    const int r = s * 32 + g * 8;
+                    const float *at = h + (c + i * SG < p.slices ? c + i * SG : c) * slice + (r < p.rank ? r : p.rank - 8);
+                    v[i][s][0] = reinterpret_cast<const v4f *>(at)[0];
+                    v[i][s][1] = reinterpret_cast<const v4f *>(at)[1];
+                }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        f[s][e] += c + i * SG < p.slices && s * 32 + g * 8 < p.rank ? v[i][s][e >> 2][e & 3] : 0.0f;
+        }
+    }
+    if constexpr (SG > 1) {
+        __shared__ __attribute__((aligned(16))) float meet[RT][SG - 1][KS][64][8];
+        if (part_h > 0)
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) meet[t_h][part_h - 1][s][lane][e] = f[s][e];
+        __syncthreads();
+        if (part_h == 0)
+#pragma unroll
+            for (int o = 0; o < SG - 1; ++o)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[s][e] += meet[t_h][o][s][lane][e];
+    }
+    if (!none && t_h < nsub && part_h == 0) {
+        float top = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        int e2 = static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14;       // the largest value below 2^15
+        e2 = e2 < -100 ? -100 : e2;
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
+        if (g == 0) factors[t_h * 16 + l16] = scale * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            v8h hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = f[s][e] * down;
+                hi[e] = static_cast<_Float16>(v);
+                lo[e] = static_cast<_Float16>(v - static_cast<float>(hi[e]));
+            }
+            parts[t_h][s][0][lane] = hi;
+            parts[t_h][s][1][lane] = lo;
+        }
+    }
+    __syncthreads();
+
+    float factor[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) factor[t] = factors[t * 16 + l16];
+    for (int32_t c0 = first + wave * kCols; c0 < end; c0 += kExpandWaves * kCols) {
+        if (c0 != first + wave * kCols) load(c0);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             if (t >= nsub) break;
@@ -378,7 +417,7 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     const Plan p = make_plan(T, K, rank);
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
-                 n_adapters, p.slices, T <= 64 ? kExpandWaves * kCols : 4 * kExpandWaves * kCols};
+                 n_adapters, p.slices, T <= 64 ? kExpandWaves * kCols : 2 * kExpandWaves * kCols};
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
     const int32_t in_block = T < kBlock ? T : kBlock;
     // tiles of a block: full ones, and a last one of every adapter (and of the rows without)

@@ -667,7 +667,8 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
 
 // ------------------------------------------------------------------------------------------------ pieces
 //
-// A wave joins the pieces of one query: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p, two channels a lane.  Queries whose slots were
+// A wave joins the pieces of one query: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p; 16 lanes hold its channels, the quarters of the wave
+// take every fourth piece, and 16 pieces are on their way at once.  Queries whose slots were
 // one piece are finished already, those that the other kernel took are its own.
 template <bool CHUNK>
 __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
@@ -702,30 +703,48 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
     }
     const int32_t n = pieces_of(a, limit_of(a, row));
     if (!CHUNK && n <= 1) return;
-    float top = -INFINITY, den = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    float top = -INFINITY;
     for (int32_t p = lane; p < n; p += 64) top = fmaxf(top, a.part_ml[at + p * stride].x);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    for (int32_t p0 = 0; p0 < n; p0 += 64) {
-        float share = 0.0f, l = 0.0f;
-        if (p0 + lane < n) {
-            const float2 ml = a.part_ml[at + (p0 + lane) * stride];
-            share = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ml.x - top) * a.scale_log2e);
-            l = share * ml.y;
+    const int ch = (lane & 15) * 8, quarter = lane >> 4;
+    float den = 0.0f, f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int kAtOnce = 4;
+    for (int32_t p0 = 0; p0 < n; p0 += 4 * kAtOnce) {
+        v4f v[kAtOnce][2];
+        float2 ml[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {                    // pieces behind the last repeat it
+            const int32_t p = p0 + i * 4 + quarter;
+            const int64_t from = at + (p < n ? p : n - 1) * stride;
+            v[i][0] = *reinterpret_cast<const v4f *>(a.part + from * kD + ch);
+            v[i][1] = *reinterpret_cast<const v4f *>(a.part + from * kD + ch + 4);
+            ml[i] = a.part_ml[from];
         }
 #pragma unroll
-        for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x, 64);
-        den += l;
-        const int32_t here = n - p0 < 64 ? n - p0 : 64;
-        for (int32_t p = 0; p < here; ++p) {
-            const float w = __shfl(share, p, 64);
-            const float2 v = *reinterpret_cast<const float2 *>(a.part + (at + (p0 + p) * stride) * kD + lane * 2);
-            o0 = __builtin_fmaf(w, v.x, o0);
-            o1 = __builtin_fmaf(w, v.y, o1);
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (p0 + i * 4 + quarter >= n || ml[i].x == -INFINITY) continue;
+            const float share = __builtin_amdgcn_exp2f((ml[i].x - top) * a.scale_log2e);
+            den = __builtin_fmaf(share, ml[i].y, den);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(share, v[i][e >> 2][e & 3], f[e]);
         }
     }
+    den += __shfl_xor(den, 16, 64);
+    den += __shfl_xor(den, 32, 64);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f[e] += __shfl_xor(f[e], 16, 64);
+        f[e] += __shfl_xor(f[e], 32, 64);
+    }
+    if (quarter != 0) return;
     const float inv = den > 0.0f ? 1.0f / den : 0.0f;
-    *reinterpret_cast<__half2 *>(a.o + row * a.ldo + static_cast<int64_t>(head) * kD + lane * 2) = __floats2half2_rn(o0 * inv, o1 * inv);
+    __half h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = __float2half_rn(f[e] * inv);
+    __half *out = a.o + row * a.ldo + static_cast<int64_t>(head) * kD + ch;
+    reinterpret_cast<uint2 *>(out)[0] = reinterpret_cast<const uint2 *>(h)[0];
+    reinterpret_cast<uint2 *>(out)[1] = reinterpret_cast<const uint2 *>(h)[1];
 }
 
 // ------------------------------------------------------------------------------------------------ dispatch

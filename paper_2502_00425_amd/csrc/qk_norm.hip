@@ -4,8 +4,9 @@
 // For a head x of 128 channels and position p:
 //   u = x * w * (sum(x^2) / 128 + eps)^(-1/2)     (no weight: u = x)
 //   y[2j] = u[2j] cos a - u[2j+1] sin a,  y[2j+1] = u[2j] sin a + u[2j+1] cos a,  a = p * base^(-2j/128)
-// A position of 16384 leaves an fp32 angle accurate to 1e-3 only, so angles and their sines are formed in double;
-// the squares' sum and the products are fp32, and the result is rounded to fp16 once.
+// A position of 16384 leaves an fp32 angle accurate to 1e-3 only, so angles are formed in double, in turns (p * base^(-2j/128) / 2 pi):
+// whole turns are taken off there, what is left, at most half a turn, is rounded to fp32 (2^-22 of a radian) for its sine and
+// cosine.  The squares' sum and the products are fp32, and the result is rounded to fp16 once.
 #include <cmath>
 
 #include "serving_common.h"
@@ -37,7 +38,7 @@ template <bool APPEND, int U>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c, Angles inv)
 {
     const int lane = threadIdx.x & 63;
-    const int32_t i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int32_t i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (i >= a.T) return;
     const int32_t first = blockIdx.y * (4 * U) + (lane >> 4), heads = a.n_q + a.n_k * (APPEND ? 2 : 1);
     const int ch = (lane & 15) * 8;
@@ -66,13 +67,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
                 slot = page * c.page_halves + static_cast<int64_t>(p & ((1 << c.page_shift) - 1)) * kD;
         }
     }
-    double sn, cs;
-    sincos(static_cast<double>(APPEND && a.rope_pos ? a.rope_pos[i] : p) * inv.f[lane], &sn, &cs);
-    float co[4], si[4];
+    const double turns = static_cast<double>(APPEND && a.rope_pos ? a.rope_pos[i] : p) * inv.f[lane];
+    float sn, cs, co[4], si[4];
+    sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        co[e] = __shfl(static_cast<float>(cs), (lane & 15) * 4 + e, 64);
-        si[e] = __shfl(static_cast<float>(sn), (lane & 15) * 4 + e, 64);
+        co[e] = __shfl(cs, (lane & 15) * 4 + e, 64);
+        si[e] = __shfl(sn, (lane & 15) * 4 + e, 64);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -133,10 +134,16 @@ int launch(const Rows &a, const PagedCache &c, double base, hipStream_t stream)
 {
     const int64_t heads = a.n_q + static_cast<int64_t>(a.n_k) * (APPEND ? 2 : 1);
     Angles inv;
-    for (int j = 0; j < kD / 2; ++j) inv.f[j] = pow(base, -2.0 * j / kD);
+    for (int j = 0; j < kD / 2; ++j) inv.f[j] = pow(base, -2.0 * j / kD) * 0.15915494309189533577;
     constexpr int U = 8;
     const int64_t groups = ceil_div(heads, 4 * U);
     if (groups > 65535) return MQUANT_ERR_UNSUPPORTED;
+    // Few rows: a wave for every four heads, since what such a launch waits for is the way of one wave.
+    if (a.T * groups < 1024 && ceil_div(heads, 4) <= 65535) {
+        MQ_LAUNCH((qk_norm_rope_kernel<APPEND, 1>), dim3(static_cast<unsigned>(ceil_div(a.T, 4)), static_cast<unsigned>(ceil_div(heads, 4))),
+                  dim3(256), 0, stream, a, c, inv);
+        return launch_status();
+    }
     MQ_LAUNCH((qk_norm_rope_kernel<APPEND, U>), dim3(static_cast<unsigned>(ceil_div(a.T, 4)), static_cast<unsigned>(groups)), dim3(256), 0,
               stream, a, c, inv);
     return launch_status();
