@@ -226,6 +226,9 @@ def _load_fast():
         ctypes.cast(getattr(lib, "mquant_" + f), ctypes.c_void_p).value
         for f in ("w4a8_linear_prefill", "w4a8_linear_prefill_static", "w4a8_linear_decode", "w4a8_linear_decode_grouped",
                   "w4a8_gemv_grouped", "hadamard_quant_act", "w4g128_gemm")))
+    mod.setup_serving(torch.float16, torch.float32, torch.int32, *(
+        ctypes.cast(getattr(lib, "mquant_" + f), ctypes.c_void_p).value
+        for f in ("qk_norm_rope", "kv_append", "paged_attention", "lora_apply")))
     return mod
 
 
@@ -584,7 +587,7 @@ def w4g128_gemm(x, w_prepacked, N: int, out=None):
 def _operand(t, dtype, what: str, shape=None):
     """A device operand of the serving entries: on the current device, of this type, and of `shape` (contiguous) or
     2-D with unit column stride, whose leading dimension is returned."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected a tensor on the current device")
     if t.dtype is not dtype:
         raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected {dtype}, got {t.dtype}")
@@ -620,6 +623,7 @@ class PagedCache:
         self.struct = PagedCacheStruct(_dp(k_pages), _dp(v_pages), _dp(page_table), self.n_seq, self.n_pages, self.page_size,
                                        self.table_pages, self.n_kv_heads, self.head_dim)
         self.address = ctypes.addressof(self.struct)
+        self.fast = (self.address, self.n_seq, self.n_kv_heads, self.head_dim, self.device_index)
 
 
 def _step(cache, row_start_dev, pos_dev, T: int) -> None:
@@ -627,6 +631,11 @@ def _step(cache, row_start_dev, pos_dev, T: int) -> None:
         raise MQuantError(ERR_UNSUPPORTED, "cache: expected tensors on the current device")
     _operand(row_start_dev, torch.int32, "row_start", (cache.n_seq + 1,))
     _operand(pos_dev, torch.int32, "pos", (T,))
+
+
+def _workspace(ws) -> None:
+    if ws is not None:
+        _operand(ws, ws.dtype, "workspace", tuple(ws.shape))
 
 
 def _weight(w, head_dim: int, what: str) -> None:
@@ -642,6 +651,10 @@ def qk_norm_rope(q, k, q_weight, k_weight, pos_dev, n_q_heads: int, n_kv_heads: 
         q_out = torch.empty((T, n_q_heads * head_dim), dtype=torch.float16, device=q.device)
     if k_out is None:
         k_out = torch.empty((T, n_kv_heads * head_dim), dtype=torch.float16, device=q.device)
+    st = _fast.norm(q, k, q_weight, k_weight, pos_dev, n_q_heads, n_kv_heads, head_dim, eps, base, q_out, k_out)
+    if st is not NotImplemented:
+        _check(st, "mquant_qk_norm_rope")
+        return q_out, k_out
     lds = [_heads(t, n, head_dim, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
                                                                (k, n_kv_heads, "k"), (k_out, n_kv_heads, "k_out"))]
     _weight(q_weight, head_dim, "q_weight"), _weight(k_weight, head_dim, "k_weight")
@@ -658,6 +671,10 @@ def kv_append(q, k, v, cache: PagedCache, row_start_dev, pos_dev, n_q_heads: int
     T, D = q.shape[0], cache.head_dim
     if q_out is None:
         q_out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
+    st = _fast.append(q, k, v, cache.fast, row_start_dev, pos_dev, n_q_heads, q_weight, k_weight, eps, base, rope_pos_dev, q_out)
+    if st is not NotImplemented:
+        _check(st, "mquant_kv_append")
+        return q_out
     lds = [_heads(t, n, D, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
                                                         (k, cache.n_kv_heads, "k"), (v, cache.n_kv_heads, "v"))]
     _weight(q_weight, D, "q_weight"), _weight(k_weight, D, "k_weight")
@@ -684,13 +701,17 @@ def paged_attention(q, cache: PagedCache, row_start_dev, pos_dev, n_q_heads: int
     T, D = q.shape[0], cache.head_dim
     if out is None:
         out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
-    ldq, ldo = _heads(q, n_q_heads, D, T, "q"), _heads(out, n_q_heads, D, T, "out")
-    _step(cache, row_start_dev, pos_dev, T)
     if workspace is None:
         need = paged_attention_workspace_bytes(T, cache, n_q_heads, max_rows, max_kv)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = _fast.attention(q, cache.fast, row_start_dev, pos_dev, n_q_heads, max_rows, max_kv, out, workspace, ws_bytes)
+    if st is not NotImplemented:
+        _check(st, "mquant_paged_attention")
+        return out
+    ldq, ldo = _heads(q, n_q_heads, D, T, "q"), _heads(out, n_q_heads, D, T, "out")
+    _step(cache, row_start_dev, pos_dev, T), _workspace(workspace)
     _check(lib.mquant_paged_attention(_dp(q), ldq, cache.address, _dp(row_start_dev), _dp(pos_dev), _dp(out), ldo, T, n_q_heads,
                                       max_rows, max_kv, _dp(workspace), ws_bytes, _stream()), "mquant_paged_attention")
     return out
@@ -710,17 +731,21 @@ def lora_apply(x, adapter_dev, a, b, scale, base, perm_dev=None, out=None, works
     N, (n_adapters, rank) = base.shape[1], a.shape[:2]
     if out is None:
         out = torch.empty((T, N), dtype=torch.float16, device=x.device)
+    if workspace is None:
+        workspace = torch.empty(max(lora_workspace_bytes(T, K, rank), 256), dtype=torch.uint8, device=x.device)
+    ws_bytes = workspace.numel() * workspace.element_size()
+    st = _fast.lora(x, adapter_dev, a, b, scale, base, perm_dev, out, workspace, ws_bytes)
+    if st is not NotImplemented:
+        _check(st, "mquant_lora_apply")
+        return out
     ldx, ldb, ldy = (_operand(t, torch.float16, what) for t, what in ((x, "x"), (base, "base"), (out, "out")))
     if base.shape[0] != T or tuple(out.shape) != (T, N):
         raise MQuantError(ERR_BAD_SHAPE, f"lora_apply: base and out must be [{T}, {N}]")
     _operand(adapter_dev, torch.int32, "adapter", (T,))
     _operand(a, torch.float16, "a", (n_adapters, rank, K)), _operand(b, torch.float16, "b", (n_adapters, N, rank))
-    _operand(scale, torch.float32, "scale", (n_adapters,))
+    _operand(scale, torch.float32, "scale", (n_adapters,)), _workspace(workspace)
     if perm_dev is not None:
         _operand(perm_dev, torch.int32, "perm", (T,))
-    if workspace is None:
-        workspace = torch.empty(max(lora_workspace_bytes(T, K, rank), 256), dtype=torch.uint8, device=x.device)
-    ws_bytes = workspace.numel() * workspace.element_size()
     _check(lib.mquant_lora_apply(_dp(x), ldx, _dp(perm_dev), _dp(adapter_dev), _dp(a), _dp(b), _dp(scale), _dp(base), ldb,
                                  _dp(out), ldy, T, N, K, rank, n_adapters, _dp(workspace), ws_bytes, _stream()),
            "mquant_lora_apply")

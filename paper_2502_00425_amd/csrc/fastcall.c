@@ -15,7 +15,7 @@
 
 #include "mquant.h"
 
-static PyObject *s_shape, *s_stride, *s_data_ptr, *s_is_contiguous;
+static PyObject *s_shape, *s_stride, *s_data_ptr, *s_is_contiguous, *s_dtype, *s_get_device;
 
 // What setup() gives a module object: torch.cuda.is_initialized, the current device, its raw stream, and the library's
 // entries.  Every load of the package has a module, and so a library, of its own.
@@ -34,6 +34,12 @@ typedef struct {
     int (*quant)(const void *, int64_t, const int32_t *, int8_t *, int32_t, int32_t, int32_t, float, float, int32_t,
                  mquant_stream_t);
     int (*weight_only)(const void *, int64_t, const uint8_t *, void *, int64_t, int32_t, int32_t, int32_t, mquant_stream_t);
+    // setup_serving(): torch.float16, torch.float32, torch.int32 and the entries of the serving step
+    PyObject *f16, *f32, *i32;
+    __typeof__(&mquant_qk_norm_rope) norm;
+    __typeof__(&mquant_kv_append) append;
+    __typeof__(&mquant_paged_attention) attention;
+    __typeof__(&mquant_lora_apply) lora;
 } State;
 
 // ---- readers: 1 on success, 0 where the slow way has to look.  An interrupt, an exit and exhausted memory are nobody's
@@ -125,6 +131,86 @@ static int read_stream(const State *m, mquant_stream_t *s)
     ok = ok && !PyErr_Occurred();
     Py_DECREF(st);
     return ok ? 1 : no();
+}
+
+// ---- operands of the serving entries: of a type, on the current device
+static int read_place(const State *m, int64_t *dev, mquant_stream_t *s)
+{
+    if (!m->f16 || !read_stream(m, s)) return 0;
+    PyObject *r = PyObject_CallNoArgs(m->f_device);
+    if (!r) return no();
+    const int ok = read_i64(r, dev);
+    Py_DECREF(r);
+    return ok;
+}
+
+static int on_device(PyObject *t, int64_t dev)
+{
+    PyObject *r = PyObject_VectorcallMethod(s_get_device, &t, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, NULL);
+    if (!r) return no();
+    int64_t at;
+    const int ok = read_i64(r, &at) && at == dev;
+    Py_DECREF(r);
+    return ok;
+}
+
+static int placed(PyObject *t, const PyObject *dtype, int64_t dev)
+{
+    PyObject *d = PyObject_GetAttr(t, s_dtype);
+    if (!d) return no();
+    Py_DECREF(d);                                              // torch's types live as long as torch
+    return d == dtype && on_device(t, dev);
+}
+
+static int read_workspace(PyObject *t, int64_t dev, void **p)
+{
+    return (t == Py_None || on_device(t, dev)) && read_dense(t, p);
+}
+
+// `rows` rows (-1: any number, but not none) of at least `cols` columns; the stride of a single row says nothing.
+static int read_placed_rows(const State *m, PyObject *t, int64_t dev, int64_t *rows, int64_t cols, void **p, int64_t *ld, int64_t *width)
+{
+    int64_t r;
+    if (!read_rows(t, p, ld, &r, width) || r < 1 || (*rows >= 0 && r != *rows) || *width < cols || !placed(t, m->f16, dev)) return 0;
+    if (r == 1) *ld = (*width + 7) & ~(int64_t)7;
+    *rows = r;
+    return 1;
+}
+
+// A contiguous operand of these sizes (-1: any, which is returned); None is NULL where it may be.
+static int read_placed(PyObject *t, const PyObject *dtype, int64_t dev, int n, int64_t *shape, int may_miss, void **p)
+{
+    *p = NULL;
+    if (t == Py_None) return may_miss;
+    PyObject *s = PyObject_GetAttr(t, s_shape);
+    if (!s) return no();
+    int ok = PyTuple_Check(s) && PyTuple_GET_SIZE(s) == n;
+    for (int i = 0; ok && i < n; ++i) {
+        int64_t v = 0;
+        ok = read_i64(PyTuple_GET_ITEM(s, i), &v) && (shape[i] < 0 || v == shape[i]);
+        shape[i] = v;
+    }
+    Py_DECREF(s);
+    return ok && placed(t, dtype, dev) && read_dense(t, p);
+}
+
+// PagedCache.fast: (address of its descriptor, sequences, key/value heads, channels of a head, device)
+static int read_cache(PyObject *t, int64_t dev, const mquant_paged_cache_t **c, int64_t *n_seq, int64_t *n_kv, int64_t *head_dim)
+{
+    int64_t at;
+    if (!PyTuple_CheckExact(t) || PyTuple_GET_SIZE(t) != 5) return 0;
+    if (!read_i64(PyTuple_GET_ITEM(t, 1), n_seq) || !read_i64(PyTuple_GET_ITEM(t, 2), n_kv) ||
+        !read_i64(PyTuple_GET_ITEM(t, 3), head_dim) || !read_i64(PyTuple_GET_ITEM(t, 4), &at) || at != dev)
+        return 0;
+    *c = PyLong_AsVoidPtr(PyTuple_GET_ITEM(t, 0));
+    return PyErr_Occurred() ? no() : 1;
+}
+
+static int read_f64(PyObject *o, double *v)
+{
+    if (!PyFloat_CheckExact(o)) return 0;
+    *v = PyFloat_AS_DOUBLE(o);
+    return 1;
 }
 
 static int read_size(int64_t v, int32_t *out)
@@ -280,6 +366,122 @@ static PyObject *weight_only(PyObject *self, PyObject *const *a, Py_ssize_t n)
     LAUNCH(m->weight_only(x, ldx, w, y, ldy, T32, N, K32, s));
 }
 
+static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // q, k, q_weight, k_weight, pos, n_q_heads, n_kv_heads, head_dim, eps, base, q_out, k_out
+    void *q, *k, *qw, *kw, *pos, *qo, *ko;
+    int64_t dev, T = -1, ldq, ldk, ldqo, ldko, w;
+    int32_t T32, n_q, n_kv, D;
+    float eps;
+    double base;
+    mquant_stream_t s;
+    if (n != 12 || !read_place(m, &dev, &s) || !read_i32(a[5], &n_q) || !read_i32(a[6], &n_kv) || !read_i32(a[7], &D) || n_q < 1 ||
+        n_kv < 1 || D < 1 || !read_f32(a[8], &eps) || !read_f64(a[9], &base))
+        SLOW_WAY;
+    int64_t one = D;
+    if (!read_placed_rows(m, a[0], dev, &T, (int64_t)n_q * D, &q, &ldq, &w) ||
+        !read_placed_rows(m, a[1], dev, &T, (int64_t)n_kv * D, &k, &ldk, &w) ||
+        !read_placed_rows(m, a[10], dev, &T, (int64_t)n_q * D, &qo, &ldqo, &w) ||
+        !read_placed_rows(m, a[11], dev, &T, (int64_t)n_kv * D, &ko, &ldko, &w) || !read_size(T, &T32) ||
+        !read_placed(a[2], m->f16, dev, 1, &one, 1, &qw) || !read_placed(a[3], m->f16, dev, 1, &one, 1, &kw) ||
+        !read_placed(a[4], m->i32, dev, 1, &T, 0, &pos))
+        SLOW_WAY;
+    LAUNCH(m->norm(q, ldq, qo, ldqo, k, ldk, ko, ldko, qw, kw, eps, pos, T32, n_q, n_kv, D, base, s));
+}
+
+static PyObject *append(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // q, k, v, cache, row_start, pos, n_q_heads, q_weight, k_weight, eps, base, rope_pos, q_out
+    void *q, *k, *v, *qw, *kw, *start, *pos, *rope, *qo;
+    const mquant_paged_cache_t *c;
+    int64_t dev, T = -1, ldq, ldk, ldv, ldqo, w, n_seq, n_kv, D;
+    int32_t T32, n_q;
+    float eps;
+    double base;
+    mquant_stream_t s;
+    if (n != 13 || !read_place(m, &dev, &s) || !read_cache(a[3], dev, &c, &n_seq, &n_kv, &D) || !read_i32(a[6], &n_q) || n_q < 1 ||
+        !read_f32(a[9], &eps) || !read_f64(a[10], &base))
+        SLOW_WAY;
+    int64_t starts = n_seq + 1, one = D;
+    if (!read_placed_rows(m, a[0], dev, &T, n_q * D, &q, &ldq, &w) || !read_placed_rows(m, a[1], dev, &T, n_kv * D, &k, &ldk, &w) ||
+        !read_placed_rows(m, a[2], dev, &T, n_kv * D, &v, &ldv, &w) || !read_placed_rows(m, a[12], dev, &T, n_q * D, &qo, &ldqo, &w) ||
+        !read_size(T, &T32) || !read_placed(a[4], m->i32, dev, 1, &starts, 0, &start) || !read_placed(a[5], m->i32, dev, 1, &T, 0, &pos) ||
+        !read_placed(a[7], m->f16, dev, 1, &one, 1, &qw) || !read_placed(a[8], m->f16, dev, 1, &one, 1, &kw) ||
+        !read_placed(a[11], m->i32, dev, 1, &T, 1, &rope))
+        SLOW_WAY;
+    LAUNCH(m->append(q, ldq, qo, ldqo, k, ldk, v, ldv, qw, kw, eps, start, pos, rope, T32, n_q, base, c, s));
+}
+
+static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // q, cache, row_start, pos, n_q_heads, max_rows, max_kv, out, workspace, its bytes
+    void *q, *start, *pos, *o, *work;
+    const mquant_paged_cache_t *c;
+    int64_t dev, T = -1, ldq, ldo, w, n_seq, n_kv, D, bytes;
+    int32_t T32, n_q, max_rows, max_kv;
+    mquant_stream_t s;
+    if (n != 10 || !read_place(m, &dev, &s) || !read_cache(a[1], dev, &c, &n_seq, &n_kv, &D) || !read_i32(a[4], &n_q) || n_q < 1 ||
+        !read_i32(a[5], &max_rows) || !read_i32(a[6], &max_kv) || !read_i64(a[9], &bytes))
+        SLOW_WAY;
+    int64_t starts = n_seq + 1;
+    if (!read_placed_rows(m, a[0], dev, &T, n_q * D, &q, &ldq, &w) || !read_placed_rows(m, a[7], dev, &T, n_q * D, &o, &ldo, &w) ||
+        !read_size(T, &T32) || !read_placed(a[2], m->i32, dev, 1, &starts, 0, &start) || !read_placed(a[3], m->i32, dev, 1, &T, 0, &pos) ||
+        !read_workspace(a[8], dev, &work))
+        SLOW_WAY;
+    LAUNCH(m->attention(q, ldq, c, start, pos, o, ldo, T32, n_q, max_rows, max_kv, work, bytes, s));
+}
+
+static PyObject *lora(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // x, adapter, a, b, scale, base, perm, out, workspace, its bytes
+    void *x, *id, *pa, *pb, *scale, *base, *perm, *y, *work;
+    int64_t dev, T = -1, ldx, ldb, ldy, K, N, wy, bytes, count = -1;
+    int32_t T32, N32, K32, rank32, n32;
+    mquant_stream_t s;
+    if (n != 10 || !read_place(m, &dev, &s) || !read_placed_rows(m, a[0], dev, &T, 0, &x, &ldx, &K) ||
+        !read_placed_rows(m, a[5], dev, &T, 0, &base, &ldb, &N) || !read_placed_rows(m, a[7], dev, &T, N, &y, &ldy, &wy) || wy != N ||
+        !read_i64(a[9], &bytes))
+        SLOW_WAY;
+    int64_t sa[3] = {-1, -1, K};
+    if (!read_placed(a[2], m->f16, dev, 3, sa, 0, &pa)) SLOW_WAY;
+    int64_t sb[3] = {sa[0], N, sa[1]};
+    count = sa[0];
+    if (!read_placed(a[3], m->f16, dev, 3, sb, 0, &pb) || !read_placed(a[4], m->f32, dev, 1, &count, 0, &scale) ||
+        !read_placed(a[1], m->i32, dev, 1, &T, 0, &id) || !read_placed(a[6], m->i32, dev, 1, &T, 1, &perm) ||
+        !read_workspace(a[8], dev, &work) ||
+        !read_size(T, &T32) || !read_size(N, &N32) || !read_size(K, &K32) || !read_size(sa[1], &rank32) || !read_size(count, &n32))
+        SLOW_WAY;
+    LAUNCH(m->lora(x, ldx, perm, id, pa, pb, scale, base, ldb, y, ldy, T32, N32, K32, rank32, n32, work, bytes, s));
+}
+
+// setup_serving(float16, float32, int32, addresses of the four entries in the order of State), behind setup()
+static PyObject *setup_serving(PyObject *self, PyObject *args)
+{
+    PyObject *f16, *f32, *i32, *addr[4];
+    if (!PyArg_ParseTuple(args, "OOOO!O!O!O!", &f16, &f32, &i32, &PyLong_Type, &addr[0], &PyLong_Type, &addr[1], &PyLong_Type, &addr[2],
+                          &PyLong_Type, &addr[3]))
+        return NULL;
+    void *p[4];
+    for (int i = 0; i < 4; ++i) {
+        p[i] = PyLong_AsVoidPtr(addr[i]);
+        if (PyErr_Occurred()) return NULL;
+    }
+    State *m = PyModule_GetState(self);
+    *(void **)&m->norm = p[0];
+    *(void **)&m->append = p[1];
+    *(void **)&m->attention = p[2];
+    *(void **)&m->lora = p[3];
+    Py_INCREF(f16), Py_INCREF(f32), Py_INCREF(i32);
+    Py_XSETREF(m->f32, f32);
+    Py_XSETREF(m->i32, i32);
+    Py_XSETREF(m->f16, f16);
+    Py_RETURN_NONE;
+}
+
 // setup(is_initialized, device, raw stream, addresses of the seven entries of the library in the order of State)
 static PyObject *setup(PyObject *self, PyObject *args)
 {
@@ -311,7 +513,8 @@ static PyObject *setup(PyObject *self, PyObject *args)
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     ENTRY(prefill), ENTRY(prefill_static), ENTRY(decode), ENTRY(decode_grouped), ENTRY(gemv_grouped), ENTRY(quant),
-    ENTRY(weight_only), {"setup", setup, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL},
+    ENTRY(weight_only), ENTRY(norm), ENTRY(append), ENTRY(attention), ENTRY(lora), {"setup", setup, METH_VARARGS, NULL},
+    {"setup_serving", setup_serving, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL},
 };
 
 static int traverse(PyObject *self, visitproc visit, void *arg)
@@ -320,6 +523,9 @@ static int traverse(PyObject *self, visitproc visit, void *arg)
     Py_VISIT(m->f_initialized);
     Py_VISIT(m->f_device);
     Py_VISIT(m->f_stream);
+    Py_VISIT(m->f16);
+    Py_VISIT(m->f32);
+    Py_VISIT(m->i32);
     return 0;
 }
 
@@ -329,6 +535,9 @@ static int clear(PyObject *self)
     Py_CLEAR(m->f_stream);                     // first: a module without it takes no call
     Py_CLEAR(m->f_initialized);
     Py_CLEAR(m->f_device);
+    Py_CLEAR(m->f16);
+    Py_CLEAR(m->f32);
+    Py_CLEAR(m->i32);
     return 0;
 }
 
@@ -338,7 +547,9 @@ static int start(PyObject *self)
     s_stride = PyUnicode_InternFromString("stride");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-    return s_shape && s_stride && s_data_ptr && s_is_contiguous ? 0 : -1;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    return s_shape && s_stride && s_data_ptr && s_is_contiguous && s_dtype && s_get_device ? 0 : -1;
 }
 
 static PyModuleDef_Slot slots[] = {{Py_mod_exec, start}, {0, NULL}};
