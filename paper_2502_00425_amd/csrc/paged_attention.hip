@@ -86,11 +86,12 @@ __device__ __forceinline__ int32_t limit_of(const Step &a, int32_t row)
     return p < 0 ? -1 : p < last ? p : last;
 }
 
-// The 16 slots block * 16 .. of a sequence, as the number of 4 KiB blocks before them in a page array; a block behind
-// `last` repeats it, a page id out of range is page 0.
-__device__ __forceinline__ uint32_t block_at(const Step &a, int32_t seq, int32_t kvh, int32_t block, int32_t last)
+// The 16 slots block * 16 .. of a sequence, as the number of 4 KiB blocks before them in a page array.  A block behind the table
+// repeats its last one, a page id out of range is page 0: any block is memory of the cache, and what a row does not see
+// is not used.
+__device__ __forceinline__ uint32_t block_at(const Step &a, int32_t seq, int32_t kvh, int32_t block)
 {
-    const int32_t b = block < last ? block : last, shift = a.c.page_shift - 4;
+    const int32_t shift = a.c.page_shift - 4, last = (a.c.table_pages << shift) - 1, b = block < last ? block : last;
     const int32_t id = a.c.table[static_cast<int64_t>(seq) * a.c.table_pages + (b >> shift)];
     const uint32_t page = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.c.n_pages) ? id : 0;
     return (page * static_cast<uint32_t>(a.c.n_kv_heads) + kvh) * (1u << shift) + (b & ((1 << shift) - 1));
@@ -144,34 +145,34 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
         const int nq = M - m0 < 16 * NQ ? (M - m0 + 15) / 16 : NQ;
         const bool split = m0 + 16 * NQ <= a.few_stride;       // the others' slots are all in piece 0
         if (!split && piece > 0) return;
+        // page ids, queries and positions are on their way together
+        const int32_t begin = split ? piece * a.piece : 0;     // slots, a multiple of kFewStep
+        const int32_t first = begin / kFewSlots + wave;
+        // lane 2 i + b: block b of this wave's tile i; 32 tiles (4096 slots of the work-group) a time
+        auto blocks_from = [&](int32_t tile0) { return block_at(a, seq, kvh, (tile0 + (lane >> 1) * kFewWaves) * 2 + (lane & 1)); };
+        uint32_t blocks = blocks_from(first);
+        v8h qf[NQ][4];
         int32_t lim[NQ], top = -1, low = INT_MAX;
-        const __half *qp[NQ];
 #pragma unroll
         for (int u = 0; u < NQ; ++u) {
             const int32_t m = m0 + u * 16 + l16, mc = m < M ? m : M - 1;
             const int32_t row = rows.x + mc / a.group;
-            qp[u] = a.q + row * a.ldq + static_cast<int64_t>(kvh * a.group + mc % a.group) * kD + g * 8;
+            const __half *qp = a.q + row * a.ldq + static_cast<int64_t>(kvh * a.group + mc % a.group) * kD + g * 8;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) qf[u][ks] = *reinterpret_cast<const v8h *>(qp + ks * 32);
             lim[u] = limit_of(a, row);
+        }
+#pragma unroll
+        for (int u = 0; u < NQ; ++u) {
             top = lim[u] > top ? lim[u] : top;
             low = lim[u] < low ? lim[u] : low;
         }
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) {
-            top = max(top, __shfl_xor(top, x, 64));
-            low = min(low, __shfl_xor(low, x, 64));
-        }
-        top = uniform(top);
-        low = uniform(low);
-        const int32_t begin = split ? piece * a.piece : 0;     // slots, a multiple of kFewStep
+        top = uniform(row16_max(top));
+        low = uniform(row16_min(low));
         if (begin > top && piece > 0) continue;
         const int32_t end = !split || piece == a.n_split - 1 || top < begin + a.piece ? top + 1 : begin + a.piece;
-        const int32_t first = begin / kFewSlots + wave, n_tiles = (end + kFewSlots - 1) / kFewSlots, last_block = top >> 4;
+        const int32_t n_tiles = (end + kFewSlots - 1) / kFewSlots;
 
-        v8h qf[NQ][4];
-#pragma unroll
-        for (int u = 0; u < NQ; ++u)
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) qf[u][ks] = *reinterpret_cast<const v8h *>(qp[u] + ks * 32);
         v4f acc[NQ][8];
         float m_ref[NQ], l_run[NQ];
 #pragma unroll
@@ -182,9 +183,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
             for (int cb = 0; cb < 8; ++cb) acc[u][cb] = v4f{0.f, 0.f, 0.f, 0.f};
         }
         const float lazy_raw = kLazy / a.scale_log2e;
-        // lane 2 i + b: block b of this wave's tile i; 32 tiles (4096 slots of the work-group) a time
         for (int32_t tile0 = first; tile0 < n_tiles; tile0 += 32 * kFewWaves) {
-            const uint32_t blocks = block_at(a, seq, kvh, (tile0 + (lane >> 1) * kFewWaves) * 2 + (lane & 1), last_block);
+            if (tile0 != first) blocks = blocks_from(tile0);
             auto copy = [&](const __half *pages, const uint32_t (&off)[4], uint32_t lds, int it) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -427,7 +427,6 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
     const int32_t t0 = piece * piece_tiles, t_all = (top + kChunkK) / kChunkK;             // top = -1: none
     if (t0 >= t_all && piece > 0) return;
     const int32_t t_end = piece == a.n_split - 1 || t_all < t0 + piece_tiles ? t_all : t0 + piece_tiles;
-    const int32_t last_block = top > 0 ? top >> 4 : 0;
 
     v8h qf[kD / 16];
     {
@@ -443,7 +442,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
     const uint32_t k_off = c_row * 256 + (((lane & 15) ^ (c_row & 15)) << 4);
     const uint32_t v_off = c_row * 256 + (((lane & 15) ^ ((c_row & 3) << 2)) << 4);
     // lane l: block 64 j + l for the keys' and for the values' tile, and the next 64 on their way
-    auto blocks_from = [&](int32_t b) { return block_at(a, seq, kvh, b + lane, last_block); };
+    auto blocks_from = [&](int32_t b) { return block_at(a, seq, kvh, b + lane); };
     const int32_t b0 = t0 * 4;
     uint32_t k_blocks = blocks_from(b0), v_blocks = k_blocks, n_blocks = blocks_from(b0 + 64);
     auto dma_k = [&](int32_t t, int b) {

@@ -32,19 +32,30 @@ struct Rows {
     int32_t T, n_q, n_k;
 };
 
-// A wave takes one row and U groups of four heads (queries first, then keys, then values): 16 lanes a head, 16 bytes
-// a lane.  Lane l forms the angle of pair l, every lane then takes the four pairs it holds, the same ones in all its heads.
+// A wave takes one row and `per` (at most U) groups of four heads (queries first, then keys, then values): 16 lanes a head, 16
+// bytes a lane.  Lane l forms the angle of pair l, every lane then takes the four pairs it holds, the same ones in all its
+// heads.  `waves` waves share a row and lie next to each other, so that rows are read and written from end to end.
+// Rows that fill the chip go past the caches (72 heads of 16384 rows 121.7 -> 107.5 us, 36 of 4096 with the append 17.8 ->
+// 14.9): lines that are written whole need not be looked up there.  Few rows stay, the next kernel reads them.
+template <bool PAST>
+__device__ __forceinline__ void put(__half *p, v8h v)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<v8h *>(p));
+    else *reinterpret_cast<v8h *>(p) = v;
+}
+
 template <bool APPEND, int U>
-__global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c, Angles inv)
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c, Angles inv, int32_t waves, int32_t per)
 {
     const int lane = threadIdx.x & 63;
-    const int32_t i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t i = static_cast<int32_t>(item / waves);
     if (i >= a.T) return;
-    const int32_t first = blockIdx.y * (4 * U) + (lane >> 4), heads = a.n_q + a.n_k * (APPEND ? 2 : 1);
+    const int32_t part = static_cast<int32_t>(item % waves);
+    const int32_t first = part * per * 4 + (lane >> 4), all = a.n_q + a.n_k * (APPEND ? 2 : 1);
+    const int32_t heads = all < (part + 1) * per * 4 ? all : (part + 1) * per * 4;         // this wave's end
     const int ch = (lane & 15) * 8;
     const int32_t p = a.pos[i];
-    const int32_t seq = APPEND ? sequence_of_row(a.row_start, c.n_seq, i) : 0;
-    if (seq < 0) return;
     v8h x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -55,6 +66,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
         x[u] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
         if (h < heads) x[u] = *reinterpret_cast<const v8h *>(row + ch);
     }
+    const int32_t seq = APPEND ? sequence_of_row(a.row_start, c.n_seq, i) : 0;
+    if (seq < 0) return;
     // the row's slot
     int64_t slot = -1;                                          // halves from a page array's start to head 0's row
     int32_t head_stride = 0;
@@ -78,7 +91,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t h = first + u * 4;
-        const bool is_q = h < a.n_q, is_v = APPEND && h >= a.n_q + a.n_k;
+        if (U > 1 && u >= per) break;
+        const bool is_q = h < a.n_q && h < heads, is_v = APPEND && h >= a.n_q + a.n_k;
         const __half *w = is_q ? a.q_weight : a.k_weight;
         float f[8], sum = 0.0f;
 #pragma unroll
@@ -86,8 +100,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
             f[e] = static_cast<float>(x[u][e]);
             sum = __builtin_fmaf(f[e], f[e], sum);
         }
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) sum += __shfl_xor(sum, m, 64);
+        sum = row16_sum(sum);
         if (w && h < heads && !is_v) {
             const float r = 1.0f / sqrtf(sum * (1.0f / kD) + a.eps);
             const v8h wt = *reinterpret_cast<const v8h *>(w + ch);
@@ -101,12 +114,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
             y[2 * e + 1] = static_cast<_Float16>(f[2 * e] * si[e] + f[2 * e + 1] * co[e]);
         }
         if (is_q) {
-            *reinterpret_cast<v8h *>(a.q_out + i * a.ldqo + static_cast<int64_t>(h) * kD + ch) = y;
+            put<(U > 1)>(a.q_out + i * a.ldqo + static_cast<int64_t>(h) * kD + ch, y);
         } else if (!APPEND) {
-            if (h < heads) *reinterpret_cast<v8h *>(a.k_out + i * a.ldko + static_cast<int64_t>(h - a.n_q) * kD + ch) = y;
+            if (h < heads) put<(U > 1)>(a.k_out + i * a.ldko + static_cast<int64_t>(h - a.n_q) * kD + ch, y);
         } else if (h < heads && slot >= 0) {
-            if (is_v) *reinterpret_cast<v8h *>(c.v + slot + static_cast<int64_t>(h - a.n_q - a.n_k) * head_stride + ch) = x[u];
-            else *reinterpret_cast<v8h *>(c.k + slot + static_cast<int64_t>(h - a.n_q) * head_stride + ch) = y;
+            if (is_v) put<(U > 1)>(c.v + slot + static_cast<int64_t>(h - a.n_q - a.n_k) * head_stride + ch, x[u]);
+            else put<(U > 1)>(c.k + slot + static_cast<int64_t>(h - a.n_q) * head_stride + ch, y);
         }
     }
 }
@@ -134,18 +147,24 @@ int launch(const Rows &a, const PagedCache &c, double base, hipStream_t stream)
 {
     const int64_t heads = a.n_q + static_cast<int64_t>(a.n_k) * (APPEND ? 2 : 1);
     Angles inv;
-    for (int j = 0; j < kD / 2; ++j) inv.f[j] = pow(base, -2.0 * j / kD) * 0.15915494309189533577;
-    constexpr int U = 8;
-    const int64_t groups = ceil_div(heads, 4 * U);
-    if (groups > 65535) return MQUANT_ERR_UNSUPPORTED;
-    // Few rows: a wave for every four heads, since what such a launch waits for is the way of one wave.
-    if (a.T * groups < 1024 && ceil_div(heads, 4) <= 65535) {
-        MQ_LAUNCH((qk_norm_rope_kernel<APPEND, 1>), dim3(static_cast<unsigned>(ceil_div(a.T, 4)), static_cast<unsigned>(ceil_div(heads, 4))),
-                  dim3(256), 0, stream, a, c, inv);
-        return launch_status();
-    }
-    MQ_LAUNCH((qk_norm_rope_kernel<APPEND, U>), dim3(static_cast<unsigned>(ceil_div(a.T, 4)), static_cast<unsigned>(groups)), dim3(256), 0,
-              stream, a, c, inv);
+    // base^(-2j/128) / 2 pi, each from the one before in 64-bit fractions (off by 2^-57 at most; 64 calls of pow cost the host 1.3 us)
+    const long double ratio = powl(static_cast<long double>(base), -2.0L / kD);
+    long double f = 0.159154943091895335768883763372514362L;
+    for (int j = 0; j < kD / 2; ++j, f *= ratio) inv.f[j] = static_cast<double>(f);
+    // A wave takes four heads where rows are few, since what such a launch waits for is the way of one wave, else up to 16.  Waves of 4 /
+    // of up to 16 heads, 32 heads: 512 rows 4.1 / 4.7 us, 700 5.0 / 5.0, 1024 5.8 / 5.3, 4096 15.0 / 11.6; 72 heads: 256 4.4 / 5.0, 512 6.2 / 6.0.
+    // (Up to 12 heads at 72 of 16384 rows 102.4 us, 16 101.1: 6.0 TB/s, 20 103.6, 40 107.3; 32 of 4096 12.8, 11.6, 12.3, 12.2.)
+    constexpr int U = 4;
+    const int64_t groups = ceil_div(heads, 4);
+    int64_t waves = ceil_div(groups, U);
+    const bool few = a.T * groups < 6000;
+    if (few) waves = groups;
+    const int64_t blocks = ceil_div(a.T * waves, 4);
+    if (blocks > 0x7fffffff || heads > 1 << 20) return MQUANT_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(blocks));
+    const int32_t per = static_cast<int32_t>(ceil_div(groups, waves)), n = static_cast<int32_t>(waves);
+    if (few) MQ_LAUNCH((qk_norm_rope_kernel<APPEND, 1>), grid, dim3(256), 0, stream, a, c, inv, n, per);
+    else MQ_LAUNCH((qk_norm_rope_kernel<APPEND, U>), grid, dim3(256), 0, stream, a, c, inv, n, per);
     return launch_status();
 }
 

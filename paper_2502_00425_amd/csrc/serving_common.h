@@ -41,6 +41,24 @@ static inline PagedCache cache_args(const mquant_paged_cache_t *c)
             static_cast<int64_t>(c->n_kv_heads) * c->page_size * kCacheHeadDim};
 }
 
+// Over the 16 lanes of a row, all of which get the result: rotations by 8, 4, 2 and 1 inside the register file (through LDS, as
+// general lane exchanges go, each of the four takes the latency of an LDS read).
+template <typename F>
+__device__ __forceinline__ int row16(int x, F f)
+{
+    x = f(x, __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(x, x, 0x124, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(x, x, 0x122, 0xf, 0xf, false));
+    return f(x, __builtin_amdgcn_update_dpp(x, x, 0x121, 0xf, 0xf, false));
+}
+
+__device__ __forceinline__ float row16_sum(float x)
+{
+    return __int_as_float(row16(__float_as_int(x), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
+__device__ __forceinline__ int32_t row16_max(int32_t x) { return row16(x, [](int a, int b) { return a > b ? a : b; }); }
+__device__ __forceinline__ int32_t row16_min(int32_t x) { return row16(x, [](int a, int b) { return a < b ? a : b; }); }
+
 // Sequence of row i: the number of sequences that start at or before it, less one; -1 for a row of none.  A wave looks at
 // 64 starts at a time (row_start does not decrease).
 __device__ __forceinline__ int32_t sequence_of_row(const int32_t *__restrict__ row_start, int32_t n_seq, int32_t i)
