@@ -28,6 +28,16 @@ __device__ __forceinline__ void lds_dma16_uniform_base(const uint8_t *base_unifo
                  : "memory", "m0");
 }
 
+// The same with a 64-bit address per lane: rows that lie anywhere.
+__device__ __forceinline__ void lds_dma16_lane_address(const void *lane_address, uint32_t lds_wave_base)
+{
+    const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds_wave_base);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(m0v), "v"(reinterpret_cast<uint64_t>(lane_address))
+                 : "memory", "m0");
+}
+
 // 4 bytes per lane, global -> LDS; LDS address = wave-uniform base + lane * 4.
 __device__ __forceinline__ void lds_dma4_uniform_base(const uint8_t *base_uniform, uint32_t lane_offset,
                                                       uint32_t lds_wave_base)

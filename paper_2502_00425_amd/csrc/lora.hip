@@ -6,6 +6,7 @@
 // rows, of the adapters.
 #include <hip/hip_fp16.h>
 
+#include "lds_dma.h"
 #include "mquant_internal.h"
 
 using namespace mquant;
@@ -83,6 +84,27 @@ __device__ __forceinline__ int32_t find_tile(const Lora &p, int32_t row0, int32_
     return cur;
 }
 
+// h in two fp16 parts of h 2^-e: e from the largest value of a row, so that this lies below 2^15.
+__device__ __forceinline__ void scale_of(float &top, float &down, float &up)
+{
+    top = fmaxf(top, __shfl_xor(top, 16, 64));                 // a row's ranks are spread over the lane groups
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    int e = static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14;
+    e = e < -100 ? -100 : e;
+    down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+}
+
+__device__ __forceinline__ void split(const float (&f)[8], float down, v8h &hi, v8h &lo)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float v = f[e] * down;
+        hi[e] = static_cast<_Float16>(v);
+        lo[e] = static_cast<_Float16>(v - static_cast<float>(hi[e]));
+    }
+}
+
 // h of one tile and slice of K.  The waves take units of 64 channels in turn: x rows are the A operand, rows of A_a the B
 // operand of 16x16x32 products, both straight from memory (16 bytes a lane), and their sums meet in LDS by halves.
 template <int RT, int RB>
@@ -93,7 +115,7 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void lora_shrink_kernel(Lora p)
     int32_t *list = reinterpret_cast<int32_t *>(sums);         // until the sums meet
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
     int32_t n = 0;
-    const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.x, list, n);
+    const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
     if (id < 0 || id == p.n_adapters) return;
     __syncthreads();
 
@@ -117,7 +139,7 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void lora_shrink_kernel(Lora p)
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int b = 0; b < RB; ++b) acc[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
-    const int32_t units = (p.K + kUnit - 1) / kUnit, slice = blockIdx.z;
+    const int32_t units = (p.K + kUnit - 1) / kUnit, slice = blockIdx.x;
     const int32_t u0 = static_cast<int32_t>(static_cast<int64_t>(units) * slice / p.slices);
     const int32_t u1 = static_cast<int32_t>(static_cast<int64_t>(units) * (slice + 1) / p.slices);
     v8h xv[RT][2], av[RB][2];
@@ -191,7 +213,7 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
     __shared__ __attribute__((aligned(16))) v8h parts[RT][KS][2][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
     int32_t n = 0;
-    const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.x, list, n);
+    const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
     if (id < 0) return;
     const bool none = id == p.n_adapters;
     if (none && p.y == p.base) return;
@@ -225,7 +247,7 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
                 }
             }
     };
-    const int32_t first = blockIdx.z * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols;
+    const int32_t first = blockIdx.x * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols;
     load(first + wave * kCols);                                // on its way while the rows' parts are prepared
 
     // The slices of h are added by all waves: wave w takes 16 rows and every SG-th slice; the groups' sums meet in LDS, and one of
@@ -286,21 +308,13 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        int e2 = static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14;       // the largest value below 2^15
-        e2 = e2 < -100 ? -100 : e2;
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
-        if (g == 0) factors[t_h * 16 + l16] = scale * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
+        float down, up;
+        scale_of(top, down, up);
+        if (g == 0) factors[t_h * 16 + l16] = scale * up;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             v8h hi, lo;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = f[s][e] * down;
-                hi[e] = static_cast<_Float16>(v);
-                lo[e] = static_cast<_Float16>(v - static_cast<float>(hi[e]));
-            }
+            split(f[s], down, hi, lo);
             parts[t_h][s][0][lane] = hi;
             parts[t_h][s][1][lane] = lo;
         }
@@ -349,40 +363,302 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
     }
 }
 
-// Rows of a tile and slices of K.  Few rows: tiles of 16, and slices short enough that each wave has about one unit; more: tiles of 64
-// (32 at ranks beyond 64: 64 accumulator registers either way), and as many slices as give every compute unit a work-group.
+// ------------------------------------------------------------------------------------------------ many rows
+//
+// Tiles of 64 rows, 16 a wave.  Straight loads of operands take 64 bytes of each of 16 rows an instruction, and the
+// path to the registers then moves 15 bytes a clock (37 GB/s a compute unit, measured with 8 waves and 16 KiB in flight
+// each); so here all that is read goes 256 bytes of a row at a time, by LDS-DMA or with 16 lanes to a row.
+typedef const v8h __attribute__((address_space(3))) *v8h_lds_ptr;
+constexpr int kRows = 64;
+constexpr int kStage = 128;                // channels of K in LDS at a time, two buffers
+
+template <int N>
+__device__ __forceinline__ void wait_copies()
+{
+    wait_vmcnt<N>();
+    asm volatile("" ::: "memory");
+}
+
+// h of 64 rows and a slice of K.  Chunk c (16 bytes) of row r lies at chunk c ^ (r & 15): a fragment read takes one chunk of 16 rows.
+template <int RB>
+__global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];           // two of: 64 rows of x, RB * 16 rows of A_a, 256 bytes each
+    __shared__ int32_t list[kRows];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
+    int32_t n = 0;
+    const int32_t id = find_tile<kRows>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
+    if (id < 0 || id == p.n_adapters) return;
+    __syncthreads();
+
+    constexpr int kBuffer = (kRows + RB * 16) * 256;
+    const uint32_t lds0 = lds_address(smem);
+    const __half *xr[4], *ar[RB];                              // where this lane copies from: rows 4 i + g of the wave's 16, of each 16 of A_a
+    int32_t xc[4], ac;                                         // and which chunk of them
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = wave * 16 + i * 4 + g;
+        const int32_t row = list[j < n ? j : n - 1];
+        int32_t src = p.perm ? p.perm[row] : row;
+        src = src >= 0 && src < p.T ? src : 0;
+        xr[i] = p.x + src * p.ldx;
+        xc[i] = (l16 ^ (i * 4 + g)) * 8;
+    }
+    ac = (l16 ^ (wave * 4 + g)) * 8;
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int r = b * 16 + wave * 4 + g;
+        ar[b] = p.a + (static_cast<int64_t>(id) * p.rank + (r < p.rank ? r : p.rank - 1)) * p.K;
+    }
+    auto copy = [&](int32_t stage, int buffer) {               // channels behind K repeat its last 8
+        const int32_t k = stage * kStage, last = p.K - 8;
+        const uint32_t at = lds0 + buffer * kBuffer;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds_dma16_lane_address(xr[i] + (k + xc[i] < p.K ? k + xc[i] : last), at + (wave * 4 + i) * 1024);
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+            lds_dma16_lane_address(ar[b] + (k + ac < p.K ? k + ac : last), at + kRows * 256 + (b * 4 + wave) * 1024);
+    };
+    const int32_t stages = (p.K + kStage - 1) / kStage, slice = blockIdx.x;
+    const int32_t s0 = static_cast<int32_t>(static_cast<int64_t>(stages) * slice / p.slices);
+    const int32_t s1 = static_cast<int32_t>(static_cast<int64_t>(stages) * (slice + 1) / p.slices);
+    v4f acc[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) acc[b] = v4f{0.f, 0.f, 0.f, 0.f};
+    if (s0 < s1) copy(s0, 0);
+    for (int32_t s = s0; s < s1; ++s) {
+        const int buffer = (s - s0) & 1;
+        if (s + 1 < s1) {
+            copy(s + 1, buffer ^ 1);
+            wait_copies<4 + RB>();
+        } else {
+            wait_copies<0>();
+        }
+        __syncthreads();
+        const uint32_t at = lds0 + buffer * kBuffer + l16 * 256;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const uint32_t chunk = ((ks * 4 + g) ^ l16) << 4;
+            v8h xv = *(v8h_lds_ptr)(uintptr_t)(at + wave * 4096 + chunk);
+            if (s * kStage + ks * 32 + g * 8 >= p.K) xv = v8h{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, *(v8h_lds_ptr)(uintptr_t)(at + kRows * 256 + b * 4096 + chunk), acc[b], 0, 0, 0);
+        }
+        __syncthreads();
+    }
+    float *h = p.h + static_cast<int64_t>(slice) * p.T * p.rank;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int j = wave * 16 + g * 4 + r;                   // result register r of lane group g is row 4 g + r
+        if (j < n)
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+                if (b * 16 + l16 < p.rank) h[static_cast<int64_t>(list[j]) * p.rank + b * 16 + l16] = acc[b][r];
+    }
+}
+
+// y of 64 rows and `cols` columns, 128 at a time.  Y = h B_a^T: 16 rows of h are the A operand (a wave prepares its own, in registers), rows of
+// B_a the B operand, column 8 c + s of the 128 as column c of product s: a lane then holds 8 consecutive columns of four rows, and 16
+// lanes a row, 256 bytes.  The 128 rows of B_a are one run of memory and are copied as such, in two buffers; chunk q (16 bytes) of them lies at q ^ h
+// inside its 16, h counting the 8 rows before it, so that a fragment read, one chunk of 16 rows 8 apart, meets no bank twice.
+template <int KS, bool VEC>
+__global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];           // two of: 128 rows of B_a
+    __shared__ int32_t list[kRows];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
+    int32_t n = 0;
+    const int32_t id = find_tile<kRows>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
+    if (id < 0) return;
+    const bool none = id == p.n_adapters;
+    if (none && p.y == p.base) return;
+    __syncthreads();
+
+    const int32_t chunks = p.rank / 8, pieces = chunks * 2;    // 1 KiB pieces of a block of 128 rows of B_a
+    const int shift = 34 - __builtin_clz(chunks);              // h = q >> (3 + log2(chunks)): exact for powers of two, else some banks meet
+    const uint32_t lds0 = lds_address(smem), buffer_bytes = pieces * 1024;
+    const int32_t first = blockIdx.x * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols, blocks = (end - first + 127) / 128;
+    const int sh = shift < 4 ? 4 : shift;
+    auto copy_b = [&](int32_t block, int buffer) {
+        const uint8_t *from = reinterpret_cast<const uint8_t *>(p.b + (static_cast<int64_t>(id) * p.N + first + block * 128) * p.rank);
+        const int32_t last = (p.N - first - block * 128) * chunks - 1;         // chunks behind the last row repeat its last one
+        for (int i = wave; i < pieces; i += 4) {
+            const int32_t at = i * 64 + lane, q = (at & ~15) | ((at & 15) ^ ((at >> sh) & 15));
+            lds_dma16_lane_address(from + static_cast<int64_t>(q < last ? q : last) * 16, lds0 + buffer * buffer_bytes + i * 1024);
+        }
+    };
+    const int32_t rows = n - wave * 16 < 16 ? n - wave * 16 : 16;              // of this wave; may be none
+    int32_t row[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int j = wave * 16 + g * 4 + r;
+        row[r] = list[j < n ? j : n - 1];
+    }
+    v8h bs[4];
+    auto load_base = [&](int32_t block) {                      // columns behind the last repeat it
+        const int32_t col = first + block * 128 + l16 * 8;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const __half *base = p.base + row[r] * p.ldb;
+            if constexpr (VEC) {
+                bs[r] = *reinterpret_cast<const v8h *>(base + (col < p.N ? col : p.N - 8));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) bs[r][e] = *reinterpret_cast<const _Float16 *>(base + (col + e < p.N ? col + e : p.N - 1));
+            }
+        }
+    };
+    load_base(0);
+
+    // ---- h of the wave's 16 rows, lane: row l16, ranks 8 g .. of every 32; two parts of h 2^-e
+    v8h hi[KS], lo[KS];
+    float factor[4] = {0.f, 0.f, 0.f, 0.f};
+    if (!none) {
+        const int j = wave * 16 + l16;
+        const int64_t slice = static_cast<int64_t>(p.T) * p.rank;
+        const float *h = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank;
+        float f[KS][8], top = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
+        constexpr int kAtOnce = KS <= 2 ? 4 : 2;
+        for (int32_t c = 0; c < p.slices; c += kAtOnce) {
+            v4f v[kAtOnce][KS][2];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {                 // ranks and slices behind the last repeat it
+                    const int r = s * 32 + g * 8;
+                    const float *at = h + (c + i < p.slices ? c + i : c) * slice + (r < p.rank ? r : p.rank - 8);
+                    v[i][s][0] = reinterpret_cast<const v4f *>(at)[0];
+                    v[i][s][1] = reinterpret_cast<const v4f *>(at)[1];
+                }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[s][e] += c + i < p.slices && s * 32 + g * 8 < p.rank ? v[i][s][e >> 2][e & 3] : 0.0f;
+        }
+        const float scale = p.scale[id];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
+        float down, up;
+        scale_of(top, down, up);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) split(f[s], down, hi[s], lo[s]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) factor[r] = scale * __shfl(up, g * 4 + r, 64);
+        wait_copies<0>();                                      // from here on the loop counts what it asks for itself
+        copy_b(0, 0);
+    }
+
+    for (int32_t block = 0; block < blocks; ++block) {
+        const int buffer = block & 1;
+        v4f acc[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (!none) {
+            // This block's rows of B_a: behind them at most the base's four loads and the stores of the block before were issued
+            if (block == 0) wait_copies<0>();
+            else wait_copies<4>();
+            __syncthreads();                                   // they are there for all waves, and the other buffer is free
+            if (block + 1 < blocks) copy_b(block + 1, buffer ^ 1);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const bool in = k * 32 + g * 8 < p.rank;
+                const int32_t c = in ? k * 4 + g : chunks - 1;
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    const int32_t q = (l16 * 8 + s) * chunks + c, at = (q & ~15) | ((q & 15) ^ ((q >> sh) & 15));
+                    const v8h bv = *(v8h_lds_ptr)(uintptr_t)(lds0 + buffer * buffer_bytes + at * 16);
+                    acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[k], bv, acc[s], 0, 0, 0);
+                    acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[k], bv, acc[s], 0, 0, 0);
+                }
+            }
+        }
+        const int32_t col = first + block * 128 + l16 * 8;
+        v8h out[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            out[r] = bs[r];
+            if (!none)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[r][e] = static_cast<_Float16>(__builtin_fmaf(factor[r], acc[e][r], static_cast<float>(bs[r][e])));
+        }
+        if (block + 1 < blocks) load_base(block + 1);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            __half *y = p.y + row[r] * p.ldy;
+            const bool mine = g * 4 + r < rows;
+            if constexpr (VEC) {
+                if (mine && col < end) *reinterpret_cast<v8h *>(y + col) = out[r];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (mine && col + e < end) *reinterpret_cast<_Float16 *>(y + col + e) = out[r][e];
+            }
+        }
+    }
+}
+
+// Up to 64 rows: tiles of 16, and slices of K short enough that each wave has about one unit.  More: tiles of 64, and as many slices as give
+// every compute unit two work-groups.
 struct Plan {
-    int rt, rb;
-    int32_t slices, tiles;                 // tiles: at most, per 256 rows, behind the first of every adapter
+    bool few;
+    int32_t slices;
 };
 
-Plan make_plan(int32_t T, int32_t K, int32_t rank)
+Plan make_plan(int32_t T, int32_t K)
 {
     Plan p;
-    p.rb = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
-    p.rt = T <= 64 ? 1 : p.rb == 8 ? 2 : 4;
-    const int32_t units = static_cast<int32_t>(ceil_div(K, kUnit));
-    int64_t s = T <= 64 ? ceil_div(units, kShrinkWaves) : kNumCU / ceil_div(T, p.rt * 16);
-    const int64_t most = T <= 64 ? kMaxSlices : ceil_div(units, 2 * kShrinkWaves);
+    p.few = T <= 64;
+    int64_t s, most;
+    if (p.few) {
+        s = most = ceil_div(K, kUnit * kShrinkWaves);
+    } else {
+        s = 2 * kNumCU / ceil_div(T, kRows);
+        most = ceil_div(ceil_div(K, kStage), 2);
+    }
     if (s > most) s = most;
     if (s > kMaxSlices) s = kMaxSlices;
     p.slices = static_cast<int32_t>(s < 1 ? 1 : s);
-    p.tiles = static_cast<int32_t>((T < kBlock ? T : kBlock) / (p.rt * 16));
     return p;
 }
 
-template <int RT, int RB>
-int launch_shrink(const Lora &a, dim3 grid, hipStream_t stream)
+template <int RB>
+int launch_shrink(const Lora &a, bool few, dim3 grid, hipStream_t stream)
 {
-    MQ_LAUNCH((lora_shrink_kernel<RT, RB>), grid, dim3(kShrinkWaves * 64), 0, stream, a);
+    if (few) {
+        MQ_LAUNCH((lora_shrink_kernel<1, RB>), grid, dim3(kShrinkWaves * 64), 0, stream, a);
+        return launch_status();
+    }
+    constexpr int lds = 2 * (kRows + RB * 16) * 256;
+    auto kern = lora_shrink_rows_kernel<RB>;
+    if constexpr (lds >= 60 * 1024) {                          // next to the list of rows
+        static LdsLimit limit;
+        if (const int st = limit.raise(reinterpret_cast<const void *>(kern), lds); st != MQUANT_OK) return st;
+    }
+    MQ_LAUNCH(kern, grid, dim3(256), lds, stream, a);
     return launch_status();
 }
 
-template <int RT, int KS>
-int launch_expand(const Lora &a, dim3 grid, bool vec, hipStream_t stream)
+template <int KS, bool VEC>
+int launch_expand(const Lora &a, bool few, dim3 grid, hipStream_t stream)
 {
-    if (vec) MQ_LAUNCH((lora_expand_kernel<RT, KS, true>), grid, dim3(kExpandWaves * 64), 0, stream, a);
-    else MQ_LAUNCH((lora_expand_kernel<RT, KS, false>), grid, dim3(kExpandWaves * 64), 0, stream, a);
+    if (few) MQ_LAUNCH((lora_expand_kernel<1, KS, VEC>), grid, dim3(kExpandWaves * 64), 0, stream, a);
+    else {
+        auto kern = lora_expand_rows_kernel<KS, VEC>;
+        if constexpr (KS == 4) {
+            static LdsLimit limit;
+            if (const int st = limit.raise(reinterpret_cast<const void *>(kern), 2 * 256 * 128); st != MQUANT_OK) return st;
+        }
+        MQ_LAUNCH(kern, grid, dim3(256), 2 * 256 * a.rank, stream, a);
+    }
     return launch_status();
 }
 
@@ -393,7 +669,7 @@ extern "C" int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t ran
     if (T < 0 || K < 0 || rank < 1) return MQUANT_ERR_BAD_SHAPE;
     if (K == 0 || K % 8 != 0 || rank % 8 != 0 || rank > 128) return MQUANT_ERR_UNSUPPORTED;
     if (T == 0) return 0;
-    return ceil_div(static_cast<int64_t>(make_plan(T, K, rank).slices) * T * rank * 4, 256) * 256;
+    return ceil_div(static_cast<int64_t>(make_plan(T, K).slices) * T * rank * 4, 256) * 256;
 }
 
 extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm, const int32_t *adapter, const void *a, const void *b,
@@ -414,32 +690,27 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     if (!aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
-    const Plan p = make_plan(T, K, rank);
+    const Plan p = make_plan(T, K);
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
-                 n_adapters, p.slices, T <= 64 ? kExpandWaves * kCols : 2 * kExpandWaves * kCols};
+                 n_adapters, p.slices, p.few ? kExpandWaves * kCols : 512};
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
+    // Tiles of 256 rows: full ones, and a last one of every adapter (and of the rows without), which may not be there: those come last in
+    // the grids.
     const int32_t in_block = T < kBlock ? T : kBlock;
-    // tiles of a block: full ones, and a last one of every adapter (and of the rows without)
-    const int32_t tiles = p.tiles + (n_adapters < in_block ? n_adapters + 1 : in_block);
-    if (blocks > 65535 || chunks > 65535) return MQUANT_ERR_UNSUPPORTED;
-    const bool vec = N % 8 == 0 && ldb % 8 == 0 && ldy % 8 == 0 && aligned_to(base, 16) && aligned_to(y, 16);
+    const int32_t tiles = in_block / (p.few ? 16 : kRows) + (n_adapters < in_block ? n_adapters + 1 : in_block);
+    if (blocks > 65535) return MQUANT_ERR_UNSUPPORTED;
     if (n_adapters > 0) {
-        const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(blocks), static_cast<unsigned>(p.slices));
-        int st;
-        if (p.rt == 1) {
-            st = p.rb == 1 ? launch_shrink<1, 1>(args, grid, stream) : p.rb == 2 ? launch_shrink<1, 2>(args, grid, stream)
-               : p.rb == 4 ? launch_shrink<1, 4>(args, grid, stream) : launch_shrink<1, 8>(args, grid, stream);
-        } else {
-            st = p.rb == 1 ? launch_shrink<4, 1>(args, grid, stream) : p.rb == 2 ? launch_shrink<4, 2>(args, grid, stream)
-               : p.rb == 4 ? launch_shrink<4, 4>(args, grid, stream) : launch_shrink<2, 8>(args, grid, stream);
-        }
+        const dim3 grid(static_cast<unsigned>(p.slices), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
+        const int st = rank <= 16 ? launch_shrink<1>(args, p.few, grid, stream) : rank <= 32 ? launch_shrink<2>(args, p.few, grid, stream)
+                     : rank <= 64 ? launch_shrink<4>(args, p.few, grid, stream) : launch_shrink<8>(args, p.few, grid, stream);
         if (st != MQUANT_OK) return st;
     }
-    const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(blocks), static_cast<unsigned>(chunks));
-    if (p.rt == 1)
-        return p.rb <= 2 ? launch_expand<1, 1>(args, grid, vec, stream) : p.rb == 4 ? launch_expand<1, 2>(args, grid, vec, stream)
-                                                                                    : launch_expand<1, 4>(args, grid, vec, stream);
-    return p.rb <= 2 ? launch_expand<4, 1>(args, grid, vec, stream) : p.rb == 4 ? launch_expand<4, 2>(args, grid, vec, stream)
-                                                                                : launch_expand<2, 4>(args, grid, vec, stream);
+    const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
+    const bool vec = N % 8 == 0 && ldb % 8 == 0 && ldy % 8 == 0 && aligned_to(base, 16) && aligned_to(y, 16);
+    if (vec)
+        return rank <= 32 ? launch_expand<1, true>(args, p.few, grid, stream) : rank <= 64 ? launch_expand<2, true>(args, p.few, grid, stream)
+                                                                                         : launch_expand<4, true>(args, p.few, grid, stream);
+    return rank <= 32 ? launch_expand<1, false>(args, p.few, grid, stream) : rank <= 64 ? launch_expand<2, false>(args, p.few, grid, stream)
+                                                                                      : launch_expand<4, false>(args, p.few, grid, stream);
 }

@@ -9,7 +9,7 @@ import pytest
 from paper_2502_00425_amd import build
 from test_attention_branches import HIPCC, unguarded
 
-KERNELS = {"paged_attention.hip": ["paged_chunk_kernel", "paged_few_kernel"], "lora.hip": ["lora_shrink_kernel", "lora_expand_kernel"]}
+KERNELS = {"paged_attention.hip": ["paged_chunk_kernel", "paged_few_kernel"], "lora.hip": ["lora_shrink_kernel", "lora_expand_kernel", "lora_shrink_rows_kernel", "lora_expand_rows_kernel"]}
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="needs hipcc")
