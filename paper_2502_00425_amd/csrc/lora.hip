@@ -6,6 +6,8 @@
 // rows, of the adapters.
 #include <hip/hip_fp16.h>
 
+#include <cmath>
+
 #include "lds_dma.h"
 #include "mquant_internal.h"
 
@@ -21,7 +23,7 @@ constexpr int kShrinkWaves = 8;
 constexpr int kUnit = 64;                  // channels of K that a wave takes at a time: a 128-byte line of every row
 constexpr int kExpandWaves = 4;
 constexpr int kCols = 64;                  // columns of y that a wave takes at a time
-constexpr int kMaxSlices = 16;
+constexpr int kMaxSlices = 16;             // of few rows
 
 struct Lora {
     const __half *x;
@@ -515,32 +517,47 @@ __global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
     v8h hi[KS], lo[KS];
     float factor[4] = {0.f, 0.f, 0.f, 0.f};
     if (!none) {
-        const int j = wave * 16 + l16;
+        // The slices are added as they lie in memory, 16 bytes a lane along the rows, and change over to the operand's order in LDS. (Read in
+        // that order, 128 bytes of 16 rows a load, a slice took 0.5 us a work-group.)
         const int64_t slice = static_cast<int64_t>(p.T) * p.rank;
-        const float *h = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank;
+        const int32_t per_row = p.rank / 4, pitch = p.rank + 4;                // 16-byte pieces of a row; floats of it in LDS
+        constexpr int NI = KS * 2;                             // pieces of a lane, at most
+        const float *from[NI];
+        v4f sum[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int32_t at = i * 64 + lane, j = wave * 16 + (at / per_row < 16 ? at / per_row : 15);
+            from[i] = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank + at % per_row * 4;
+            sum[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        }
+        constexpr int kAtOnce = KS == 1 ? 8 : KS == 2 ? 4 : 2;
+        for (int32_t c = 0; c < p.slices; c += kAtOnce) {
+            v4f v[kAtOnce][NI];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                for (int i = 0; i < NI; ++i)                   // slices behind the last repeat it
+                    v[u][i] = *reinterpret_cast<const v4f *>(from[i] + (c + u < p.slices ? c + u : p.slices - 1) * slice);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+                if (c + u < p.slices)
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) sum[i] += v[u][i];
+        }
+        float *mine = reinterpret_cast<float *>(smem) + wave * 16 * pitch;     // of this wave alone
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int32_t at = i * 64 + lane;
+            if (at < 16 * per_row) *reinterpret_cast<v4f *>(mine + at / per_row * pitch + at % per_row * 4) = sum[i];
+        }
         float f[KS][8], top = 0.0f;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < KS; ++s) {
+            const int r = s * 32 + g * 8;
+            const float *at = mine + l16 * pitch + (r < p.rank ? r : 0);
+            const v4f f0 = reinterpret_cast<const v4f *>(at)[0], f1 = reinterpret_cast<const v4f *>(at)[1];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
-        constexpr int kAtOnce = KS <= 2 ? 4 : 2;
-        for (int32_t c = 0; c < p.slices; c += kAtOnce) {
-            v4f v[kAtOnce][KS][2];
-#pragma unroll
-            for (int i = 0; i < kAtOnce; ++i)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {                 // ranks and slices behind the last repeat it
-                    const int r = s * 32 + g * 8;
-                    const float *at = h + (c + i < p.slices ? c + i : c) * slice + (r < p.rank ? r : p.rank - 8);
-                    v[i][s][0] = reinterpret_cast<const v4f *>(at)[0];
-                    v[i][s][1] = reinterpret_cast<const v4f *>(at)[1];
-                }
-#pragma unroll
-            for (int i = 0; i < kAtOnce; ++i)
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[s][e] += c + i < p.slices && s * 32 + g * 8 < p.rank ? v[i][s][e >> 2][e & 3] : 0.0f;
+            for (int e = 0; e < 8; ++e) f[s][e] = r < p.rank ? (e < 4 ? f0[e & 3] : f1[e & 3]) : 0.0f;
         }
         const float scale = p.scale[id];
 #pragma unroll
@@ -554,6 +571,7 @@ __global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
 #pragma unroll
         for (int r = 0; r < 4; ++r) factor[r] = scale * __shfl(up, g * 4 + r, 64);
         wait_copies<0>();                                      // from here on the loop counts what it asks for itself
+        __syncthreads();                                       // all waves are done with their sums
         copy_b(0, 0);
     }
 
@@ -596,7 +614,7 @@ __global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
             __half *y = p.y + row[r] * p.ldy;
             const bool mine = g * 4 + r < rows;
             if constexpr (VEC) {
-                if (mine && col < end) *reinterpret_cast<v8h *>(y + col) = out[r];
+                if (mine && col < end) __builtin_nontemporal_store(out[r], reinterpret_cast<v8h *>(y + col));
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -606,8 +624,10 @@ __global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
     }
 }
 
-// Up to 64 rows: tiles of 16, and slices of K short enough that each wave has about one unit.  More: tiles of 64, and as many slices as give
-// every compute unit two work-groups.
+// Up to 64 rows: tiles of 16, and slices of K short enough that each wave has about one unit.  More: tiles of 64; a slice's stage takes
+// 0.55 us and every slice costs the expansion 0.28, so about sqrt(2 stages) slices (rank 64, K = 3584, 28 stages, shrink + expansion in us with
+// 2 / 4 / 8 / 14 slices: 512 rows 25.2 / 20.6 / 19.8 / 21.7, 1024 26.2 / 22.3 / 22.2 / 24.9), but no more than give every compute unit a
+// work-group (4096 rows: 4 slices 33.2, 8 41.9).
 struct Plan {
     bool few;
     int32_t slices;
@@ -619,13 +639,13 @@ Plan make_plan(int32_t T, int32_t K)
     p.few = T <= 64;
     int64_t s, most;
     if (p.few) {
-        s = most = ceil_div(K, kUnit * kShrinkWaves);
+        s = ceil_div(K, kUnit * kShrinkWaves);
+        most = kMaxSlices;
     } else {
-        s = 2 * kNumCU / ceil_div(T, kRows);
-        most = ceil_div(ceil_div(K, kStage), 2);
+        s = static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)))));
+        most = kNumCU / ceil_div(T, kRows);
     }
     if (s > most) s = most;
-    if (s > kMaxSlices) s = kMaxSlices;
     p.slices = static_cast<int32_t>(s < 1 ? 1 : s);
     return p;
 }
@@ -694,6 +714,10 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
                  n_adapters, p.slices, p.few ? kExpandWaves * kCols : 512};
+    // Many rows: 512 columns a work-group, which prepares its rows once for all of them, fewer where that leaves compute units idle (K = 3584,
+    // N = 4608, rank 64, expansion with 128 / 256 / 512 / 1024 columns: 128 rows 9.1 / 10.4 / 13.4 / 18.9 us, 1024 15.7 / 14.8 / 16.3 / 21.2, 4096
+    // 28.2 / 24.4 / 21.7 / 23.1).
+    while (!p.few && args.cols > 128 && ceil_div(T, kRows) * ceil_div(N, args.cols) < kNumCU) args.cols /= 2;
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
     // Tiles of 256 rows: full ones, and a last one of every adapter (and of the rows without), which may not be there: those come last in
     // the grids.
