@@ -624,31 +624,29 @@ __global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
     }
 }
 
-// Up to 64 rows: tiles of 16, and slices of K short enough that each wave has about one unit.  More: tiles of 64; a slice's stage takes
-// 0.55 us and every slice costs the expansion 0.28, so about sqrt(2 stages) slices (rank 64, K = 3584, 28 stages, shrink + expansion in us with
-// 2 / 4 / 8 / 14 slices: 512 rows 25.2 / 20.6 / 19.8 / 21.7, 1024 26.2 / 22.3 / 22.2 / 24.9), but no more than give every compute unit a
-// work-group (4096 rows: 4 slices 33.2, 8 41.9).
-struct Plan {
-    bool few;
-    int32_t slices;
-};
-
-Plan make_plan(int32_t T, int32_t K)
+// Few rows: tiles of 16, and slices of K short enough that each wave has about one unit.
+int64_t few_slices(int32_t K)
 {
-    Plan p;
-    p.few = T <= 64;
-    int64_t s, most;
-    if (p.few) {
-        s = ceil_div(K, kUnit * kShrinkWaves);
-        most = kMaxSlices;
-    } else {
-        s = static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)))));
-        most = kNumCU / ceil_div(T, kRows);
-    }
-    if (s > most) s = most;
-    p.slices = static_cast<int32_t>(s < 1 ? 1 : s);
-    return p;
+    const int64_t s = ceil_div(K, kUnit * kShrinkWaves);
+    return s < kMaxSlices ? s : kMaxSlices;
 }
+
+// Many: tiles of 64; a slice's stage takes 0.55 us and every slice costs the expansion 0.28, so about sqrt(2 stages) slices (rank 64, K = 3584,
+// 28 stages, shrink + expansion in us with 2 / 4 / 8 / 14 slices: 512 rows 25.2 / 20.6 / 19.8 / 21.7, 1024 26.2 / 22.3 / 22.2 / 24.9), but no
+// more than give every compute unit a work-group (4096 rows: 4 slices 33.2, 8 41.9).
+int64_t many_slices(int32_t T, int32_t K)
+{
+    int64_t s = static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)))));
+    const int64_t most = kNumCU / ceil_div(T, kRows);
+    if (s > most) s = most;
+    return s < 1 ? 1 : s;
+}
+
+// Tiles of 16 rows or of 64: 64 where they are full.  Tiles of 64 / of 16, shrink + expansion in us, K = 3584, N = 4608, rank 16 and 64, 4 adapters:
+// 128 rows 10.2 / 9.6 and 14.5 / 13.4, 256 10.6 / 10.9 and 14.9 / 16.5, 512 11.3 / 13.2 and 16.6 / 22.1; 64 adapters, each row another:
+// 128 rows 52.4 / 35.8 and 61.0 / 42.7, 512 89 / 61 and 111 / 73, 1024 108 / 107 and 141 / 132.
+constexpr int32_t kFewMax = 1024;
+bool few_rows(int32_t T, int32_t n_adapters) { return T <= 128 || (T <= kFewMax && n_adapters >= T / 16); }
 
 template <int RB>
 int launch_shrink(const Lora &a, bool few, dim3 grid, hipStream_t stream)
@@ -689,7 +687,9 @@ extern "C" int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t ran
     if (T < 0 || K < 0 || rank < 1) return MQUANT_ERR_BAD_SHAPE;
     if (K == 0 || K % 8 != 0 || rank % 8 != 0 || rank > 128) return MQUANT_ERR_UNSUPPORTED;
     if (T == 0) return 0;
-    return ceil_div(static_cast<int64_t>(make_plan(T, K).slices) * T * rank * 4, 256) * 256;
+    int64_t slices = many_slices(T, K);
+    if (T <= kFewMax && few_slices(K) > slices) slices = few_slices(K);        // whichever the number of adapters asks for
+    return ceil_div(slices * T * rank * 4, 256) * 256;
 }
 
 extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm, const int32_t *adapter, const void *a, const void *b,
@@ -710,31 +710,32 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     if (!aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
-    const Plan p = make_plan(T, K);
+    const bool few = few_rows(T, n_adapters);
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
-                 n_adapters, p.slices, p.few ? kExpandWaves * kCols : 512};
+                 n_adapters, static_cast<int32_t>(few ? few_slices(K) : many_slices(T, K)),
+                 few ? kExpandWaves * kCols : 512};
     // Many rows: 512 columns a work-group, which prepares its rows once for all of them, fewer where that leaves compute units idle (K = 3584,
     // N = 4608, rank 64, expansion with 128 / 256 / 512 / 1024 columns: 128 rows 9.1 / 10.4 / 13.4 / 18.9 us, 1024 15.7 / 14.8 / 16.3 / 21.2, 4096
     // 28.2 / 24.4 / 21.7 / 23.1).
-    while (!p.few && args.cols > 128 && ceil_div(T, kRows) * ceil_div(N, args.cols) < kNumCU) args.cols /= 2;
+    while (!few && args.cols > 128 && ceil_div(T, kRows) * ceil_div(N, args.cols) < kNumCU) args.cols /= 2;
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
     // Tiles of 256 rows: full ones, and a last one of every adapter (and of the rows without), which may not be there: those come last in
     // the grids.
     const int32_t in_block = T < kBlock ? T : kBlock;
-    const int32_t tiles = in_block / (p.few ? 16 : kRows) + (n_adapters < in_block ? n_adapters + 1 : in_block);
+    const int32_t tiles = in_block / (few ? 16 : kRows) + (n_adapters < in_block ? n_adapters + 1 : in_block);
     if (blocks > 65535) return MQUANT_ERR_UNSUPPORTED;
     if (n_adapters > 0) {
-        const dim3 grid(static_cast<unsigned>(p.slices), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
-        const int st = rank <= 16 ? launch_shrink<1>(args, p.few, grid, stream) : rank <= 32 ? launch_shrink<2>(args, p.few, grid, stream)
-                     : rank <= 64 ? launch_shrink<4>(args, p.few, grid, stream) : launch_shrink<8>(args, p.few, grid, stream);
+        const dim3 grid(static_cast<unsigned>(args.slices), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
+        const int st = rank <= 16 ? launch_shrink<1>(args, few, grid, stream) : rank <= 32 ? launch_shrink<2>(args, few, grid, stream)
+                     : rank <= 64 ? launch_shrink<4>(args, few, grid, stream) : launch_shrink<8>(args, few, grid, stream);
         if (st != MQUANT_OK) return st;
     }
     const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
     const bool vec = N % 8 == 0 && ldb % 8 == 0 && ldy % 8 == 0 && aligned_to(base, 16) && aligned_to(y, 16);
     if (vec)
-        return rank <= 32 ? launch_expand<1, true>(args, p.few, grid, stream) : rank <= 64 ? launch_expand<2, true>(args, p.few, grid, stream)
-                                                                                         : launch_expand<4, true>(args, p.few, grid, stream);
-    return rank <= 32 ? launch_expand<1, false>(args, p.few, grid, stream) : rank <= 64 ? launch_expand<2, false>(args, p.few, grid, stream)
-                                                                                      : launch_expand<4, false>(args, p.few, grid, stream);
+        return rank <= 32 ? launch_expand<1, true>(args, few, grid, stream) : rank <= 64 ? launch_expand<2, true>(args, few, grid, stream)
+                                                                                         : launch_expand<4, true>(args, few, grid, stream);
+    return rank <= 32 ? launch_expand<1, false>(args, few, grid, stream) : rank <= 64 ? launch_expand<2, false>(args, few, grid, stream)
+                                                                                      : launch_expand<4, false>(args, few, grid, stream);
 }
