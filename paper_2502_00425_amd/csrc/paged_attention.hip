@@ -359,11 +359,12 @@ __device__ __forceinline__ void halves_of(float x, float &lo, float &hi)
 // MFMA 32x32 result register r of lane group g holds row (r/4)*8 + g*4 + r%4.
 __device__ __forceinline__ int acc_row(int r, int g) { return (r >> 2) * 8 + g * 4 + (r & 3); }
 
-__global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcds_per_kv)
+template <int KG>
+__global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_t xcds_per_kv)
 {
-    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];           // KG * kChunkLds
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
-    const int wave = uniform(tid >> 6);
+    const int wave = uniform((tid >> 6) & 3), kg = KG > 1 ? uniform(tid >> 8) : 0;
     // Work-groups are dealt round-robin to the 8 XCDs, each with its own L2: one key/value head per XCD where they divide
     // evenly, so that an L2 fetches the tiles its work-groups walk together once.
     int32_t kvh, item;
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
             if (lane >= x) sum += o;
         }
         const int32_t total = __builtin_amdgcn_readlane(sum, 63);
-        if (a.c.n_seq <= 64 && a.n_split == 1 && total <= 2 * kNumCU / a.c.n_kv_heads) {
+        if (KG == 1 && a.c.n_seq <= 64 && a.n_split == 1 && total <= 2 * kNumCU / a.c.n_kv_heads) {
             const int32_t half = kNumCU / a.c.n_kv_heads;
             if (left >= half && left < total) left = total - 1 - (left - half);
         }
@@ -438,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
             low = min(low, __shfl_xor(low, x, 64));
             hi = max(hi, __shfl_xor(hi, x, 64));
         }
-        if (lane == 0) tops[wave] = hi;
+        if (kg == 0 && lane == 0) tops[wave] = hi;
         __syncthreads();
         top = uniform(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
         low = uniform(low);
@@ -457,37 +458,44 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
 
     // ---- tile copies: block i of 16 slots is 4 KiB of one page; a wave copies four rows of each block.  Key chunk c of row r lies at
     // chunk c ^ (r & 15) (a fragment read takes one chunk of 16 rows), value chunk c at c ^ 4 (r & 3) (a transposing read: 64 bytes of 4 rows).
-    const uint32_t lds0 = lds_address(smem);
+    const uint32_t lds0 = lds_address(smem) + kg * kChunkLds;
     const int c_row = wave * 4 + (lane >> 4);
     const uint32_t k_off = c_row * 256 + (((lane & 15) ^ (c_row & 15)) << 4);
     const uint32_t v_off = c_row * 256 + (((lane & 15) ^ ((c_row & 3) << 2)) << 4);
-    // lane l: block 64 j + l for the keys' and for the values' tile, and the next 64 on their way
-    auto blocks_from = [&](int32_t b) { return block_at(a, seq, kvh, b + lane); };
-    const int32_t b0 = t0 * 4;
-    uint32_t k_blocks = blocks_from(b0), v_blocks = k_blocks, n_blocks = blocks_from(b0 + 64);
-    auto dma_k = [&](int32_t t, int b) {
-        const int32_t at = (t - t0) * 4;
+    // Key group kg takes the tiles t0 + kg, t0 + kg + KG, ...: tile i of its own.  The groups do the same number of steps; one whose tiles
+    // are used up repeats the piece's last one with nothing of it visible.
+    const int32_t steps = t_end > t0 ? (t_end - t0 + KG - 1) / KG : 0;
+    auto tile_of = [&](int32_t i) {
+        const int32_t t = t0 + kg + KG * i;
+        return KG == 1 || t < t_end ? t : t_end > 0 ? t_end - 1 : 0;            // t_end = 0: no slot is visible, and no tile is taken
+    };
+    // lane l: block l % 4 of tile 16 j + l / 4, for the keys' tile and for the values', and the next 16 tiles on their way
+    auto blocks_from = [&](int32_t i) { return block_at(a, seq, kvh, tile_of(i + (lane >> 2)) * 4 + (lane & 3)); };
+    uint32_t k_blocks = blocks_from(0), v_blocks = k_blocks, n_blocks = blocks_from(16);
+    auto dma_k = [&](int32_t i, int b) {
+        const int32_t at = i * 4;
         if ((at & 63) == 0 && at > 0) {
             k_blocks = n_blocks;
-            n_blocks = blocks_from(b0 + at + 64);
+            n_blocks = blocks_from(i + 16);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            lds_dma16_uniform_base(block_ptr(a.c.k, __builtin_amdgcn_readlane(k_blocks, (at & 63) + i)), k_off,
-                                   lds0 + b * kTileBytes + (i * 4 + wave) * 1024);
+        for (int u = 0; u < 4; ++u)
+            lds_dma16_uniform_base(block_ptr(a.c.k, __builtin_amdgcn_readlane(k_blocks, (at & 63) + u)), k_off,
+                                   lds0 + b * kTileBytes + (u * 4 + wave) * 1024);
     };
-    auto dma_v = [&](int32_t t, int b) {                       // one tile behind the keys: their blocks are in k_blocks by then
-        const int32_t at = (t - t0) * 4;
+    auto dma_v = [&](int32_t i, int b) {                       // one tile behind the keys: their blocks are in k_blocks by then
+        const int32_t at = i * 4;
         if ((at & 63) == 0) v_blocks = k_blocks;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            lds_dma16_uniform_base(block_ptr(a.c.v, __builtin_amdgcn_readlane(v_blocks, (at & 63) + i)), v_off,
-                                   lds0 + (2 + b) * kTileBytes + (i * 4 + wave) * 1024);
+        for (int u = 0; u < 4; ++u)
+            lds_dma16_uniform_base(block_ptr(a.c.v, __builtin_amdgcn_readlane(v_blocks, (at & 63) + u)), v_off,
+                                   lds0 + (2 + b) * kTileBytes + (u * 4 + wave) * 1024);
     };
     // Value rows behind the last slot become zeros once they have landed (every lane those it copied): they may hold anything,
     // and a zero probability times NaN is NaN.
     const int32_t ragged = (top + 1) % kChunkK != 0 ? t_all - 1 : -1;
-    auto zero_tail = [&](int32_t t, int b) {
+    auto zero_tail = [&](int32_t i, int b) {
+        const int32_t t = tile_of(i);
         if (t != ragged) return;
         uint32_t at = lds0 + (2 + b) * kTileBytes + wave * 1024 + lane * 16;
         int32_t slot = t * kChunkK + c_row;
@@ -544,16 +552,17 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
     const float scale_log2e = a.scale_log2e, lazy_raw = kLazy / scale_log2e;
     float m_ref = -INFINITY, l_run = 0.0f;
 
-    // One step: softmax and P V of tile t (scores in s_cur, values in V buffer par) while the scores of tile t + 1 (keys in K
+    // One step: softmax and P V of the group's tile i_cur (scores in s_cur, values in V buffer par) while the scores of its next tile (keys in K
     // buffer par ^ 1) go to s_nxt between the exponentials.  On entry a barrier has published those buffers and freed K
     // buffer par and V buffer par ^ 1.  The last tile computes scores of whatever lies in the other K buffer, which nothing reads: a
     // second form of the step without them cost 69 spilled registers.
-    auto step = [&](v16f (&s_cur)[2], v16f (&s_nxt)[2], const int32_t t, const int par) {
-        if (t + 2 < t_end) dma_k(t + 2, par);
-        if (t + 1 < t_end) dma_v(t + 1, par ^ 1);
+    auto step = [&](v16f (&s_cur)[2], v16f (&s_nxt)[2], const int32_t i_cur, const int par) {
+        if (i_cur + 2 < steps) dma_k(i_cur + 2, par);
+        if (i_cur + 1 < steps) dma_v(i_cur + 1, par ^ 1);
+        const int32_t t = t0 + kg + KG * i_cur;
         const uint32_t kb_lds = (par ^ 1) * kTileBytes, vb_lds = (2 + par) * kTileBytes;
-        if (t * kChunkK + kChunkK - 1 > low) {                 // some query of the wave does not see some slot
-            int32_t room = limit - t * kChunkK - 4 * g;
+        if (t * kChunkK + kChunkK - 1 > low || (KG > 1 && t >= t_end)) {       // some query of the wave does not see some slot
+            int32_t room = KG > 1 && t >= t_end ? -1 : limit - t * kChunkK - 4 * g;
             asm volatile("" : "+v"(room));
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -629,58 +638,100 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(Step a, int32_t xcd
             __builtin_amdgcn_sched_barrier(0);
         }
         wait_copies<0>();
-        zero_tail(t + 1, par ^ 1);
+        zero_tail(i_cur + 1, par ^ 1);
         __syncthreads();
     };
     // Two steps a turn of the loop, which has one exit: an odd tile goes ahead of it (a way out between the two steps had the
     // compiler move the 64 sums to other registers every turn).
-    if (t0 < t_end) {
-        const int par = (t_end - t0) & 1;
-        dma_k(t0, par);
-        dma_v(t0, par);
-        if (t0 + 1 < t_end) dma_k(t0 + 1, par ^ 1);
+    if (steps > 0) {
+        const int par = steps & 1;
+        dma_k(0, par);
+        dma_v(0, par);
+        if (steps > 1) dma_k(1, par ^ 1);
         wait_copies<0>();
-        zero_tail(t0, par);
+        zero_tail(0, par);
         __syncthreads();
         v16f s_a[2], s_b[2];
-        int32_t t = t0;
+        int32_t i = 0;
         if (par != 0) {
             scores(kTileBytes, s_b);
             __syncthreads();                                   // the first tile's K buffer is free
-            step(s_b, s_a, t++, 1);
+            step(s_b, s_a, i++, 1);
         } else {
             scores(0, s_a);
             __syncthreads();
         }
-        for (; t < t_end; t += 2) {
-            step(s_a, s_b, t, 0);
-            step(s_b, s_a, t + 1, 1);
+        for (; i < steps; i += 2) {
+            step(s_a, s_b, i, 0);
+            step(s_b, s_a, i + 1, 1);
         }
     }
 
     // ---- lane = query, registers = head channels (4 consecutive per group)
-    if (m >= M) return;
-    if (a.n_split == 1) {
+    const bool partial = a.n_split > 1;
+    const bool write = m < M && (!partial || limit >= t0 * kChunkK);
+    const int64_t at = (static_cast<int64_t>(piece) * a.T + row) * a.n_q + head;
+    __half *out = a.o + row * a.ldo + static_cast<int64_t>(head) * kD;
+    auto store4 = [&](int dt, int r4, const v4f &f, float inv_l) {
+        if (partial) {
+            *reinterpret_cast<v4f *>(a.part + at * kD + dt * 32 + r4 * 8 + g * 4) = f;
+            return;
+        }
+        __half h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = __float2half_rn(f[e] * inv_l);
+        *reinterpret_cast<uint2 *>(out + dt * 32 + r4 * 8 + g * 4) = *reinterpret_cast<const uint2 *>(h);
+    };
+    if constexpr (KG == 1) {
+        if (!write) return;
         const float inv_l = l_run > 0.0f ? 1.0f / l_run : 0.0f;                 // a row that sees nothing: zeros
-        __half *out = a.o + row * a.ldo + static_cast<int64_t>(head) * kD;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                __half h[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = __float2half_rn(acc_o[dt][r4 * 4 + e] * inv_l);
-                *reinterpret_cast<uint2 *>(out + dt * 32 + r4 * 8 + g * 4) = *reinterpret_cast<const uint2 *>(h);
-            }
-    } else if (limit >= t0 * kChunkK) {
-        const int64_t at = (static_cast<int64_t>(piece) * a.T + row) * a.n_q + head;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4)
-                *reinterpret_cast<v4f *>(a.part + at * kD + dt * 32 + r4 * 8 + g * 4) =
-                    v4f{acc_o[dt][r4 * 4], acc_o[dt][r4 * 4 + 1], acc_o[dt][r4 * 4 + 2], acc_o[dt][r4 * 4 + 3]};
-        if (g == 0) a.part_ml[at] = make_float2(m_ref, l_run);
+                store4(dt, r4, v4f{acc_o[dt][r4 * 4], acc_o[dt][r4 * 4 + 1], acc_o[dt][r4 * 4 + 2], acc_o[dt][r4 * 4 + 3]}, inv_l);
+        if (partial && g == 0) a.part_ml[at] = make_float2(m_ref, l_run);
+    } else {
+        // The two key groups of a query exchange halves of the channels: group kg finishes channels 64 kg .. 64 kg + 63.  The last
+        // barrier of the loop has freed the tile buffers.
+        float *xch = reinterpret_cast<float *>(smem);          // [8 waves][34][64]
+        static_assert(8 * 34 * 64 * 4 <= 2 * kChunkLds, "exchange of the key groups");
+        float *mine = xch + (kg * 4 + wave) * (34 * 64) + lane;
+        const float *theirs = xch + ((kg ^ 1) * 4 + wave) * (34 * 64) + lane;
+        auto give = [&](const v16f &x, const v16f &y) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                mine[r * 64] = x[r];
+                mine[(16 + r) * 64] = y[r];
+            }
+        };
+        if (kg == 0) give(acc_o[2], acc_o[3]);
+        else give(acc_o[0], acc_o[1]);
+        mine[32 * 64] = m_ref;
+        mine[33 * 64] = l_run;
+        __syncthreads();
+        if (!write) return;
+        const float m_o = theirs[32 * 64], l_o = theirs[33 * 64], top_m = fmaxf(m_ref, m_o);
+        const float own = m_ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_ref - top_m) * scale_log2e);
+        const float other = m_o == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_o - top_m) * scale_log2e);
+        const float l_all = l_run * own + l_o * other, inv_l = l_all > 0.0f ? 1.0f / l_all : 0.0f;
+        auto finish = [&](int dt, const v16f &acc, const float *from) {
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                v4f f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = acc[r4 * 4 + e] * own + from[(r4 * 4 + e) * 64] * other;
+                store4(dt, r4, f, inv_l);
+            }
+        };
+        if (kg == 0) {
+            finish(0, acc_o[0], theirs);
+            finish(1, acc_o[1], theirs + 16 * 64);
+        } else {
+            finish(2, acc_o[2], theirs);
+            finish(3, acc_o[3], theirs + 16 * 64);
+        }
+        if (partial && kg == 0 && g == 0) a.part_ml[at] = make_float2(top_m, l_all);
     }
 }
 
@@ -781,6 +832,7 @@ int check_sizes(int32_t T, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
 struct Plan {
     bool few = false, chunk = false;       // the kernels that may be needed; alone, a kernel takes every sequence
     int32_t few_split = 1, few_piece = 1 << 30, few_stride = 0, few_nq = 1;
+    bool chunk_two = false;                // two key groups to a work-group
     int32_t chunk_split = 1, chunk_piece = 1 << 30, chunk_tiles = 0;
     int64_t few_part = 0, chunk_part = 0;  // partial results (queries x pieces)
     int64_t bytes() const
@@ -822,6 +874,7 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
             p.chunk_piece = static_cast<int32_t>(ceil_div(ceil_div(kv, split), kChunkK) * kChunkK);
             p.chunk_split = static_cast<int32_t>(ceil_div(kv, p.chunk_piece));
         }
+        p.chunk_two = groups * p.chunk_split <= kNumCU;
         if (p.chunk_split > 1) p.chunk_part = static_cast<int64_t>(T) * n_q * p.chunk_split;
     }
     return p;
@@ -868,9 +921,11 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
         const int64_t items = static_cast<int64_t>(p.chunk_tiles) * p.chunk_split;
         const int64_t groups = xcds_per_kv > 0 ? 8 * ceil_div(items, xcds_per_kv) : items * n_kv;
         if (groups > 0x7fffffff) return MQUANT_ERR_UNSUPPORTED;
-        static LdsLimit limit;
-        if (const int st = limit.raise(reinterpret_cast<const void *>(paged_chunk_kernel), kChunkLds); st != MQUANT_OK) return st;
-        MQ_LAUNCH(paged_chunk_kernel, dim3(static_cast<unsigned>(groups)), dim3(256), kChunkLds, stream, a, xcds_per_kv);
+        auto kern = p.chunk_two ? paged_chunk_kernel<2> : paged_chunk_kernel<1>;
+        const int key_groups = p.chunk_two ? 2 : 1;
+        static LdsLimit limits[2];
+        if (const int st = limits[p.chunk_two].raise(reinterpret_cast<const void *>(kern), key_groups * kChunkLds); st != MQUANT_OK) return st;
+        MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(key_groups * 256), key_groups * kChunkLds, stream, a, xcds_per_kv);
         if (const int st = launch_status(); st != MQUANT_OK) return st;
         if (p.chunk_split > 1) {
             MQ_LAUNCH(paged_combine_kernel<true>, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * n_q_heads, 4))), dim3(256), 0,
