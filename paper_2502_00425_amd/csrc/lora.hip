@@ -48,10 +48,12 @@ template <int TR>
 __device__ __forceinline__ int32_t find_tile(const Lora &p, int32_t row0, int32_t tile, int32_t *list, int32_t &n)
 {
     const int lane = threadIdx.x & 63;
-    int32_t key[4];
-    uint64_t left[4], mine[4];
+    const int quarters = p.T - row0 < kBlock ? (p.T - row0 + 63) / 64 : 4;     // that hold rows
+    int32_t key[4] = {0, 0, 0, 0};
+    uint64_t left[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
+        if (q >= quarters) break;
         const int32_t i = row0 + q * 64 + lane;
         key[q] = i < p.T ? p.adapter[i] : -1;
         key[q] = key[q] >= 0 && key[q] < p.n_adapters ? key[q] : p.n_adapters;
@@ -67,6 +69,7 @@ __device__ __forceinline__ int32_t find_tile(const Lora &p, int32_t row0, int32_
         count = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
+            if (q >= quarters) break;
             mine[q] = left[q] & __ballot(key[q] == cur);
             left[q] &= ~mine[q];
             count += __builtin_popcountll(mine[q]);
@@ -107,124 +110,97 @@ __device__ __forceinline__ void split(const float (&f)[8], float down, v8h &hi, 
     }
 }
 
-// h of one tile and slice of K.  The waves take units of 64 channels in turn: x rows are the A operand, rows of A_a the B
+// h of 16 rows and a slice of K.  The waves take units of 64 channels in turn: x rows are the A operand, rows of A_a the B
 // operand of 16x16x32 products, both straight from memory (16 bytes a lane), and their sums meet in LDS by halves.
-template <int RT, int RB>
+template <int RB>
 __global__ __launch_bounds__(kShrinkWaves * 64) void lora_shrink_kernel(Lora p)
 {
-    constexpr int TR = RT * 16;
-    __shared__ __attribute__((aligned(16))) v4f sums[kShrinkWaves / 2][RT * RB][64];
-    int32_t *list = reinterpret_cast<int32_t *>(sums);         // until the sums meet
+    __shared__ int32_t list[16];
+    __shared__ __attribute__((aligned(16))) v4f sums[kShrinkWaves / 2][RB][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
     int32_t n = 0;
-    const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
+    const int32_t id = find_tile<16>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
     if (id < 0 || id == p.n_adapters) return;
     __syncthreads();
 
-    int32_t row[RT];                                           // of y, lane l: row l % 16 of each 16
-    const __half *xr[RT], *ar[RB];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int j = t * 16 + l16;
-        row[t] = list[j < n ? j : n - 1];
-        int32_t src = p.perm ? p.perm[row[t]] : row[t];
-        src = src >= 0 && src < p.T ? src : 0;
-        xr[t] = p.x + src * p.ldx;
-    }
+    const int32_t row = list[l16 < n ? l16 : n - 1];           // of y
+    int32_t src = p.perm ? p.perm[row] : row;
+    src = src >= 0 && src < p.T ? src : 0;
+    const __half *xr = p.x + src * p.ldx, *ar[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int r = b * 16 + l16;
         ar[b] = p.a + (static_cast<int64_t>(id) * p.rank + (r < p.rank ? r : p.rank - 1)) * p.K;
     }
-    v4f acc[RT][RB];
+    v4f acc[RB];
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) acc[t][b] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < RB; ++b) acc[b] = v4f{0.f, 0.f, 0.f, 0.f};
     const int32_t units = (p.K + kUnit - 1) / kUnit, slice = blockIdx.x;
     const int32_t u0 = static_cast<int32_t>(static_cast<int64_t>(units) * slice / p.slices);
     const int32_t u1 = static_cast<int32_t>(static_cast<int64_t>(units) * (slice + 1) / p.slices);
-    v8h xv[RT][2], av[RB][2];
-    // K is a multiple of 8; what lies behind it in the last unit is read from the row's last 8 channels and multiplied by zero
-    auto load = [&](int32_t u) {
+    for (int32_t u = u0 + wave; u < u1; u += kShrinkWaves) {
+        v8h xv[2], av[RB][2];
+        // K is a multiple of 8; what lies behind it in the last unit is read from the row's last 8 channels and multiplied by zero
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int32_t k = u * kUnit + s * 32 + g * 8, at = k < p.K ? k : p.K - 8;
 #pragma unroll
             for (int b = 0; b < RB; ++b) av[b][s] = *reinterpret_cast<const v8h *>(ar[b] + at);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) xv[t][s] = *reinterpret_cast<const v8h *>(xr[t] + at);
+            xv[s] = *reinterpret_cast<const v8h *>(xr + at);
         }
-    };
-    auto multiply = [&](int32_t u) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if ((u + 1) * kUnit > p.K && u * kUnit + s * 32 + g * 8 >= p.K)
+            if ((u + 1) * kUnit > p.K && u * kUnit + s * 32 + g * 8 >= p.K) xv[s] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-                for (int b = 0; b < RB; ++b) av[b][s] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int b = 0; b < RB; ++b) acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[t][s], av[b][s], acc[t][b], 0, 0, 0);
+            for (int b = 0; b < RB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[s], av[b][s], acc[b], 0, 0, 0);
         }
-    };
-    for (int32_t u = u0 + wave; u < u1; u += kShrinkWaves) {
-        load(u);
-        multiply(u);
     }
-    __syncthreads();
 #pragma unroll
     for (int half = kShrinkWaves / 2; half >= 1; half >>= 1) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int b = 0; b < RB; ++b) sums[wave - half][t * RB + b][lane] = acc[t][b];
+            for (int b = 0; b < RB; ++b) sums[wave - half][b][lane] = acc[b];
         __syncthreads();
         if (wave < half)
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int b = 0; b < RB; ++b) acc[t][b] += sums[wave][t * RB + b][lane];
+            for (int b = 0; b < RB; ++b) acc[b] += sums[wave][b][lane];
         __syncthreads();
     }
     if (wave != 0) return;
     float *h = p.h + static_cast<int64_t>(slice) * p.T * p.rank;
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
+    for (int r = 0; r < 4; ++r) {
+        const int j = g * 4 + r;                               // result register r of lane group g is row 4 g + r
+        if (j < n)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t i = __shfl(row[t], g * 4 + r, 64);   // result register r of lane group g is row 4 g + r
-            if (t * 16 + g * 4 + r < n)
-#pragma unroll
-                for (int b = 0; b < RB; ++b)
-                    if (b * 16 + l16 < p.rank) h[i * p.rank + b * 16 + l16] = acc[t][b][r];
-        }
+            for (int b = 0; b < RB; ++b)
+                if (b * 16 + l16 < p.rank) h[static_cast<int64_t>(list[j]) * p.rank + b * 16 + l16] = acc[b][r];
+    }
 }
 
-// y of one tile and `cols` columns.  Y^T = B_a h^T: rows of B_a are the A operand, rows of h the B operand, so that a lane is a row
-// of y.  A-row rho of product s is column 32 (s / 2) + 8 (rho / 4) + 4 (s % 2) + rho % 4 of the wave's 64: a lane's four products hold two
-// times 8 consecutive columns, 16 bytes each.  h goes in as two fp16 parts of h 2^-e, e per row from its largest value: what is lost is
-// 2^-22 of that value, and no magnitude of h overflows.
-template <int RT, int KS, bool VEC>
+// y of 16 rows and `cols` columns, 64 a wave.  Y^T = B_a h^T: rows of B_a are the A operand, rows of h the B operand, so that a lane is a row of
+// y.  A-row rho of product s is column 32 (s / 2) + 8 (rho / 4) + 4 (s % 2) + rho % 4 of the 64: a lane's four products hold two times 8
+// consecutive columns, 16 bytes each.  h goes in as two fp16 parts of h 2^-e, e per row from its largest value: what is lost is 2^-22 of
+// that value, and no magnitude of h overflows.
+template <int KS, bool VEC>
 __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
 {
-    constexpr int TR = RT * 16;
-    __shared__ int32_t list[TR];
-    __shared__ float factors[TR];
-    __shared__ __attribute__((aligned(16))) v8h parts[RT][KS][2][64];
+    __shared__ int32_t list[16];
+    __shared__ float factors[16];
+    __shared__ __attribute__((aligned(16))) v8h parts[KS][2][64];
+    __shared__ __attribute__((aligned(16))) float meet[kExpandWaves - 1][KS][64][8];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x >> 6);
     int32_t n = 0;
-    const int32_t id = find_tile<TR>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
+    const int32_t id = find_tile<16>(p, blockIdx.y * kBlock, blockIdx.z, list, n);
     if (id < 0) return;
     const bool none = id == p.n_adapters;
     if (none && p.y == p.base) return;
     __syncthreads();
 
-    int32_t row[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) row[t] = list[t * 16 + l16 < n ? t * 16 + l16 : n - 1];
-    v8h bv[4][KS], bs[RT][2];
+    const bool mine = l16 < n;
+    const int32_t row = list[mine ? l16 : n - 1];
+    const __half *base = p.base + row * p.ldb;
+    v8h bv[4][KS], bs[2];
     // Rows, columns and ranks behind the last repeat it, so that no load is a branch; what they give is multiplied by zero or not stored
     auto load = [&](int32_t c0) {
         if (!none)
@@ -236,46 +212,38 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
                 for (int k = 0; k < KS; ++k) bv[s][k] = *reinterpret_cast<const v8h *>(br + (k * 32 + g * 8 < p.rank ? k * 32 + g * 8 : p.rank - 8));
             }
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+        for (int w = 0; w < 2; ++w) {
+            const int32_t col = c0 + w * 32 + g * 8;
+            if constexpr (VEC) {
+                bs[w] = *reinterpret_cast<const v8h *>(base + (col < p.N ? col : p.N - 8));
+            } else {
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int32_t col = c0 + w * 32 + g * 8;
-                const __half *base = p.base + row[t] * p.ldb;
-                if constexpr (VEC) {
-                    bs[t][w] = *reinterpret_cast<const v8h *>(base + (col < p.N ? col : p.N - 8));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) bs[t][w][e] = *reinterpret_cast<const _Float16 *>(base + (col + e < p.N ? col + e : p.N - 1));
-                }
+                for (int e = 0; e < 8; ++e) bs[w][e] = *reinterpret_cast<const _Float16 *>(base + (col + e < p.N ? col + e : p.N - 1));
             }
+        }
     };
     const int32_t first = blockIdx.x * p.cols, end = p.N - first < p.cols ? p.N : first + p.cols;
     load(first + wave * kCols);                                // on its way while the rows' parts are prepared
 
-    // The slices of h are added by all waves: wave w takes 16 rows and every SG-th slice; the groups' sums meet in LDS, and one of
-    // them leaves the rows' parts where all waves read them.
-    constexpr int SG = kExpandWaves / RT;
-    const int nsub = (n + 15) / 16;
-    const float scale = none ? 0.0f : p.scale[id];
-    const int t_h = wave / SG, part_h = wave % SG;
+    // The slices of h are added by all waves, every fourth by each; their sums meet in LDS, and the first leaves the rows' parts where all
+    // waves read them.
     float f[KS][8];
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
-    if (!none && t_h < nsub) {
-        const int j = t_h * 16 + l16;
+    if (!none) {
         const int64_t slice = static_cast<int64_t>(p.T) * p.rank;
-        const float *h = p.h + static_cast<int64_t>(list[j < n ? j : n - 1]) * p.rank;
+        const float *h = p.h + static_cast<int64_t>(row) * p.rank;
         constexpr int kAtOnce = KS <= 2 ? 4 : 2;
-        for (int32_t c = part_h; c < p.slices; c += kAtOnce * SG) {
+        for (int32_t c = wave; c < p.slices; c += kAtOnce * kExpandWaves) {
             v4f v[kAtOnce][KS][2];
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {                 // ranks and slices behind the last repeat it
-                    const int r = s * 32 + g * 8;
-                    const float *at = h + (c + i * SG < p.slices ? c + i * SG : c) * slice + (r < p.rank ? r : p.rank - 8);
+                    const int r = s * 32 + g * 8, at_c = c + i * kExpandWaves;
+                    const float *at = h + (at_c < p.slices ? at_c : c) * slice + (r < p.rank ? r : p.rank - 8);
                     v[i][s][0] = reinterpret_cast<const v4f *>(at)[0];
                     v[i][s][1] = reinterpret_cast<const v4f *>(at)[1];
                 }
@@ -285,81 +253,69 @@ __global__ __launch_bounds__(kExpandWaves * 64) void lora_expand_kernel(Lora p)
                 for (int s = 0; s < KS; ++s)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        f[s][e] += c + i * SG < p.slices && s * 32 + g * 8 < p.rank ? v[i][s][e >> 2][e & 3] : 0.0f;
+                        f[s][e] += c + i * kExpandWaves < p.slices && s * 32 + g * 8 < p.rank ? v[i][s][e >> 2][e & 3] : 0.0f;
         }
     }
-    if constexpr (SG > 1) {
-        __shared__ __attribute__((aligned(16))) float meet[RT][SG - 1][KS][64][8];
-        if (part_h > 0)
+    if (wave > 0)
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) meet[wave - 1][s][lane][e] = f[s][e];
+    __syncthreads();
+    if (!none && wave == 0) {
+#pragma unroll
+        for (int o = 0; o < kExpandWaves - 1; ++o)
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) meet[t_h][part_h - 1][s][lane][e] = f[s][e];
-        __syncthreads();
-        if (part_h == 0)
-#pragma unroll
-            for (int o = 0; o < SG - 1; ++o)
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[s][e] += meet[t_h][o][s][lane][e];
-    }
-    if (!none && t_h < nsub && part_h == 0) {
-        float top = 0.0f;
+                for (int e = 0; e < 8; ++e) f[s][e] += meet[o][s][lane][e];
+        float top = 0.0f, down, up;
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[s][e]));
-        float down, up;
         scale_of(top, down, up);
-        if (g == 0) factors[t_h * 16 + l16] = scale * up;
+        if (g == 0) factors[l16] = p.scale[id] * up;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             v8h hi, lo;
             split(f[s], down, hi, lo);
-            parts[t_h][s][0][lane] = hi;
-            parts[t_h][s][1][lane] = lo;
+            parts[s][0][lane] = hi;
+            parts[s][1][lane] = lo;
         }
     }
     __syncthreads();
 
-    float factor[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) factor[t] = factors[t * 16 + l16];
+    const float factor = factors[l16];
+    __half *out = p.y + row * p.ldy;
     for (int32_t c0 = first + wave * kCols; c0 < end; c0 += kExpandWaves * kCols) {
         if (c0 != first + wave * kCols) load(c0);
+        v4f acc[4];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (t >= nsub) break;
-            v4f acc[4];
+        for (int s = 0; s < 4; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (!none)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) acc[s] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int part = 1; part >= 0; --part) {
+                    const v8h hv = parts[k][part][lane];
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[s][k], hv, acc[s], 0, 0, 0);
+                }
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int32_t col = c0 + w * 32 + g * 8;
+            v8h r = bs[w];
             if (!none)
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
+                for (int e = 0; e < 8; ++e)
+                    r[e] = static_cast<_Float16>(__builtin_fmaf(factor, acc[w * 2 + (e >> 2)][e & 3], static_cast<float>(r[e])));
+            if constexpr (VEC) {
+                if (mine && col < p.N) *reinterpret_cast<v8h *>(out + col) = r;
+            } else {
 #pragma unroll
-                    for (int part = 1; part >= 0; --part) {
-                        const v8h hv = parts[t][k][part][lane];
-#pragma unroll
-                        for (int s = 0; s < 4; ++s) acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[s][k], hv, acc[s], 0, 0, 0);
-                    }
-            __half *out = p.y + row[t] * p.ldy;
-            const bool mine = t * 16 + l16 < n;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int32_t col = c0 + w * 32 + g * 8;
-                v8h r = bs[t][w];
-                if (!none)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        r[e] = static_cast<_Float16>(__builtin_fmaf(factor[t], acc[w * 2 + (e >> 2)][e & 3], static_cast<float>(r[e])));
-                if constexpr (VEC) {
-                    if (mine && col < p.N) *reinterpret_cast<v8h *>(out + col) = r;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (mine && col + e < p.N) *reinterpret_cast<_Float16 *>(out + col + e) = r[e];
-                }
+                for (int e = 0; e < 8; ++e)
+                    if (mine && col + e < p.N) *reinterpret_cast<_Float16 *>(out + col + e) = r[e];
             }
         }
     }
@@ -652,7 +608,7 @@ template <int RB>
 int launch_shrink(const Lora &a, bool few, dim3 grid, hipStream_t stream)
 {
     if (few) {
-        MQ_LAUNCH((lora_shrink_kernel<1, RB>), grid, dim3(kShrinkWaves * 64), 0, stream, a);
+        MQ_LAUNCH(lora_shrink_kernel<RB>, grid, dim3(kShrinkWaves * 64), 0, stream, a);
         return launch_status();
     }
     constexpr int lds = 2 * (kRows + RB * 16) * 256;
@@ -668,7 +624,7 @@ int launch_shrink(const Lora &a, bool few, dim3 grid, hipStream_t stream)
 template <int KS, bool VEC>
 int launch_expand(const Lora &a, bool few, dim3 grid, hipStream_t stream)
 {
-    if (few) MQ_LAUNCH((lora_expand_kernel<1, KS, VEC>), grid, dim3(kExpandWaves * 64), 0, stream, a);
+    if (few) MQ_LAUNCH((lora_expand_kernel<KS, VEC>), grid, dim3(kExpandWaves * 64), 0, stream, a);
     else {
         auto kern = lora_expand_rows_kernel<KS, VEC>;
         if constexpr (KS == 4) {
