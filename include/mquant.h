@@ -539,8 +539,8 @@ int mquant_qk_norm_rope(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t
  *   rope_pos_dev        : NULL: the rotation takes pos; else int32 [T], the rotary position ids (models whose
  *                         ids differ from the token's place)
  * A row whose position is negative or beyond the table, or whose page id is outside [0, n_pages), gets no slot:
- * nothing of it is cached (its q is written all the same).  Rows of one sequence with equal positions leave one of them,
- * unspecified which.  q_out_dev may be q_dev as above; the pages must not overlap the rows.
+ * nothing of it is cached (its q is written all the same).  Rows of one sequence have different positions; what a
+ * slot holds that several rows of a call write is unspecified.  q_out_dev may be q_dev as above; the pages must not overlap the rows.
  * n_q_heads may be 0 (q and q_out are then not touched).
  * Errors: as mquant_qk_norm_rope; ERR_NULL (cache or one of its pointers), ERR_BAD_SHAPE (a negative count, n_pages or
  *         table_pages < 1 where there are sequences).

@@ -138,3 +138,72 @@ def test_stale_workspace_and_replays(mq):
         torch.cuda.synchronize()
         check(c, out, what=f"replay {rep}")
         assert torch.equal(mq.lora_apply(x, ids, *rest, base), out)
+
+
+@pytest.mark.parametrize("T,K,N,rank,n", [(200, 264, 257, 24, 3), (513, 520, 333, 40, 2), (1500, 136, 72, 8, 4), (140, 128, 128, 16, 1),
+                                          (256, 1000, 640, 128, 3), (700, 3584, 136, 64, 5), (1100, 8, 1, 8, 2), (300, 392, 1288, 104, 2)])
+def test_many_rows(mq, T, K, N, rank, n):
+    """More rows of an adapter than a tile holds, odd sizes and ranks that are no power of two."""
+    c = make(np.random.default_rng(T * 3 + rank), T, K, N, rank, n)
+    check(c, call(mq, c), what=f"{T} {K} {N} r{rank}")
+
+
+@pytest.mark.parametrize("ids", ["one", "none", "runs", "each its own", "alternating", "last row only"])
+def test_who_has_which_adapter_among_many_rows(mq, ids):
+    T, n = 700, 20
+    rows = {"one": np.full(T, 3), "none": np.where(np.arange(T) % 2, -1, n), "runs": np.arange(T) // 90, "each its own": np.arange(T) % n,
+            "alternating": np.where(np.arange(T) % 2, 0, 19), "last row only": np.where(np.arange(T) == T - 1, 5, -5)}[ids]
+    c = make(np.random.default_rng(11), T, 256, 264, 16, n, ids=rows)
+    check(c, call(mq, c), what=ids)
+
+
+def test_many_rows_in_place_with_strides(mq):
+    rng = np.random.default_rng(12)
+    for N in (96, 91):
+        c = make(rng, 300, 128, N, 32, 3)
+        y = torch.full((300, N + 21), 2.0, dtype=torch.float16, device="cuda")
+        y[:, 5:5 + N] = dev(c["base"])
+        mq.lora_apply(dev(c["x"]), dev(c["ids"]), dev(c["a"]), dev(c["b"]), dev(c["scale"]), y[:, 5:5 + N], out=y[:, 5:5 + N])
+        check(c, y[:, 5:5 + N], what="in place")
+        assert bool((y[:, :5] == 2).all()) and bool((y[:, 5 + N:] == 2).all())
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_results_repeat_and_two_streams_run_at_once(mq, T):
+    """The same bits every time, also with another call on another stream beside it."""
+    rng = np.random.default_rng(13)
+    c = make(rng, T, 2048, 520, 32, 4)
+    t = [dev(c[k]) for k in ("x", "ids", "a", "b", "scale", "base")]
+    want = mq.lora_apply(*t)
+    check(c, want, what="alone")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(10):
+        for s in streams:
+            with torch.cuda.stream(s):
+                outs.append(mq.lora_apply(*t))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_many_rows_replayed(mq):
+    rng = np.random.default_rng(14)
+    c = make(rng, 260, 1024, 136, 64, 3)
+    x, ids, base = dev(c["x"]), dev(c["ids"]), dev(c["base"])
+    rest = dev(c["a"]), dev(c["b"]), dev(c["scale"])
+    ws = torch.empty(mq.lora_workspace_bytes(260, 1024, 64), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(base)
+    run = lambda: mq.lora_apply(x, ids, *rest, base, out=out, workspace=ws)
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for rep in range(3):
+        c["ids"] = rng.integers(-1, 4, 260).astype(np.int32)
+        ids.copy_(dev(c["ids"]))
+        ws.fill_(0xff)
+        g.replay()
+        torch.cuda.synchronize()
+        check(c, out, what=f"replay {rep}")

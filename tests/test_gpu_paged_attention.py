@@ -213,3 +213,81 @@ def test_captured_step_follows_its_lengths(mq):
         eager = torch.full_like(out, 5.0)
         mq.paged_attention(q, cache, start, pos, hq, 3, 600, out=eager)
         assert torch.equal(eager, out)
+
+
+@pytest.mark.parametrize("seqs,hq,hkv", [([(1, 150)], 8, 8), ([(3, 40), (1, 161)], 8, 8), ([(100, 170)], 8, 8)])
+def test_pages_beyond_32_bits(mq, seqs, hq, hkv):
+    """Pages whose offset passes 2^31 halves (4.3 GB of pages each): the same bits as from a small cache."""
+    rng = np.random.default_rng(12)
+    st = make_step(rng, seqs, hq, hkv, 128, poison=False)
+    q, cache, start, pos, _ = device_step(mq, st)
+    small = mq.paged_attention(q, cache, start, pos, hq)
+    check(st, small, what="small")
+    n = (1 << 31) // (hkv * 128 * D) + len(st["kp"]) + 1
+    up = n - len(st["kp"])
+    big = []
+    for p in (cache.k_pages, cache.v_pages):
+        b = torch.zeros((n, hkv, 128, D), dtype=torch.float16, device="cuda")
+        b[up:] = p
+        big.append(b)
+    table = torch.where(cache.page_table >= 0, cache.page_table + up, cache.page_table)
+    assert torch.equal(mq.paged_attention(q, mq.PagedCache(*big, table), start, pos, hq), small)
+
+
+def test_results_repeat_and_two_streams_run_at_once(mq):
+    """The same bits every time, also with other calls on another stream beside them (each with a workspace of its own)."""
+    rng = np.random.default_rng(13)
+    for seqs in ([(1, 1500), (1, 200)], [(4, 900)], [(90, 1100), (1, 700)]):
+        st = make_step(rng, seqs, 14, 2, 16)
+        t = device_step(mq, st)
+        want = mq.paged_attention(*t, *bounds_of(st))
+        check(st, want, what="alone")
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        outs = []
+        for _ in range(10):
+            for s in streams:
+                with torch.cuda.stream(s):
+                    outs.append(mq.paged_attention(*t, *bounds_of(st)))
+        torch.cuda.synchronize()
+        mine = torch.from_numpy(np.concatenate([np.arange(a, b) for a, b in zip(st["start"], st["start"][1:])])).cuda()
+        assert all(torch.equal(o[mine], want[mine]) for o in outs)
+
+
+def test_two_graphs_that_share_a_workspace(mq):
+    """A decode step and a chunk captured with the same scratch memory and replayed in turn, eager work between."""
+    rng = np.random.default_rng(14)
+    steps = [make_step(rng, seqs, 14, 2, 16, poison=False) for seqs in ([(1, 1500), (1, 900)], [(60, 1500)])]
+    args = [(*device_step(mq, st), *bounds_of(st)) for st in steps]
+    need = max(mq.paged_attention_workspace_bytes(a[0].shape[0], a[1], 14, *a[5:]) for a in args)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    outs, graphs = [torch.zeros_like(a[0]) for a in args], []
+    for a, o in zip(args, outs):
+        mq.paged_attention(*a, out=o, workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            mq.paged_attention(*a, out=o, workspace=ws)
+    for rep in range(3):
+        for st, a, o, g in zip(steps, args, outs, graphs):
+            o.zero_()
+            g.replay()
+            check(st, o, what=f"replay {rep}")
+            assert torch.equal(mq.paged_attention(*a), o)
+
+
+def test_routes(mq):
+    """Which kernels a step's bounds choose: few queries, chunks, both, and the join of pieces where slots are split."""
+    from kernel_trace import kernels
+    rng = np.random.default_rng(15)
+    for seqs, hq, hkv, bounds, want in [
+            ([(1, 100)], 28, 4, True, ["paged_few_kernel<1>"]), ([(1, 1281)], 28, 4, True, ["paged_few_kernel<1>", "paged_combine_kernel<false>"]),
+            ([(5, 300)], 28, 4, True, ["paged_few_kernel<3>", "paged_combine_kernel<false>"]),
+            ([(7, 60)], 28, 4, True, ["paged_chunk_kernel<2>"]), ([(1300, 1300)], 28, 4, True, ["paged_chunk_kernel<1>"]),
+            ([(20, 3000)], 28, 4, True, ["paged_chunk_kernel<2>", "paged_combine_kernel<true>"]),
+            ([(100, 200), (1, 100)], 4, 2, False, ["paged_chunk_kernel<2>", "paged_few_kernel<3>", "paged_combine_kernel<false>"])]:
+        st = make_step(rng, seqs, hq, hkv, 16, poison=False)
+        args = (*device_step(mq, st), *(bounds_of(st) if bounds else (0, 0)))
+        names = kernels(lambda: mq.paged_attention(*args))
+        assert [n for n in names if "paged" in n] == want, (seqs, names)

@@ -159,3 +159,39 @@ def test_append_beyond_32_bits(mq):
     assert int(torch.count_nonzero(vp[n_pages - 1])) <= hkv * D and not bool(vp[:4].any())
     o = mq.paged_attention(q, cache, dev(np.array([0, 1], dtype=np.int32)), dev(np.array([77], dtype=np.int32)), 8, max_kv=78)
     assert np.isfinite(host(o)).all()
+
+
+@pytest.mark.parametrize("T", [7, 900])
+def test_append_captured(mq, T):
+    """A captured append replayed while rows, positions and pages change under it, eager work between."""
+    rng = np.random.default_rng(T)
+    hq, hkv, page, n_pages = 28, 4, 16, 140
+    x = dev(rng.standard_normal((T, (hq + 2 * hkv) * D)).astype(np.float16))
+    q, k, v = x[:, :hq * D], x[:, hq * D:(hq + hkv) * D], x[:, (hq + hkv) * D:]
+    table = dev(rng.permutation(n_pages)[:130].reshape(2, 65).astype(np.int32))
+    start, pos = dev(np.array([0, 2, T], dtype=np.int32)), dev(np.arange(T, dtype=np.int32))
+    w = dev(rng.uniform(0.5, 1.5, D).astype(np.float16))
+    cache = mq.PagedCache(*(torch.zeros((n_pages, hkv, page, D), dtype=torch.float16, device="cuda") for _ in range(2)), table)
+    qo = torch.zeros((T, hq * D), dtype=torch.float16, device="cuda")
+    run = lambda c, o: mq.kv_append(q, k, v, c, start, pos, hq, w, w, q_out=o)
+    run(cache, qo)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run(cache, qo)
+    for rep in range(3):
+        x.copy_(dev(rng.standard_normal(x.shape).astype(np.float16)))
+        pos.copy_(dev(rng.permutation(1040)[:T].astype(np.int32)))
+        start.copy_(dev(np.array([0, rep, T - rep], dtype=np.int32)))
+        table.copy_(dev(rng.permutation(n_pages)[:130].reshape(2, 65).astype(np.int32)))
+        cache.k_pages.zero_(), cache.v_pages.zero_(), qo.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        kp, vp, o = cache.k_pages.clone(), cache.v_pages.clone(), qo.clone()
+        cache.k_pages.zero_(), cache.v_pages.zero_()
+        o2 = torch.zeros_like(o)
+        run(cache, o2)
+        assert torch.equal(cache.k_pages, kp) and torch.equal(cache.v_pages, vp) and torch.equal(o, o2)
+        ref = orc.qk_norm_rope_f64(host(q), w.cpu().numpy(), pos.cpu().numpy(), hq)
+        check(host(o)[:T - rep], ref[:T - rep], f"replay {rep}")
+        assert bool(vp.any()) and not bool(o[T - rep:].any())
