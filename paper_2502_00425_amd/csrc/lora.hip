@@ -604,6 +604,11 @@ int64_t many_slices(int32_t T, int32_t K)
 constexpr int32_t kFewMax = 1024;
 bool few_rows(int32_t T, int32_t n_adapters) { return T <= 128 || (T <= kFewMax && n_adapters >= T / 16); }
 
+// The expansion on its own: with many columns reading B_a for 64 rows at once is worth empty places in a tile from a few tiles of 16 on (N = 37888,
+// tiles of 64 / of 16, rank 16 and 64: 100 rows of one adapter 7.6 / 9.3 and 10.1 / 18.6, 156 rows of 15 adapters, each another, 22.5 / 18.9
+// and 31.0 / 33.1, 300 of 20 39.7 / 53.7 and 54.3 / 84.5).
+bool few_rows_to_expand(int32_t T, int32_t N, int32_t n_adapters) { return T <= 64 || (N < 16384 && few_rows(T, n_adapters)); }
+
 template <int RB>
 int launch_shrink(const Lora &a, bool few, dim3 grid, hipStream_t stream)
 {
@@ -666,32 +671,36 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     if (!aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
-    const bool few = few_rows(T, n_adapters);
+    const bool few = few_rows(T, n_adapters), few_to_expand = few_rows_to_expand(T, N, n_adapters);
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
                  n_adapters, static_cast<int32_t>(few ? few_slices(K) : many_slices(T, K)),
-                 few ? kExpandWaves * kCols : 512};
+                 few_to_expand ? kExpandWaves * kCols : 512};
+    // Few rows: a block of columns a wave, two of many columns (34 rows of 12 adapters, rank 32, N = 37888, one / two / four: 11.4 / 8.5 / 9.0 us, 64 of 3,
+    // rank 64, 15.7 / 12.4 / 12.7, 4 of 4, rank 16, 4.6 / 4.9 / 5.8; N = 10240, 48 of 12, rank 16, 5.8 / 5.9 / 6.8).
+    if (few_to_expand && N >= 16384 && T > 8) args.cols *= 2;
     // Many rows: 512 columns a work-group, which prepares its rows once for all of them, fewer where that leaves compute units idle (K = 3584,
     // N = 4608, rank 64, expansion with 128 / 256 / 512 / 1024 columns: 128 rows 9.1 / 10.4 / 13.4 / 18.9 us, 1024 15.7 / 14.8 / 16.3 / 21.2, 4096
     // 28.2 / 24.4 / 21.7 / 23.1).
-    while (!few && args.cols > 128 && ceil_div(T, kRows) * ceil_div(N, args.cols) < kNumCU) args.cols /= 2;
+    while (!few_to_expand && args.cols > 128 && ceil_div(T, kRows) * ceil_div(N, args.cols) < kNumCU) args.cols /= 2;
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
+    if (blocks > 65535) return MQUANT_ERR_UNSUPPORTED;
     // Tiles of 256 rows: full ones, and a last one of every adapter (and of the rows without), which may not be there: those come last in
     // the grids.
-    const int32_t in_block = T < kBlock ? T : kBlock;
-    const int32_t tiles = in_block / (few ? 16 : kRows) + (n_adapters < in_block ? n_adapters + 1 : in_block);
-    if (blocks > 65535) return MQUANT_ERR_UNSUPPORTED;
+    auto tiles = [&](int32_t rows) {
+        const int32_t in_block = T < kBlock ? T : kBlock;
+        return static_cast<unsigned>(in_block / rows + (n_adapters < in_block ? n_adapters + 1 : in_block));
+    };
     if (n_adapters > 0) {
-        const dim3 grid(static_cast<unsigned>(args.slices), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
+        const dim3 grid(static_cast<unsigned>(args.slices), static_cast<unsigned>(blocks), tiles(few ? 16 : kRows));
         const int st = rank <= 16 ? launch_shrink<1>(args, few, grid, stream) : rank <= 32 ? launch_shrink<2>(args, few, grid, stream)
                      : rank <= 64 ? launch_shrink<4>(args, few, grid, stream) : launch_shrink<8>(args, few, grid, stream);
         if (st != MQUANT_OK) return st;
     }
-    const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(blocks), static_cast<unsigned>(tiles));
-    const bool vec = N % 8 == 0 && ldb % 8 == 0 && ldy % 8 == 0 && aligned_to(base, 16) && aligned_to(y, 16);
-    if (vec)
-        return rank <= 32 ? launch_expand<1, true>(args, few, grid, stream) : rank <= 64 ? launch_expand<2, true>(args, few, grid, stream)
-                                                                                         : launch_expand<4, true>(args, few, grid, stream);
-    return rank <= 32 ? launch_expand<1, false>(args, few, grid, stream) : rank <= 64 ? launch_expand<2, false>(args, few, grid, stream)
-                                                                                      : launch_expand<4, false>(args, few, grid, stream);
+    const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(blocks), tiles(few_to_expand ? 16 : kRows));
+    if (N % 8 == 0 && ldb % 8 == 0 && ldy % 8 == 0 && aligned_to(base, 16) && aligned_to(y, 16))
+        return rank <= 32 ? launch_expand<1, true>(args, few_to_expand, grid, stream)
+             : rank <= 64 ? launch_expand<2, true>(args, few_to_expand, grid, stream) : launch_expand<4, true>(args, few_to_expand, grid, stream);
+    return rank <= 32 ? launch_expand<1, false>(args, few_to_expand, grid, stream)
+         : rank <= 64 ? launch_expand<2, false>(args, few_to_expand, grid, stream) : launch_expand<4, false>(args, few_to_expand, grid, stream);
 }

@@ -856,9 +856,13 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
         const int64_t m = most * G < kFew ? most * G : kFew;
         p.few_nq = m <= 16 ? 1 : 3;
         p.few_stride = static_cast<int32_t>(ceil_div(m, 16 * p.few_nq) * 16 * p.few_nq);
-        // Pieces: as few as keep the compute units busy, since each costs a work-group's way in and out; more of them where the sequences
-        // alone are enough and their lengths may differ.
-        int64_t split = ceil_div(units < kNumCU ? kNumCU : 1024, units);
+        // Pieces: each costs a work-group's way in and out and a share of the join, and one work-group to a compute unit is enough to
+        // keep the memory busy; but host and device know a longest sequence only, and a long one among short ones must not be what
+        // the launch waits for.  us by pieces: 64 heads on 8, 7 sequences of 15000 slots 4 79.4, 9 81.0, 18 84.7; 20 of 6000 1 84.3, 3 91.6, 6 95.2, 20
+        // of 600 to 6000 1 44.3, 3 42.9, 6 39.7; 32 of 8192 1 182, 2 189, 4 194, 32 of 500 to 16384 1 177, 2 184, 4 125, 8 131; 28 on 4, 8 of 1000 to
+        // 16000 8 24.4, 16 26.7, 32 28.5, 64 of 100 to 8000 1 56.9, 2 58.8, 4 47.5, 16 49.3.
+        int64_t split = units < kNumCU / 2 ? kNumCU / units : units < kNumCU ? ceil_div(2 * kNumCU, units) : ceil_div(4 * kNumCU, units);
+        if (units < kNumCU / 2 && split < ceil_div(kv, 4096)) split = ceil_div(kv, 4096);
         if (split > ceil_div(kv, kFewStep)) split = ceil_div(kv, kFewStep);
         p.few_piece = static_cast<int32_t>(ceil_div(ceil_div(kv, split), kFewStep) * kFewStep);
         p.few_split = static_cast<int32_t>(ceil_div(kv, p.few_piece));
