@@ -119,6 +119,8 @@ __device__ __forceinline__ int32_t pieces_of(const Step &a, int32_t limit)
 // product, so about 14 of the 16 KiB are in flight all the time, for 8 waves a compute unit.
 // Key chunk c (16 bytes) of row r lies at chunk c ^ (r & 15): a fragment read takes one chunk of 16 rows.  Value chunk c lies
 // at c ^ 2 (r & 7): a transposing read takes 32 bytes of 8 rows.
+// NQ: 16 queries each, all of them computed, whatever a sequence has (skipping the ones behind the last query cost the others
+// the overlap of their products and exponentials: 20.4 against 17.7 us at 8 sequences of 5 rows x 28 heads over 4096 slots).
 template <int NQ>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 {
@@ -201,12 +203,16 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
             for (int it = 0; it < n; ++it) {
                 const int32_t slot0 = (tile0 + it * kFewWaves) * kFewSlots;
                 wait_copies<8>();                              // keys are there, values may be on the way
+                // For the compiler, other addresses in every tile: the sums of each fragment read, held through the walk, and those of the
+                // way out below spilled ten registers at NQ = 3 (11 % of the time of 35 queries over 4096 slots).
+                uint32_t k_at = k_lds + l16 * 256, v_at = v_lds;
+                asm volatile("" : "+v"(k_at), "+v"(v_at));
                 v8h kf[2][4];
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        kf[kb][ks] = *(v8h_lds_ptr)(uintptr_t)(k_lds + kb * 4096 + l16 * 256 + (((ks * 4 + g) ^ l16) << 4));
+                        kf[kb][ks] = *(v8h_lds_ptr)(uintptr_t)(k_at + kb * 4096 + (((ks * 4 + g) ^ l16) << 4));
                 wait_lgkm0();
                 asm volatile("" ::: "memory");
                 const bool more = it + 1 < n;
@@ -214,7 +220,6 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
                 v8h p[NQ];
 #pragma unroll
                 for (int u = 0; u < NQ; ++u) {
-                    if (u >= nq) break;
                     v4f s[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
@@ -267,7 +272,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
                 // Operand slot j of lane group g is the slot that score register j holds there: 4 g + j, 16 + 4 g + j - 4.  A transposing
                 // read takes, per 16 lanes, the 32 bytes of four rows that lanes 4 r .. 4 r + 3 point at, and gives lane i channel i.
                 const int vr = 4 * g + ((lane >> 2) & 3);
-                const uint32_t v_row = v_lds + vr * 256 + (lane & 1) * 8;
+                const uint32_t v_row = v_at + vr * 256 + (lane & 1) * 8;
 #pragma unroll
                 for (int cb = 0; cb < 8; ++cb) {
                     union {
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
                     vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4f16((tr4_lds_ptr)(uintptr_t)(at + 4096));
 #pragma unroll
                     for (int u = 0; u < NQ; ++u)
-                        if (u < nq) acc[u][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf.f8, p[u], acc[u][cb], 0, 0, 0);
+                        acc[u][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf.f8, p[u], acc[u][cb], 0, 0, 0);
                 }
                 wait_lgkm0();
                 asm volatile("" ::: "memory");
@@ -288,6 +293,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
         }
 
         // ---- the four waves meet in LDS, 16 queries at a time: thread t finishes 8 channels of query t / 16
+        int t = tid;
+        asm volatile("" : "+v"(t));
         float *sums = reinterpret_cast<float *>(smem);                          // [4][16][kFewPitch]
         float2 *ml = reinterpret_cast<float2 *>(smem + kFewWaves * 16 * kFewPitch * 4);        // [4][16]
         static_assert(kFewWaves * 16 * (kFewPitch * 4 + 8) <= kFewLds, "exchange of the waves");
@@ -303,7 +310,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
                 *reinterpret_cast<v4f *>(sums + (wave * 16 + l16) * kFewPitch + cb * 16 + g * 4) = acc[u][cb];
             if (g == 0) ml[wave * 16 + l16] = make_float2(m_ref[u], l);
             __syncthreads();
-            const int qi = tid >> 4, ch = (tid & 15) * 8;
+            const int qi = t >> 4, ch = (t & 15) * 8;
             const int32_t m = m0 + u * 16 + qi;
             if (m < M) {
                 float top_m = -INFINITY, den = 0.0f, f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -854,8 +861,8 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
     const int64_t units = static_cast<int64_t>(n_seq) * n_kv, kv = max_kv > 0 ? max_kv : 1;
     if (p.few) {
         const int64_t m = most * G < kFew ? most * G : kFew;
-        p.few_nq = m <= 16 ? 1 : 3;
-        p.few_stride = static_cast<int32_t>(ceil_div(m, 16 * p.few_nq) * 16 * p.few_nq);
+        p.few_nq = static_cast<int32_t>(ceil_div(m, 16));
+        p.few_stride = 16 * p.few_nq;
         // Pieces: each costs a work-group's way in and out and a share of the join, and one work-group to a compute unit is enough to
         // keep the memory busy; but host and device know a longest sequence only, and a long one among short ones must not be what
         // the launch waits for.  us by pieces: 64 heads on 8, 7 sequences of 15000 slots 4 79.4, 9 81.0, 18 84.7; 20 of 6000 1 84.3, 3 91.6, 6 95.2, 20
@@ -945,9 +952,9 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
         a.part_ml += p.chunk_part;
         const int64_t units = static_cast<int64_t>(cache->n_seq) * n_kv, groups = units * p.few_split;
         if (groups > 0x7fffffff) return MQUANT_ERR_UNSUPPORTED;
-        auto kern = p.few_nq == 1 ? paged_few_kernel<1> : paged_few_kernel<3>;
-        static LdsLimit limits[2];
-        if (const int st = limits[p.few_nq == 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
+        auto kern = p.few_nq == 1 ? paged_few_kernel<1> : p.few_nq == 2 ? paged_few_kernel<2> : paged_few_kernel<3>;
+        static LdsLimit limits[3];
+        if (const int st = limits[p.few_nq - 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
         MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(kFewWaves * 64), kFewLds, stream, a);
         if (const int st = launch_status(); st != MQUANT_OK) return st;
         if (p.few_split > 1) {

@@ -53,6 +53,8 @@ STEPS = {
     "one kv head": ([(1, 200), (1, 77)], 71, 1, 16),
     "drafts": ([(5, 300), (3, 90), (1, 17), (9, 9)], 28, 4, 16),
     "drafts, long": ([(5, 2100), (4, 1111)], 7, 1, 64),
+    "drafts of 17 to 32 queries": ([(3, 300), (4, 1111), (1, 40), (2, 2)], 28, 4, 16),
+    "24 heads on one": ([(1, 900), (1, 3), (1, 31)], 24, 1, 16),
     "a prompt": ([(130, 130)], 4, 2, 16),
     "a ragged prompt": ([(77, 77)], 28, 4, 64),
     "a chunk": ([(100, 700)], 8, 2, 16),
