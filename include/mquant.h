@@ -597,8 +597,8 @@ int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t rank);
  *                 overlap; 16-byte accesses where N, ldb and ldy are multiples of 8 and both are 16-byte aligned
  *   workspace_dev : mquant_lora_workspace_bytes(T, K, rank) bytes, 256-byte aligned; scratch, concurrent
  *                 calls must not share it
- * rank: a multiple of 8 up to 128, K a multiple of 8 (ERR_UNSUPPORTED otherwise).  Rows of one adapter next to each
- * other are the fast case; any order is right.
+ * rank: a multiple of 8 up to 128, K a multiple of 8, K and N at most 2^30, T at most 65535 * 256 (ERR_UNSUPPORTED
+ * otherwise).  Rows of one adapter next to each other are the fast case; any order is right.
  * T == 0 or N == 0 is a no-op.  Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_ALIGNMENT.
  */
 int mquant_lora_apply(const void *x_dev, int64_t ldx, const int32_t *perm_dev, const int32_t *adapter_dev,

@@ -24,6 +24,7 @@ constexpr int kUnit = 64;                  // channels of K that a wave takes at
 constexpr int kExpandWaves = 4;
 constexpr int kCols = 64;                  // columns of y that a wave takes at a time
 constexpr int kMaxSlices = 16;             // of few rows
+constexpr int32_t kMaxSide = 1 << 30;      // of K and N: kernels step past their end in 32 bits
 
 struct Lora {
     const __half *x;
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(256) void lora_expand_rows_kernel(Lora p)
     const int sh = shift < 4 ? 4 : shift;
     auto copy_b = [&](int32_t block, int buffer) {
         const uint8_t *from = reinterpret_cast<const uint8_t *>(p.b + (static_cast<int64_t>(id) * p.N + first + block * 128) * p.rank);
-        const int32_t last = (p.N - first - block * 128) * chunks - 1;         // chunks behind the last row repeat its last one
+        const int32_t rest = p.N - first - block * 128, last = (rest < 128 ? rest : 128) * chunks - 1;     // chunks behind the last row repeat its last one
         for (int i = wave; i < pieces; i += 4) {
             const int32_t at = i * 64 + lane, q = (at & ~15) | ((at & 15) ^ ((at >> sh) & 15));
             lds_dma16_lane_address(from + static_cast<int64_t>(q < last ? q : last) * 16, lds0 + buffer * buffer_bytes + i * 1024);
@@ -661,6 +662,7 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     if (N < 0 || n_adapters < 0) return MQUANT_ERR_BAD_SHAPE;
     const int64_t need = mquant_lora_workspace_bytes(T, K, rank);
     if (need < 0) return static_cast<int>(need);
+    if (N > kMaxSide || K > kMaxSide) return MQUANT_ERR_UNSUPPORTED;
     if (T == 0 || N == 0) return MQUANT_OK;
     if (!x || !adapter || !base || !y || (n_adapters > 0 && (!a || !b || !scale))) return MQUANT_ERR_NULL;
     if (ldx < K || ldb < N || ldy < N || (y == base && ldy != ldb)) return MQUANT_ERR_BAD_SHAPE;

@@ -93,6 +93,8 @@ def test_attention_refusals():
         assert call(**big, ws=P + 16) == mq.ERR_ALIGNMENT
     assert size(-1, 2, 28, 4, 128, 0, 100) == mq.ERR_BAD_SHAPE and size(2, 2, 28, 3, 128, 0, 100) == mq.ERR_BAD_SHAPE
     assert size(2, 2, 28, 4, 96, 0, 100) == mq.ERR_UNSUPPORTED
+    assert size(1 << 24, 1, 64, 8, 128, 0, 100) >= 0 and size((1 << 24) + 1, 1, 64, 8, 128, 0, 100) == mq.ERR_UNSUPPORTED
+    assert call(T=1 << 30, hq=4) == mq.ERR_UNSUPPORTED
     assert size(0, 0, 28, 4, 128, 0, 0) == 0
 
 
@@ -110,7 +112,8 @@ def test_adapter_refusals():
         assert call(**bad) == mq.ERR_BAD_SHAPE, bad
     for bad in (dict(x=None), dict(ids=None), dict(a=None), dict(b=None), dict(scale=None), dict(base=None), dict(y=None)):
         assert call(**bad) == mq.ERR_NULL, bad
-    for bad in (dict(rank=12), dict(rank=136), dict(K=516, ldx=520), dict(K=0)):
+    for bad in (dict(rank=12), dict(rank=136), dict(K=516, ldx=520), dict(K=0), dict(K=(1 << 30) + 8, ldx=1 << 31, ws_bytes=1 << 50),
+                dict(N=(1 << 30) + 1, ldb=1 << 31, ldy=1 << 31), dict(T=65536 * 256, ws_bytes=1 << 50)):
         assert call(**bad) == mq.ERR_UNSUPPORTED, bad
     for bad in (dict(x=P + 8), dict(ldx=516), dict(a=P + 2), dict(b=P + 8), dict(base=P + 1), dict(y=Q + 1), dict(ids=P + 2),
                 dict(perm=P + 2), dict(scale=P + 2), dict(ws=P + 16)):
