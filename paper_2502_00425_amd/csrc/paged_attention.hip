@@ -296,9 +296,11 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
         // ---- the four waves meet in LDS, 16 queries at a time: thread t finishes 8 channels of query t / 16
         int t = tid;
         asm volatile("" : "+v"(t));
+        const int my_q = t & 15, my_ch = (t >> 4 & 3) * 4;
         float *sums = reinterpret_cast<float *>(smem);                          // [4][16][kFewPitch]
         float2 *ml = reinterpret_cast<float2 *>(smem + kFewWaves * 16 * kFewPitch * 4);        // [4][16]
-        static_assert(kFewWaves * 16 * (kFewPitch * 4 + 8) <= kFewLds, "exchange of the waves");
+        int32_t *lims = reinterpret_cast<int32_t *>(ml + kFewWaves * 16);       // [16]
+        static_assert(kFewWaves * 16 * (kFewPitch * 4 + 8) + 16 * 4 <= kFewLds, "exchange of the waves");
 #pragma unroll
         for (int u = 0; u < NQ; ++u) {
             if (u >= nq) break;
@@ -308,8 +310,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
             __syncthreads();
 #pragma unroll
             for (int cb = 0; cb < 8; ++cb)
-                *reinterpret_cast<v4f *>(sums + (wave * 16 + l16) * kFewPitch + cb * 16 + g * 4) = acc[u][cb];
-            if (g == 0) ml[wave * 16 + l16] = make_float2(m_ref[u], l);
+                *reinterpret_cast<v4f *>(sums + (wave * 16 + my_q) * kFewPitch + cb * 16 + my_ch) = acc[u][cb];
+            if (my_ch == 0) ml[wave * 16 + my_q] = make_float2(m_ref[u], l);
+            if (t < 16) lims[t] = lim[u];
             __syncthreads();
             const int qi = t >> 4, ch = (t & 15) * 8;
             const int32_t m = m0 + u * 16 + qi;
@@ -325,7 +328,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] += share * sums[(w * 16 + qi) * kFewPitch + ch + e];
                 }
-                const int32_t row = rows.x + m / a.group, limit = limit_of(a, row);
+                const int32_t row = rows.x + m / a.group, limit = lims[qi];
                 if (!split || pieces_of(a, limit) <= 1) {
                     if (piece == 0) {
                         const float inv = den > 0.0f ? 1.0f / den : 0.0f;       // a row that sees nothing: zeros
@@ -779,29 +782,40 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
         at = item;
         stride = static_cast<int64_t>(units) * a.few_stride;
     }
-    const int32_t n = pieces_of(a, limit_of(a, row));
-    if (!CHUNK && n <= 1) return;
-    float top = -INFINITY;
-    for (int32_t p = lane; p < n; p += 64) top = fmaxf(top, a.part_ml[at + p * stride].x);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const int32_t limit = limit_of(a, row);
     const int ch = (lane & 15) * 8, quarter = lane >> 4;
-    float den = 0.0f, f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, den = 0.0f, f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     constexpr int kAtOnce = 4;
+    int32_t n = a.n_split;
     for (int32_t p0 = 0; p0 < n; p0 += 4 * kAtOnce) {
         v4f v[kAtOnce][2];
         float2 ml[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {                    // pieces behind the last repeat it
+        for (int i = 0; i < kAtOnce; ++i) {                    // asked for before the row's limit is there: what lies in pieces behind it is not used
             const int32_t p = p0 + i * 4 + quarter;
-            const int64_t from = at + (p < n ? p : n - 1) * stride;
+            const int64_t from = at + (p < a.n_split ? p : a.n_split - 1) * stride;
+            ml[i] = a.part_ml[from];
             v[i][0] = *reinterpret_cast<const v4f *>(a.part + from * kD + ch);
             v[i][1] = *reinterpret_cast<const v4f *>(a.part + from * kD + ch + 4);
-            ml[i] = a.part_ml[from];
         }
+        n = pieces_of(a, limit);
+        if (!CHUNK && n <= 1) return;
+        float top_p = top;
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-            if (p0 + i * 4 + quarter >= n || ml[i].x == -INFINITY) continue;
+            if (p0 + i * 4 + quarter >= n) ml[i].x = -INFINITY;
+            top_p = fmaxf(top_p, ml[i].x);
+        }
+        top_p = fmaxf(top_p, __shfl_xor(top_p, 16, 64));
+        top_p = fmaxf(top_p, __shfl_xor(top_p, 32, 64));
+        const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - top_p) * a.scale_log2e);
+        top = top_p;
+        den *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= keep;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (ml[i].x == -INFINITY) continue;
             const float share = __builtin_amdgcn_exp2f((ml[i].x - top) * a.scale_log2e);
             den = __builtin_fmaf(share, ml[i].y, den);
 #pragma unroll

@@ -279,6 +279,19 @@ def test_two_graphs_that_share_a_workspace(mq):
             assert torch.equal(mq.paged_attention(*a), o)
 
 
+@pytest.mark.parametrize("fill", [float("nan"), float("inf"), float("-inf"), 3e38])
+def test_scratch_holds_anything(mq, fill):
+    """What a workspace held before the call leaves no trace: sequences with fewer pieces than the longest one among them."""
+    rng = np.random.default_rng(16)
+    for seqs, hq, hkv in ([(1, 3000), (1, 130), (1, 900)], 28, 4), ([(5, 2500), (4, 300), (3, 129)], 28, 4), ([(3, 2500), (3, 257)], 28, 4), \
+            ([(60, 2600), (50, 90), (40, 1200)], 7, 1), ([(60, 2600), (1, 1200), (2, 5)], 8, 2):
+        st = make_step(rng, seqs, hq, hkv, 16)
+        need = mq.paged_attention_workspace_bytes(st["T"], device_step(mq, st)[1], hq, *bounds_of(st))
+        assert need > 0
+        ws = torch.full((need // 4,), fill, dtype=torch.float32, device="cuda")
+        check(st, mq.paged_attention(*device_step(mq, st), *bounds_of(st), workspace=ws), what=f"{seqs} {fill}")
+
+
 def test_routes(mq):
     """Which kernels a step's bounds choose: few queries, chunks, both, and the join of pieces where slots are split."""
     from kernel_trace import kernels
