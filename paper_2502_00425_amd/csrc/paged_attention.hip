@@ -394,16 +394,18 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     const int32_t piece = item % a.n_split;
     int32_t left = item / a.n_split;
     int32_t seq = -1, tile = 0;
+    int2 rows = make_int2(0, 0);
     for (int32_t at = 0; at < a.c.n_seq; at += 64) {
         int32_t s = a.c.n_seq - 1 - at - lane;
         int32_t tiles = 0, length = -1;
+        int2 r = make_int2(0, 0);
         if (s >= 0) {
-            const int2 r = rows_of(a, s);
+            r = rows_of(a, s);
             const int32_t M = r.y > r.x ? (r.y - r.x) * a.group : 0;
             tiles = a.all || M > kFew ? (M + kChunkQ - 1) / kChunkQ : 0;
-            if (tiles > 0) length = limit_of(a, r.y - 1);
         }
         if (a.c.n_seq > 1 && a.c.n_seq <= 64) {
+            if (tiles > 0) length = limit_of(a, r.y - 1);
             int32_t rank = 0;
             for (int32_t j = 0; j < a.c.n_seq; ++j) {
                 const int32_t other = __builtin_amdgcn_readlane(length, j);
@@ -429,43 +431,47 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
             const int who = __builtin_ctzll(behind);
             seq = __builtin_amdgcn_readlane(s, who);
             tile = __builtin_amdgcn_readlane(sum, who) - 1 - left;
+            const int from = a.c.n_seq - 1 - at - seq;         // the lane that looked at it
+            rows = make_int2(__builtin_amdgcn_readlane(r.x, from), __builtin_amdgcn_readlane(r.y, from));
             break;
         }
         left -= total;
     }
     if (seq < 0) return;
-    const int2 rows = rows_of(a, seq);
     const int32_t M = (rows.y - rows.x) * a.group;
 
-    // ---- this lane's query: the slots it sees, Q^T fragments
+    // ---- this lane's query: the slots it sees, Q^T fragments; page ids are on their way with them
     const int32_t m = tile * kChunkQ + wave * 32 + l32, mc = m < M ? m : M - 1;
     const int32_t row = rows.x + mc / a.group, head = kvh * a.group + mc % a.group;
     const int32_t limit = limit_of(a, row);
-    int32_t top, low = limit;
-    {
-        __shared__ int32_t tops[4];
-        int32_t hi = limit;
-#pragma unroll
-        for (int x = 1; x < 32; x <<= 1) {                     // lanes 32.. hold the same queries
-            low = min(low, __shfl_xor(low, x, 64));
-            hi = max(hi, __shfl_xor(hi, x, 64));
-        }
-        if (kg == 0 && lane == 0) tops[wave] = hi;
-        __syncthreads();
-        top = uniform(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
-        low = uniform(low);
-    }
-    const int32_t piece_tiles = a.piece / kChunkK;
-    const int32_t t0 = piece * piece_tiles, t_all = (top + kChunkK) / kChunkK;             // top = -1: none
-    if (t0 >= t_all && piece > 0) return;
-    const int32_t t_end = piece == a.n_split - 1 || t_all < t0 + piece_tiles ? t_all : t0 + piece_tiles;
-
     v8h qf[kD / 16];
     {
         const __half *qp = a.q + row * a.ldq + static_cast<int64_t>(head) * kD + g * 8;
 #pragma unroll
         for (int ks = 0; ks < kD / 16; ++ks) qf[ks] = *reinterpret_cast<const v8h *>(qp + ks * 16);
     }
+    // Key group kg takes the tiles t0 + kg, t0 + kg + KG, ...: tile i of its own.  The groups do the same number of steps: the last tile
+    // of one may lie behind the piece, and nothing of it is visible then.
+    const int32_t piece_tiles = a.piece / kChunkK, t0 = piece * piece_tiles;
+    auto tile_of = [&](int32_t i) { return t0 + kg + KG * i; };
+    // lane l: block l % 4 of tile 16 j + l / 4, for the keys' tile and for the values', and the next 16 tiles on their way
+    auto blocks_from = [&](int32_t i) { return block_at(a, seq, kvh, tile_of(i + (lane >> 2)) * 4 + (lane & 3)); };
+    uint32_t k_blocks = blocks_from(0), v_blocks = k_blocks, n_blocks = blocks_from(16);
+
+    int32_t top, low = row16_min(limit);
+    {
+        __shared__ int32_t tops[4];
+        int32_t hi = row16_max(limit);
+        low = uniform(min(low, __shfl_xor(low, 16, 64)));      // lanes 32.. hold the same queries
+        hi = max(hi, __shfl_xor(hi, 16, 64));
+        if (kg == 0 && lane == 0) tops[wave] = hi;
+        __syncthreads();
+        top = uniform(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+    }
+    const int32_t t_all = (top + kChunkK) / kChunkK;           // top = -1: none
+    if (t0 >= t_all && piece > 0) return;
+    const int32_t t_end = piece == a.n_split - 1 || t_all < t0 + piece_tiles ? t_all : t0 + piece_tiles;
+    const int32_t steps = t_end > t0 ? (t_end - t0 + KG - 1) / KG : 0;
 
     // ---- tile copies: block i of 16 slots is 4 KiB of one page; a wave copies four rows of each block.  Key chunk c of row r lies at
     // chunk c ^ (r & 15) (a fragment read takes one chunk of 16 rows), value chunk c at c ^ 4 (r & 3) (a transposing read: 64 bytes of 4 rows).
@@ -473,16 +479,6 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     const int c_row = wave * 4 + (lane >> 4);
     const uint32_t k_off = c_row * 256 + (((lane & 15) ^ (c_row & 15)) << 4);
     const uint32_t v_off = c_row * 256 + (((lane & 15) ^ ((c_row & 3) << 2)) << 4);
-    // Key group kg takes the tiles t0 + kg, t0 + kg + KG, ...: tile i of its own.  The groups do the same number of steps; one whose tiles
-    // are used up repeats the piece's last one with nothing of it visible.
-    const int32_t steps = t_end > t0 ? (t_end - t0 + KG - 1) / KG : 0;
-    auto tile_of = [&](int32_t i) {
-        const int32_t t = t0 + kg + KG * i;
-        return KG == 1 || t < t_end ? t : t_end > 0 ? t_end - 1 : 0;            // t_end = 0: no slot is visible, and no tile is taken
-    };
-    // lane l: block l % 4 of tile 16 j + l / 4, for the keys' tile and for the values', and the next 16 tiles on their way
-    auto blocks_from = [&](int32_t i) { return block_at(a, seq, kvh, tile_of(i + (lane >> 2)) * 4 + (lane & 3)); };
-    uint32_t k_blocks = blocks_from(0), v_blocks = k_blocks, n_blocks = blocks_from(16);
     auto dma_k = [&](int32_t i, int b) {
         const int32_t at = i * 4;
         if ((at & 63) == 0 && at > 0) {
@@ -504,10 +500,9 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     };
     // Value rows behind the last slot become zeros once they have landed (every lane those it copied): they may hold anything,
     // and a zero probability times NaN is NaN.
-    const int32_t ragged = (top + 1) % kChunkK != 0 ? t_all - 1 : -1;
     auto zero_tail = [&](int32_t i, int b) {
         const int32_t t = tile_of(i);
-        if (t != ragged) return;
+        if (t * kChunkK + kChunkK - 1 <= top) return;
         uint32_t at = lds0 + (2 + b) * kTileBytes + wave * 1024 + lane * 16;
         int32_t slot = t * kChunkK + c_row;
         asm volatile("" : "+v"(at), "+v"(slot) : : "memory");
