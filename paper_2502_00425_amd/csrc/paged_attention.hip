@@ -890,11 +890,24 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
         const int64_t longer = p.few ? (T / (kFew / G + 1) < n_seq ? T / (kFew / G + 1) : n_seq) : n_seq;    // sequences it may take
         p.chunk_tiles = static_cast<int32_t>(static_cast<int64_t>(T) * G / kChunkQ + longer);
         const int64_t groups = p.chunk_tiles * static_cast<int64_t>(n_kv);
-        int64_t split = 2 * kNumCU / groups;
-        if (split > kv / 512) split = kv / 512;
-        if (split > 1) {
-            p.chunk_piece = static_cast<int32_t>(ceil_div(ceil_div(kv, split), kChunkK) * kChunkK);
-            p.chunk_split = static_cast<int32_t>(ceil_div(kv, p.chunk_piece));
+        // Pieces: the fewest estimated us.  A step of the walk, which waits for memory where compute units are idle, takes 1.7 with two key
+        // groups, 1.0 where two work-groups share a compute unit; the join is a launch, and partial results are written and read.
+        // us by pieces: 28 heads on 4, 64 rows on 2000 slots 1 35.6, 2 26.3, 4 20.4, 8 18.9, 16 21.4; 256 on 1000 1 22.6, 2 24.8, 6 26.4; 256 on
+        // 8000 1 118, 4 49.3, 8 46.6; 512 on 512 1 16.0, 2 27.7; 600 on 2000 1 36.8, 3 41.6; 5 on 1, 300 on 9000 1 131, 8 29.5, 16 26.6.
+        const int64_t tiles = ceil_div(kv, kChunkK), queries = static_cast<int64_t>(T) * n_q;
+        int64_t best = tiles;                                  // tiles of a piece
+        double best_us = INFINITY;
+        for (int64_t split = 1; split <= (tiles + 1) / 2 && groups * split <= 2 * kNumCU; ++split) {
+            const int64_t piece = ceil_div(tiles, split);
+            const double walk = groups * split <= kNumCU ? 1.7 * static_cast<double>((piece + 1) / 2) : static_cast<double>(piece);
+            const double us = walk + (split > 1 ? 6.0 + 0.25e-3 * static_cast<double>(queries * split) : 0.0);
+            if (us >= best_us) continue;
+            best_us = us;
+            best = piece;
+        }
+        if (best < tiles) {
+            p.chunk_piece = static_cast<int32_t>(best * kChunkK);
+            p.chunk_split = static_cast<int32_t>(ceil_div(tiles, best));
         }
         p.chunk_two = groups * p.chunk_split <= kNumCU;
         if (p.chunk_split > 1) p.chunk_part = static_cast<int64_t>(T) * n_q * p.chunk_split;
