@@ -119,6 +119,8 @@ __device__ __forceinline__ int32_t pieces_of(const Step &a, int32_t limit)
 // product, so about 14 of the 16 KiB are in flight all the time, for 8 waves a compute unit.
 // Key chunk c (16 bytes) of row r lies at chunk c ^ (r & 15): a fragment read takes one chunk of 16 rows.  Value chunk c lies
 // at c ^ 2 (r & 7): a transposing read takes 32 bytes of 8 rows.
+// Bound by the bytes of the cache where they are many: 32 sequences of 500 to 16384 slots, 64 heads on 8 (633 MB), 126 us with the
+// join, 5.0 TB/s (a device copy 4.9).  One row over 1281 slots is five trips to memory, one behind another, and two launches: 8.0 us.
 // NQ: 16 queries each, all of them computed, whatever a sequence has: skipping by branches those behind the last query cost the
 // others the overlap of their products and exponentials (20.4 against 17.7 us at 8 sequences of 5 rows x 28 heads over 4096 slots), and
 // a form for each number beside one another gave nothing (32 sequences of one row among one of 512, 8000 slots each: 194 and 193 us).
@@ -295,7 +297,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 
         // ---- the four waves meet in LDS, 16 queries at a time: thread t finishes 8 channels of query t / 16
         int t = tid;
-        asm volatile("" : "+v"(t));
+        asm volatile("" : "+v"(t));                            // what is worked out from it is not held through the walk
         const int my_q = t & 15, my_ch = (t >> 4 & 3) * 4;
         float *sums = reinterpret_cast<float *>(smem);                          // [4][16][kFewPitch]
         float2 *ml = reinterpret_cast<float2 *>(smem + kFewWaves * 16 * kFewPitch * 4);        // [4][16]
@@ -360,6 +362,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 // buffers each, keys one step ahead of values, one barrier a tile.
 // Consecutive queries are the group's heads of one row, then of the next: a work-group spans 128 / G rows whose limits lie
 // close together, so it walks its tiles without skipping any for single waves, and only the last tiles are compared slot by slot.
+// Bound by the power of the matrix cores: 4096 rows x 64 heads on 16384 slots 1750 to 1930 us by card, 1.0 to 1.1 PFLOP/s, as a large
+// library product; an MFMA is in the matrix pipes 63 % of the cycles, the vector pipes are busy 54 %, the clock is 1.55 GHz.  Few
+// work-groups wait for a step's copies instead (KG = 2: two key groups of four waves, which meet in LDS, for those).
 __device__ __forceinline__ void halves_of(float x, float &lo, float &hi)
 {
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
@@ -744,8 +749,9 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
 // ------------------------------------------------------------------------------------------------ pieces
 //
 // A wave joins the pieces of one query: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p; 16 lanes hold its channels, the quarters of the wave
-// take every fourth piece, and 16 pieces are on their way at once.  Queries whose slots were
-// one piece are finished already, those that the other kernel took are its own.
+// take every fourth piece, and 16 pieces are on their way at once, with the running maximum and sum over the sixteens.  Queries whose slots
+// were one piece are finished already, those that the other kernel took are its own.  Bound by latency: 3.5 to 5.5 us, of which a launch
+// takes 2 and the way row_start, position and partial results, result the rest.
 template <bool CHUNK>
 __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
 {

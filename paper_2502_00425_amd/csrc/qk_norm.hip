@@ -34,7 +34,8 @@ struct Rows {
 
 // A wave takes one row and `per` (at most U) groups of four heads (queries first, then keys, then values): 16 lanes a head, 16
 // bytes a lane.  Lane l forms the angle of pair l, every lane then takes the four pairs it holds, the same ones in all its
-// heads.  `waves` waves share a row and lie next to each other, so that rows are read and written from end to end.
+// heads.  `waves` waves share a row and lie next to each other, so that rows are read and written from end to end.  Bound by the bytes: 72
+// heads of 16384 rows 104 us, 604 MB, 5.8 TB/s.  Few rows are bound by the launch and two trips to memory: 77 rows of 32 heads 3.2 us.
 // Rows that fill the chip go past the caches (72 heads of 16384 rows 121.7 -> 107.5 us, 36 of 4096 with the append 17.8 ->
 // 14.9): lines that are written whole need not be looked up there.  Few rows stay, the next kernel reads them.
 template <bool PAST>
