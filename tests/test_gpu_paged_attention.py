@@ -279,6 +279,21 @@ def test_two_graphs_that_share_a_workspace(mq):
             assert torch.equal(mq.paged_attention(*a), o)
 
 
+@pytest.mark.parametrize("n,spans", [(77, [(5, 30)]), (300, [(0, 64), (100, 130)]), (1, []), (640, [])])
+def test_a_prompt_as_the_attention_without_a_cache_sees_it(mq, n, spans):
+    """One whole prompt in AIFS order: the unified mask over its rows and the slots by position are the same sum.  Each side is off by its
+    own bound: this one's, and 1.5 * 2^-11 (sum p |v| + |o|) + 1e-6 of the other."""
+    st = make_step(np.random.default_rng(n), [(n, n)], 14, 2, 16, spans=spans, poison=False)
+    q, cache, start, pos, hq = device_step(mq, st)
+    at = st["table"][0, st["pos"] // 16], st["pos"] % 16
+    k, v = (dev(st[p][at[0], :, at[1]].reshape(n, -1)) for p in ("kp", "vp"))       # rows in AIFS order
+    ref = orc.paged_attention_f64(st["q"], st["kp"], st["vp"], st["table"], st["start"], st["pos"], hq)
+    mass = orc.paged_attention_f64(st["q"], st["kp"], np.abs(st["vp"]), st["table"], st["start"], st["pos"], hq)
+    tol = attention_bound(st, ref) + 1.5 * 2.0 ** -11 * (mass + np.abs(ref)) + 1e-6
+    a, b = (o.cpu().numpy().astype(np.float64) for o in (mq.paged_attention(q, cache, start, pos, hq, n, n), mq.aifs_attention(q, k, v, pos, hq, 2)))
+    assert (np.abs(a - b) <= tol).all()
+
+
 @pytest.mark.parametrize("fill", [float("nan"), float("inf"), float("-inf"), 3e38])
 def test_scratch_holds_anything(mq, fill):
     """What a workspace held before the call leaves no trace: sequences with fewer pieces than the longest one among them."""
