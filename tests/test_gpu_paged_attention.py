@@ -279,6 +279,24 @@ def test_two_graphs_that_share_a_workspace(mq):
             assert torch.equal(mq.paged_attention(*a), o)
 
 
+def test_large_logits(mq):
+    """Logits up to 2.96e6 (sums that are exact in fp32, 2896 apart where they differ): the mean over the slots of the largest one.  Their
+    probabilities are equal, so the sum over them is off by the fp32 accumulation (1024 slots of 2^-24 of the largest value) and by the
+    rounding of the output."""
+    rng = np.random.default_rng(17)
+    for seqs, hq, hkv in ([(1, 700), (1, 64)], 28, 4), ([(4, 500)], 7, 1), ([(130, 900)], 4, 2):
+        st = make_step(rng, seqs, hq, hkv, 16)
+        sign = rng.choice([-1.0, 1.0], D)
+        st["q"][:] = np.tile(256 * sign, hq)
+        steps = rng.integers(-1024, 1025, st["kp"].shape[:3]).astype(np.float64)
+        steps[rng.random(steps.shape) < 0.05] = 1024
+        st["kp"][:] = np.where(np.isnan(st["kp"]) | np.isinf(st["kp"]), st["kp"], (steps[..., None] * sign).astype(np.float16))
+        ref = orc.paged_attention_f64(st["q"], st["kp"], st["vp"], st["table"], st["start"], st["pos"], hq)
+        got = mq.paged_attention(*device_step(mq, st), *bounds_of(st)).cpu().numpy().astype(np.float64)
+        top = np.abs(np.nan_to_num(st["vp"].astype(np.float64), nan=0, posinf=0)).max()
+        assert (np.abs(got - ref) <= 2.0 ** -11 * np.abs(ref) + 2.0 ** -25 + 2.0 ** -14 * top).all()
+
+
 @pytest.mark.parametrize("n,spans", [(77, [(5, 30)]), (300, [(0, 64), (100, 130)]), (1, []), (640, [])])
 def test_a_prompt_as_the_attention_without_a_cache_sees_it(mq, n, spans):
     """One whole prompt in AIFS order: the unified mask over its rows and the slots by position are the same sum.  Each side is off by its
