@@ -342,7 +342,8 @@ __device__ __forceinline__ void wait_copies()
 
 // h of 64 rows and a slice of K.  Chunk c (16 bytes) of row r lies at chunk c ^ (r & 15): a fragment read takes one chunk of 16 rows.
 // 4096 rows of 3584 channels, rank 64: 11.6 us (29 MB of x, 2.5 TB/s): 256 work-groups that hold rows, one to a compute unit, which
-// wait for a stage of 32 KiB at a time (a wave waits 63 % of its life).
+// wait for a stage of 32 KiB at a time (a wave waits 63 % of its life).  Ranks beyond 64 are a second part, in work-groups of its own: 128 of them
+// in one, with stages of 48 KiB and one work-group to a compute unit, took 26.0 us where two parts take 18.4.
 template <int RB>
 __global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
 {
@@ -354,6 +355,7 @@ __global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
     if (id < 0 || id == p.n_adapters) return;
     __syncthreads();
 
+    const int32_t parts = p.rank > RB * 16 ? 2 : 1, r0 = static_cast<int32_t>(blockIdx.x) % parts * RB * 16;    // first rank
     constexpr int kBuffer = (kRows + RB * 16) * 256;
     const uint32_t lds0 = lds_address(smem);
     const __half *xr[4], *ar[RB];                              // where this lane copies from: rows 4 i + g of the wave's 16, of each 16 of A_a
@@ -370,7 +372,7 @@ __global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
     ac = (l16 ^ (wave * 4 + g)) * 8;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        const int r = b * 16 + wave * 4 + g;
+        const int r = r0 + b * 16 + wave * 4 + g;
         ar[b] = p.a + (static_cast<int64_t>(id) * p.rank + (r < p.rank ? r : p.rank - 1)) * p.K;
     }
     auto copy = [&](int32_t stage, int buffer) {               // channels behind K repeat its last 8
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
         for (int b = 0; b < RB; ++b)
             lds_dma16_lane_address(ar[b] + (k + ac < p.K ? k + ac : last), at + kRows * 256 + (b * 4 + wave) * 1024);
     };
-    const int32_t stages = (p.K + kStage - 1) / kStage, slice = blockIdx.x;
+    const int32_t stages = (p.K + kStage - 1) / kStage, slice = blockIdx.x / parts;
     const int32_t s0 = static_cast<int32_t>(static_cast<int64_t>(stages) * slice / p.slices);
     const int32_t s1 = static_cast<int32_t>(static_cast<int64_t>(stages) * (slice + 1) / p.slices);
     v4f acc[RB];
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
         if (j < n)
 #pragma unroll
             for (int b = 0; b < RB; ++b)
-                if (b * 16 + l16 < p.rank) h[static_cast<int64_t>(list[j]) * p.rank + b * 16 + l16] = acc[b][r];
+                if (r0 + b * 16 + l16 < p.rank) h[static_cast<int64_t>(list[j]) * p.rank + r0 + b * 16 + l16] = acc[b][r];
     }
 }
 
@@ -596,11 +598,14 @@ int64_t few_slices(int32_t K)
 
 // Many: tiles of 64; a slice's stage takes 0.55 us and every slice costs the expansion 0.28, so about sqrt(2 stages) slices (rank 64, K = 3584,
 // 28 stages, shrink + expansion in us with 2 / 4 / 8 / 14 slices: 512 rows 25.2 / 20.6 / 19.8 / 21.7, 1024 26.2 / 22.3 / 22.2 / 24.9), but no
-// more than give every compute unit a work-group (4096 rows: 4 slices 33.2, 8 41.9).
-int64_t many_slices(int32_t T, int32_t K)
+// more than give every compute unit a work-group (4096 rows: 4 slices 33.2, 8 41.9).  Two parts of the rank cost twice in the expansion (rank
+// 128 with 2 / 3 / 4 slices: 2889 rows 40.0 / 40.2 / 39.3, 4096 48.6 / 48.6 / 54.1, 1000 29.4 / 27.2 / 25.5 and 28.2 with 8).
+constexpr int32_t kManyRank = 64;          // ranks of a part
+int64_t rank_parts(int32_t rank) { return rank > kManyRank ? 2 : 1; }
+int64_t many_slices(int32_t T, int32_t K, int32_t rank)
 {
-    int64_t s = static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)))));
-    const int64_t most = kNumCU / ceil_div(T, kRows);
+    int64_t s = static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)) / static_cast<double>(rank_parts(rank)))));
+    const int64_t most = kNumCU / (ceil_div(T, kRows) * rank_parts(rank));
     if (s > most) s = most;
     return s < 1 ? 1 : s;
 }
@@ -617,12 +622,15 @@ bool few_rows(int32_t T, int32_t n_adapters) { return T <= 128 || (T <= kFewMax 
 bool few_rows_to_expand(int32_t T, int32_t N, int32_t n_adapters) { return T <= 64 || (N < 16384 && few_rows(T, n_adapters)); }
 
 template <int RB>
-int launch_shrink(const Lora &a, bool few, dim3 grid, hipStream_t stream)
+int launch_shrink(const Lora &a, dim3 grid, hipStream_t stream)
 {
-    if (few) {
-        MQ_LAUNCH(lora_shrink_kernel<RB>, grid, dim3(kShrinkWaves * 64), 0, stream, a);
-        return launch_status();
-    }
+    MQ_LAUNCH(lora_shrink_kernel<RB>, grid, dim3(kShrinkWaves * 64), 0, stream, a);
+    return launch_status();
+}
+
+template <int RB>
+int launch_shrink_rows(const Lora &a, dim3 grid, hipStream_t stream)
+{
     constexpr int lds = 2 * (kRows + RB * 16) * 256;
     auto kern = lora_shrink_rows_kernel<RB>;
     if constexpr (lds >= 60 * 1024) {                          // next to the list of rows
@@ -655,7 +663,7 @@ extern "C" int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t ran
     if (T < 0 || K < 0 || rank < 1) return MQUANT_ERR_BAD_SHAPE;
     if (K == 0 || K % 8 != 0 || rank % 8 != 0 || rank > 128) return MQUANT_ERR_UNSUPPORTED;
     if (T == 0) return 0;
-    int64_t slices = many_slices(T, K);
+    int64_t slices = many_slices(T, K, rank);
     if (T <= kFewMax && few_slices(K) > slices) slices = few_slices(K);        // whichever the number of adapters asks for
     return ceil_div(slices * T * rank * 4, 256) * 256;
 }
@@ -682,14 +690,14 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
     const bool few = few_rows(T, n_adapters), few_to_expand = few_rows_to_expand(T, N, n_adapters);
     Lora args = {static_cast<const __half *>(x), ldx, perm, adapter, static_cast<const __half *>(a), static_cast<const __half *>(b), scale,
                  static_cast<const __half *>(base), ldb, static_cast<__half *>(y), ldy, static_cast<float *>(workspace), T, N, K, rank,
-                 n_adapters, static_cast<int32_t>(few ? few_slices(K) : many_slices(T, K)),
-                 few_to_expand ? kExpandWaves * kCols : 512};
+                 n_adapters, static_cast<int32_t>(few ? few_slices(K) : many_slices(T, K, rank)),
+                 few_to_expand ? kExpandWaves * kCols : rank > 64 ? 1024 : 512};
     // Few rows: a block of columns a wave, two of many columns (34 rows of 12 adapters, rank 32, N = 37888, one / two / four: 11.4 / 8.5 / 9.0 us, 64 of 3,
     // rank 64, 15.7 / 12.4 / 12.7, 4 of 4, rank 16, 4.6 / 4.9 / 5.8; N = 10240, 48 of 12, rank 16, 5.8 / 5.9 / 6.8).
     if (few_to_expand && N >= 16384 && T > 8) args.cols *= 2;
     // Many rows: 512 columns a work-group, which prepares its rows once for all of them, fewer where that leaves compute units idle (K = 3584,
     // N = 4608, rank 64, expansion with 128 / 256 / 512 / 1024 columns: 128 rows 9.1 / 10.4 / 13.4 / 18.9 us, 1024 15.7 / 14.8 / 16.3 / 21.2, 4096
-    // 28.2 / 24.4 / 21.7 / 23.1).
+    // 28.2 / 24.4 / 21.7 / 23.1; rank 128, 4096 rows, 512 / 1024: 35.9 / 30.7).
     while (!few_to_expand && args.cols > 128 && ceil_div(T, kRows) * ceil_div(N, args.cols) < kNumCU) args.cols /= 2;
     const int64_t blocks = ceil_div(T, kBlock), chunks = ceil_div(N, args.cols);
     if (blocks > 65535) return MQUANT_ERR_UNSUPPORTED;
@@ -700,9 +708,11 @@ extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm
         return static_cast<unsigned>(in_block / rows + (n_adapters < in_block ? n_adapters + 1 : in_block));
     };
     if (n_adapters > 0) {
-        const dim3 grid(static_cast<unsigned>(args.slices), static_cast<unsigned>(blocks), tiles(few ? 16 : kRows));
-        const int st = rank <= 16 ? launch_shrink<1>(args, few, grid, stream) : rank <= 32 ? launch_shrink<2>(args, few, grid, stream)
-                     : rank <= 64 ? launch_shrink<4>(args, few, grid, stream) : launch_shrink<8>(args, few, grid, stream);
+        const dim3 grid(static_cast<unsigned>(args.slices * (few ? 1 : rank_parts(rank))), static_cast<unsigned>(blocks), tiles(few ? 16 : kRows));
+        const int st = few ? (rank <= 16 ? launch_shrink<1>(args, grid, stream) : rank <= 32 ? launch_shrink<2>(args, grid, stream)
+                              : rank <= 64 ? launch_shrink<4>(args, grid, stream) : launch_shrink<8>(args, grid, stream))
+                     : rank <= 16 ? launch_shrink_rows<1>(args, grid, stream) : rank <= 32 ? launch_shrink_rows<2>(args, grid, stream)
+                                  : launch_shrink_rows<kManyRank / 16>(args, grid, stream);
         if (st != MQUANT_OK) return st;
     }
     const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(blocks), tiles(few_to_expand ? 16 : kRows));

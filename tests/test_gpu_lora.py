@@ -115,6 +115,14 @@ def test_wide_ranges(mq):
     check(c, call(mq, c), what="no adapters")
 
 
+@pytest.mark.parametrize("T,K,N,rank,n", [(1100, 1032, 130, 72, 2), (1025, 640, 96, 128, 1), (700, 2056, 200, 104, 3), (300, 256, 1160, 128, 2),
+                                          (129, 3584, 512, 80, 1)])
+def test_many_rows_of_two_parts_of_ranks(mq, T, K, N, rank, n):
+    """Ranks beyond 64, which many rows take in two parts; the last part nearly empty or full."""
+    c = make(np.random.default_rng(T + rank), T, K, N, rank, n)
+    check(c, call(mq, c), what=f"{T} {K} {N} r{rank}")
+
+
 def test_stale_workspace_and_replays(mq):
     """A captured call replayed with other ids and inputs, its workspace full of NaN patterns before each replay."""
     rng = np.random.default_rng(5)
