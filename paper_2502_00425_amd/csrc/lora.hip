@@ -341,8 +341,9 @@ __device__ __forceinline__ void wait_copies()
 }
 
 // h of 64 rows and a slice of K.  Chunk c (16 bytes) of row r lies at chunk c ^ (r & 15): a fragment read takes one chunk of 16 rows.
-// 4096 rows of 3584 channels, rank 64: 11.6 us (29 MB of x, 2.5 TB/s): 256 work-groups that hold rows, one to a compute unit, which
-// wait for a stage of 32 KiB at a time (a wave waits 63 % of its life).  Ranks beyond 64 are a second part, in work-groups of its own: 128 of them
+// 4096 rows of 3584 channels, rank 64: 12 us (29 MB of x, 2.5 TB/s): about one work-group to a compute unit, which waits for a stage of
+// 32 KiB at a time (a wave waits 63 % of its life).  Three buffers are no faster where two work-groups still fit a compute unit
+// (rank 16 8.1 / 8.6), and cost a second round of work-groups where they do not (rank 64 12.0 / 19.5).  Ranks beyond 64 are a second part, in work-groups of its own: 128 of them
 // in one, with stages of 48 KiB and one work-group to a compute unit, took 26.0 us where two parts take 18.4.
 template <int RB>
 __global__ __launch_bounds__(256) void lora_shrink_rows_kernel(Lora p)
