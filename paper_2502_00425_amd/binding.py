@@ -592,8 +592,8 @@ def _operand(t, dtype, what: str, shape=None):
     if t.dtype is not dtype:
         raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected {dtype}, got {t.dtype}")
     if shape is None:
-        ld = _rows(t, what)
-        return ld if t.shape[0] > 1 else t.shape[1] + -t.shape[1] % 8       # the stride of a single row says nothing
+        ld = 0 if t.dim() == 2 and t.shape[0] == 0 else _rows(t, what)
+        return ld if t.shape[0] > 1 else t.shape[1] + -t.shape[1] % 8       # the stride of a single row, or of none, says nothing
     if tuple(t.shape) != shape:
         raise MQuantError(ERR_BAD_SHAPE, f"{what}: expected shape {shape}, got {tuple(t.shape)}")
     _dense(t, what)

@@ -279,6 +279,52 @@ def test_two_graphs_that_share_a_workspace(mq):
             assert torch.equal(mq.paged_attention(*a), o)
 
 
+@pytest.mark.parametrize("seqs,hq,hkv,page", [
+    ([(13 + i % 5, 13 + 11 * i % 300) if i % 7 else (0, 9) for i in range(70)], 4, 1, 16), ([(1, 5000), (1, 4096), (3, 4097)], 4, 2, 4096),
+    ([(40, 2500), (1, 2048)], 7, 1, 2048), ([(1, 30)] * 130 + [(20, 90)] + [(2, 8)] * 5, 6, 2, 16)])
+def test_many_chunks_and_large_pages(mq, seqs, hq, hkv, page):
+    """More sequences than a wave sorts, some without rows, and the largest pages."""
+    seqs = [(n, max(n, length)) for n, length in seqs]
+    st = make_step(np.random.default_rng(len(seqs)), seqs, hq, hkv, page, behind=1)
+    for bounds in (bounds_of(st), (0, 0), (1, 1)):
+        check(st, mq.paged_attention(*device_step(mq, st), *bounds), what=f"{len(seqs)} {bounds}")
+
+
+def test_sequences_that_share_pages(mq):
+    """Two sequences with the same first pages: a prompt that both continue."""
+    st = make_step(np.random.default_rng(18), [(1, 700), (5, 600), (60, 640)], 14, 2, 16)
+    st["table"][1, :20], st["table"][2, :30] = st["table"][0, :20], st["table"][0, :30]
+    check(st, mq.paged_attention(*device_step(mq, st), *bounds_of(st)))
+
+
+def test_queries_of_rows_that_see_nothing_may_be_anything(mq):
+    for seqs in ([(6, 300)], [(1, 40), (90, 700)]):
+        st = make_step(np.random.default_rng(19), seqs, 7, 1, 16, behind=2)
+        blind = np.arange(0, st["T"] - 2, 5)
+        st["pos"][blind] = -1
+        clean = {**st, "q": st["q"].copy()}
+        st["q"][blind], st["q"][-2:] = np.nan, np.inf
+        out = mq.paged_attention(*device_step(mq, st), *bounds_of(st))
+        check(clean, out, what=f"{seqs}")
+        assert (out[torch.from_numpy(blind).cuda()] == 0).all()
+
+
+def test_nothing_to_do(mq):
+    """No rows, and no sequences."""
+    st = make_step(np.random.default_rng(20), [(0, 40), (0, 3)], 4, 2, 16)
+    q, cache, start, pos, hq = device_step(mq, st)
+    assert mq.paged_attention(q, cache, start, pos, hq).shape == (0, 4 * D)
+    none = mq.PagedCache(cache.k_pages, cache.v_pages, cache.page_table[:0])
+    x = torch.ones((3, 4 * D), dtype=torch.float16, device="cuda")
+    at = torch.zeros(3, dtype=torch.int32, device="cuda")
+    out = torch.full_like(x, 5)
+    assert (mq.paged_attention(x, none, start[:1], at, 4, out=out) == 5).all()
+    assert (mq.kv_append(x, x[:, :2 * D], x[:, :2 * D], none, start[:1], at, 4, q_out=out) == 5).all()
+    before = cache.k_pages.clone()
+    assert mq.kv_append(q, q[:, :2 * D], q[:, :2 * D], cache, start, pos, 4).shape == (0, 4 * D)
+    assert torch.equal(cache.k_pages.view(torch.int16), before.view(torch.int16))
+
+
 def test_large_logits(mq):
     """Logits up to 2.96e6 (sums that are exact in fp32, 2896 apart where they differ): the mean over the slots of the largest one.  Their
     probabilities are equal, so the sum over them is off by the fp32 accumulation (1024 slots of 2^-24 of the largest value) and by the
