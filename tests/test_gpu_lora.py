@@ -98,6 +98,36 @@ def test_in_place_strides_and_streams(mq):
         assert bool((y[:, :5] == 2).all()) and bool((y[:, 5 + N:] == 2).all())
 
 
+@pytest.mark.parametrize("T", [21, 400])
+def test_rows_that_are_not_finite_stay_by_themselves(mq, T):
+    """NaN in x of rows without an adapter is not read; infinities in x and NaN in base show in their own rows only."""
+    rng = np.random.default_rng(T)
+    c = make(rng, T, 264, 200, 24, 3, ids=rng.integers(-1, 4, T))
+    want = call(mq, c)
+    off = np.flatnonzero((c["ids"] < 0) | (c["ids"] >= 3))
+    on = np.flatnonzero((c["ids"] >= 0) & (c["ids"] < 3))
+    c["x"][off] = np.nan
+    c["x"][on[2], 7], c["base"][on[4]] = np.inf, np.nan
+    got = call(mq, c)
+    odd = torch.tensor([int(on[2]), int(on[4])]).cuda()
+    assert not torch.isfinite(got[odd]).any(dim=1).all() and torch.isnan(got[odd[1]]).all()
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[odd] = False
+    assert torch.equal(got[rest], want[rest])
+
+
+def test_nothing_to_do(mq):
+    h = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")
+    ids, scale = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.ones(2, device="cuda")
+    assert mq.lora_apply(h(0, 64), ids, h(2, 8, 64), h(2, 40, 8), scale, h(0, 40)).shape == (0, 40)
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert mq.lora_apply(h(3, 64), ids, h(2, 8, 64), h(2, 0, 8), scale, h(3, 0)).shape == (3, 0)
+    base = h(3, 40) + 2
+    assert torch.equal(mq.lora_apply(h(3, 64) + 1, ids, h(0, 8, 64), h(0, 40, 8), scale[:0], base), base)
+    pos = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert [tuple(t.shape) for t in mq.qk_norm_rope(h(0, 512), h(0, 128), None, None, pos, 4, 1)] == [(0, 512), (0, 128)]
+
+
 def test_wide_ranges(mq):
     """Visual activations with outlier channels, an intermediate beyond fp16's range, tiny ones, no adapters at all."""
     rng = np.random.default_rng(4)
