@@ -569,7 +569,7 @@ int64_t mquant_paged_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t
  *   workspace_dev  : mquant_paged_attention_workspace_bytes(...) bytes, 256-byte aligned; scratch, concurrent
  *                    calls must not share it.  NULL where that is 0.
  * Slots up to the largest position of a sequence's rows must hold finite values, and logits (q k / sqrt(head_dim)) lie
- * below 2^22 in magnitude (fp32 holds the exponent's argument beyond that to whole units only); slots behind it are not
+ * below 2^22 in magnitude (fp32 holds q k beyond that in steps of 4 and more); slots behind it are not
  * looked at.  A page id outside [0, n_pages) reads page 0.  o must not overlap q or the pages.
  * Errors: ERR_NULL, ERR_BAD_SHAPE (n_q_heads not a multiple of n_kv_heads, ...), ERR_UNSUPPORTED (head_dim,
  *         page_size, sizes beyond the grid), ERR_WORKSPACE, ERR_ALIGNMENT.

@@ -43,7 +43,9 @@ constexpr int kChunkLds = 4 * kTileBytes;  // two key and two value tiles
 constexpr int kAhead = 4;                  // LDS fragment reads in flight ahead of the MFMA that uses them
 
 // The running maximum that the sums are scaled to follows the true one lazily: only when some query's has grown by more
-// than kLazy (a factor 2^8 in the probabilities, harmless in fp16 and fp32) are the sums rescaled.
+// than kLazy (a factor 2^8 in the probabilities, harmless in fp16 and fp32) are the sums rescaled.  The exponents see it
+// times scale_log2e and rounded, in eighths at a score of 8e6: so sums meet under a factor of the rounded products' difference (exact where the
+// factor matters), under one of the maxima's own they would be up to 2^(1/8) apart.  No product is contracted into an addition here (-ffp-contract=off).
 constexpr float kLazy = 8.0f;
 
 struct Step {
@@ -54,7 +56,7 @@ struct Step {
     int32_t T, n_q, group;                 // group: query heads per key/value head
     float scale_log2e;
     PagedCache c;
-    // pieces of slots: how many at most, slots of one, and the partial results of (piece, query): sums [128], then (maximum, denominator)
+    // pieces of slots: how many at most, slots of one, and the partial results of (piece, query): sums [128], then (what they are scaled to, denominator)
     int32_t n_split, piece;
     int32_t few_stride;                    // queries of a (sequence, key/value head) that have room among the partial results
     int32_t all;                           // this kernel takes every sequence, whatever its rows
@@ -244,7 +246,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
                     if (__any(m > m_ref[u] + lazy_raw)) {      // also the first visible slot (m_ref = -inf)
                         m = fmaxf(m, __shfl_xor(m, 16, 64));
                         m = fmaxf(m, __shfl_xor(m, 32, 64));
-                        const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_ref[u] - m) * a.scale_log2e);
+                        const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref[u] * a.scale_log2e - m * a.scale_log2e);
                         l_run[u] *= alpha;
 #pragma unroll
                         for (int cb = 0; cb < 8; ++cb) acc[u][cb] *= alpha;
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 #pragma unroll
             for (int cb = 0; cb < 8; ++cb)
                 *reinterpret_cast<v4f *>(sums + (wave * 16 + my_q) * kFewPitch + cb * 16 + my_ch) = acc[u][cb];
-            if (my_ch == 0) ml[wave * 16 + my_q] = make_float2(m_ref[u], l);
+            if (my_ch == 0) ml[wave * 16 + my_q] = make_float2(m_ref[u] * a.scale_log2e, l);
             if (t < 16) lims[t] = lim[u];
             __syncthreads();
             const int qi = t >> 4, ch = (t & 15) * 8;
@@ -325,7 +327,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 #pragma unroll
                 for (int w = 0; w < kFewWaves; ++w) {
                     const float2 x = ml[w * 16 + qi];
-                    const float share = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((x.x - top_m) * a.scale_log2e);
+                    const float share = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - top_m);
                     den += share * x.y;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] += share * sums[(w * 16 + qi) * kFewPitch + ch + e];
@@ -593,7 +595,7 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
         }
         if (__any(m_new > m_ref + lazy_raw)) {                 // also the first visible tile (m_ref = -inf)
             const float m_use = m_new == -INFINITY ? 0.0f : m_new;
-            const float alpha = __builtin_amdgcn_exp2f((m_ref - m_use) * scale_log2e);
+            const float alpha = __builtin_amdgcn_exp2f(m_ref * scale_log2e - m_use * scale_log2e);
             l_run *= alpha;
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)
@@ -678,6 +680,8 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
         }
     }
 
+    const float ref = m_ref * scale_log2e;
+
     // ---- lane = query, registers = head channels (4 consecutive per group)
     const bool partial = a.n_split > 1;
     const bool write = m < M && (!partial || limit >= t0 * kChunkK);
@@ -701,7 +705,7 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4)
                 store4(dt, r4, v4f{acc_o[dt][r4 * 4], acc_o[dt][r4 * 4 + 1], acc_o[dt][r4 * 4 + 2], acc_o[dt][r4 * 4 + 3]}, inv_l);
-        if (partial && g == 0) a.part_ml[at] = make_float2(m_ref, l_run);
+        if (partial && g == 0) a.part_ml[at] = make_float2(ref, l_run);
     } else {
         // The two key groups of a query exchange halves of the channels: group kg finishes channels 64 kg .. 64 kg + 63.  The last
         // barrier of the loop has freed the tile buffers.
@@ -718,13 +722,13 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
         };
         if (kg == 0) give(acc_o[2], acc_o[3]);
         else give(acc_o[0], acc_o[1]);
-        mine[32 * 64] = m_ref;
+        mine[32 * 64] = ref;
         mine[33 * 64] = l_run;
         __syncthreads();
         if (!write) return;
-        const float m_o = theirs[32 * 64], l_o = theirs[33 * 64], top_m = fmaxf(m_ref, m_o);
-        const float own = m_ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_ref - top_m) * scale_log2e);
-        const float other = m_o == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_o - top_m) * scale_log2e);
+        const float m_o = theirs[32 * 64], l_o = theirs[33 * 64], top_m = fmaxf(ref, m_o);
+        const float own = ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top_m);
+        const float other = m_o == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_o - top_m);
         const float l_all = l_run * own + l_o * other, inv_l = l_all > 0.0f ? 1.0f / l_all : 0.0f;
         auto finish = [&](int dt, const v16f &acc, const float *from) {
 #pragma unroll
@@ -809,7 +813,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
         }
         top_p = fmaxf(top_p, __shfl_xor(top_p, 16, 64));
         top_p = fmaxf(top_p, __shfl_xor(top_p, 32, 64));
-        const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - top_p) * a.scale_log2e);
+        const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - top_p);
         top = top_p;
         den *= keep;
 #pragma unroll
@@ -817,7 +821,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
             if (ml[i].x == -INFINITY) continue;
-            const float share = __builtin_amdgcn_exp2f((ml[i].x - top) * a.scale_log2e);
+            const float share = __builtin_amdgcn_exp2f(ml[i].x - top);
             den = __builtin_fmaf(share, ml[i].y, den);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(share, v[i][e >> 2][e & 3], f[e]);

@@ -385,3 +385,33 @@ def test_routes(mq):
         args = (*device_step(mq, st), *(bounds_of(st) if bounds else (0, 0)))
         names = kernels(lambda: mq.paged_attention(*args))
         assert [n for n in names if "paged" in n] == want, (seqs, names)
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,slope,rows", [
+    ([(1, 200), (1, 70)], 28, 4, 400, None), ([(1, 1281)], 28, 4, 400, None), ([(5, 2500), (4, 300)], 28, 4, 30, None),
+    ([(60, 256)], 7, 1, 400, None), ([(40, 2000), (1, 700)], 8, 2, 30, None), ([(1300, 1300)], 28, 4, 4, [0, 700, 1023, 1024, 1298, 1299])])
+def test_large_logits_that_differ_by_single_steps(mq, seqs, hq, hkv, slope, rows):
+    """Scores are whole numbers of about 8e6 and exact in fp32 (logits 6.8e5 to 7.4e5): what waves, key groups, pieces and tiles have seen last
+    differs by a few of them, and what each adds to the sum has to be scaled alike.  Values are one-hot in the slot's number, so that the
+    channels of a result are the shares of the parts: in its lowest bits, then in its highest ones.  Probabilities are off by half a
+    step each (2^-11, 2^-25 in the subnormal range), in the numerator and in the denominator, the output by another, the fp32 sums by 2^-14."""
+    rng = np.random.default_rng(len(seqs) + slope)
+    st = make_step(rng, seqs, hq, hkv, 16, poison=False)
+    q = np.ones((st["T"], hq, D), dtype=np.float16)
+    q[:, :, :127] = (256 - np.arange(hq) % 20)[None, :, None]           # a head's scores: (256 - h) * 256 * 127 + the slot's step
+    st["q"] = q.reshape(st["T"], hq * D)
+    st["kp"][..., :127] = 256
+    longest = max(n for _, n in seqs)
+    for high in (False, True):
+        for s, (_, length) in enumerate(seqs):
+            for i in range(length):
+                page, r = orc.cache_slot(st["table"], 16, s, i, len(st["vp"]))
+                st["kp"][page, :, r, 127] = i // slope + 2 * (i // 32 % 4) + rng.integers(0, 3)
+                st["vp"][page, :, r] = np.eye(D, dtype=np.float16)[i * D // longest if high else i % D]
+        ref = orc.paged_attention_f64(st["q"], st["kp"], st["vp"], st["table"], st["start"], st["pos"], hq, rows=rows)
+        got = mq.paged_attention(*device_step(mq, st), *bounds_of(st)).cpu().numpy().astype(np.float64)
+        mine = ~np.isnan(ref[:, 0])
+        tol = (3 * 2.0 ** -11 + 2.0 ** -14) * ref + 2.0 ** -25 * (1 + 2 * longest)
+        err = np.abs(got - ref)[mine] - tol[mine]
+        worst = np.unravel_index(err.argmax(), err.shape)
+        assert (err <= 0).all(), f"high {high}: {(err + tol[mine])[worst]:.3e} > {tol[mine][worst]:.3e} at {worst}"
