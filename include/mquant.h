@@ -551,7 +551,8 @@ int mquant_kv_append(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ld
                      int32_t n_q_heads, double base, const mquant_paged_cache_t *cache, mquant_stream_t stream);
 
 /* Workspace of mquant_paged_attention for the same sizes and bounds (max_kv: table_pages * page_size where the call
- * passes 0): 0 where no sequence's keys are split. */
+ * passes 0 or more than that; asked with more it may be far larger, and does as well): 0 where no sequence's keys are
+ * split. */
 int64_t mquant_paged_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
                                                int32_t head_dim, int32_t max_rows, int32_t max_kv);
 
@@ -565,7 +566,8 @@ int64_t mquant_paged_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t
  *   q_dev, o_dev   : fp16 [T, n_q_heads * head_dim]; ldq a multiple of 8, ldo of 4; q 16-byte aligned, o 8-byte
  *   max_rows       : most rows a sequence has in this call, max_kv: largest pos + 1.  They choose the kernel and how keys
  *                    are split over work-groups, so that host values are enough to capture the call;
- *                    data beyond them still get right results.  0: not known (T, and the table's slots).
+ *                    data beyond them still get right results.  0: not known (T, and the table's slots); a max_kv
+ *                    beyond the table's slots counts as those.
  *   workspace_dev  : mquant_paged_attention_workspace_bytes(...) bytes, 256-byte aligned; scratch, concurrent
  *                    calls must not share it.  NULL where that is 0.
  * Slots up to the largest position of a sequence's rows must hold finite values, and logits (q k / sqrt(head_dim)) lie

@@ -619,6 +619,7 @@ class PagedCache:
         _operand(page_table, torch.int32, "page_table", tuple(page_table.shape))
         self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
         (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim), (self.n_seq, self.table_pages) = k_pages.shape, page_table.shape
+        self.slots = self.table_pages * self.page_size
         self.device_index = k_pages.device.index
         self.struct = PagedCacheStruct(_dp(k_pages), _dp(v_pages), _dp(page_table), self.n_seq, self.n_pages, self.page_size,
                                        self.table_pages, self.n_kv_heads, self.head_dim)
@@ -689,7 +690,7 @@ def kv_append(q, k, v, cache: PagedCache, row_start_dev, pos_dev, n_q_heads: int
 
 def paged_attention_workspace_bytes(T: int, cache: PagedCache, n_q_heads: int, max_rows: int = 0, max_kv: int = 0) -> int:
     n = int(lib.mquant_paged_attention_workspace_bytes(T, cache.n_seq, n_q_heads, cache.n_kv_heads, cache.head_dim, max_rows,
-                                                       max_kv or cache.table_pages * cache.page_size))
+                                                       min(max_kv, cache.slots) if max_kv else cache.slots))
     if n < 0:
         raise MQuantError(n, "mquant_paged_attention_workspace_bytes")
     return n
@@ -699,6 +700,8 @@ def paged_attention(q, cache: PagedCache, row_start_dev, pos_dev, n_q_heads: int
                     out=None, workspace=None):
     """q [T, >= Hq*D] fp16 of the step's rows -> o [T, Hq*D]; max_rows, max_kv: host bounds (0: not known)."""
     T, D = q.shape[0], cache.head_dim
+    if max_kv > cache.slots:
+        max_kv = cache.slots
     if out is None:
         out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
     if workspace is None:

@@ -40,6 +40,7 @@ constexpr int kChunkQ = 128;               // queries of a work-group (32 a wave
 constexpr int kChunkK = 64;                // slots of a tile
 constexpr int kTileBytes = kChunkK * 256;
 constexpr int kChunkLds = 4 * kTileBytes;  // two key and two value tiles
+constexpr int64_t kMaxThreads = 0xffffffffll;              // of a launch along one dimension
 constexpr int kAhead = 4;                  // LDS fragment reads in flight ahead of the MFMA that uses them
 
 // The running maximum that the sums are scaled to follows the true one lazily: only when some query's has grown by more
@@ -892,8 +893,11 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
         int64_t split = units < kNumCU / 2 ? kNumCU / units : units < kNumCU ? ceil_div(2 * kNumCU, units) : ceil_div(4 * kNumCU, units);
         if (units < kNumCU / 2 && split < ceil_div(kv, 4096)) split = ceil_div(kv, 4096);
         if (split > ceil_div(kv, kFewStep)) split = ceil_div(kv, kFewStep);
-        p.few_piece = static_cast<int32_t>(ceil_div(ceil_div(kv, split), kFewStep) * kFewStep);
-        p.few_split = static_cast<int32_t>(ceil_div(kv, p.few_piece));
+        if (split > kMaxThreads / (kFewWaves * 64) / units) split = kMaxThreads / (kFewWaves * 64) / units;
+        if (split > 1) {                                       // one piece has no length: rounded up it would not fit 32 bits
+            p.few_piece = static_cast<int32_t>(ceil_div(ceil_div(kv, split), kFewStep) * kFewStep);
+            p.few_split = static_cast<int32_t>(ceil_div(kv, p.few_piece));
+        }
         if (p.few_split > 1) p.few_part = units * p.few_stride * p.few_split;
     }
     if (p.chunk) {
@@ -948,7 +952,10 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
     if (ldq % 8 != 0 || ldo % 4 != 0 || !aligned_to(q, 16) || !aligned_to(o, 8) || !aligned_to(pos, 4) || !aligned_to(row_start, 4))
         return MQUANT_ERR_ALIGNMENT;
     const int32_t n_kv = cache->n_kv_heads;
-    const Plan p = make_plan(T, cache->n_seq, n_q_heads, n_kv, max_rows, max_kv > 0 ? max_kv : cache->table_pages * cache->page_size);
+    const int32_t slots = cache->table_pages * cache->page_size;
+    Plan p = make_plan(T, cache->n_seq, n_q_heads, n_kv, max_rows, max_kv > 0 && max_kv < slots ? max_kv : slots);
+    // scratch that was asked for with a bound beyond the table may be another size: then that bound's pieces are taken
+    if (max_kv > slots && workspace_bytes < p.bytes()) p = make_plan(T, cache->n_seq, n_q_heads, n_kv, max_rows, max_kv);
     const int64_t need = p.bytes();
     if (need > 0 && (!workspace || workspace_bytes < need)) return MQUANT_ERR_WORKSPACE;
     if (need > 0 && !aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
@@ -965,9 +972,9 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
         const int32_t xcds_per_kv = 8 % n_kv == 0 ? 8 / n_kv : 0;
         const int64_t items = static_cast<int64_t>(p.chunk_tiles) * p.chunk_split;
         const int64_t groups = xcds_per_kv > 0 ? 8 * ceil_div(items, xcds_per_kv) : items * n_kv;
-        if (groups > 0x7fffffff) return MQUANT_ERR_UNSUPPORTED;
-        auto kern = p.chunk_two ? paged_chunk_kernel<2> : paged_chunk_kernel<1>;
         const int key_groups = p.chunk_two ? 2 : 1;
+        if (groups * key_groups * 256 > kMaxThreads) return MQUANT_ERR_UNSUPPORTED;
+        auto kern = p.chunk_two ? paged_chunk_kernel<2> : paged_chunk_kernel<1>;
         static LdsLimit limits[2];
         if (const int st = limits[p.chunk_two].raise(reinterpret_cast<const void *>(kern), key_groups * kChunkLds); st != MQUANT_OK) return st;
         MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(key_groups * 256), key_groups * kChunkLds, stream, a, xcds_per_kv);
@@ -985,7 +992,6 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
         a.part += p.chunk_part * kD;
         a.part_ml += p.chunk_part;
         const int64_t units = static_cast<int64_t>(cache->n_seq) * n_kv, groups = units * p.few_split;
-        if (groups > 0x7fffffff) return MQUANT_ERR_UNSUPPORTED;
         auto kern = p.few_nq == 1 ? paged_few_kernel<1> : p.few_nq == 2 ? paged_few_kernel<2> : paged_few_kernel<3>;
         static LdsLimit limits[3];
         if (const int st = limits[p.few_nq - 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;

@@ -166,3 +166,17 @@ def test_errors_and_interrupts(both):
             with pytest.raises(error):
                 call(**{**operands, "ids": t})
     assert not seen
+
+
+@pytest.mark.parametrize("bound", [70, 80, 81, 2 ** 31 - 1, 2 ** 32 + 3, 2 ** 40])
+def test_a_bound_beyond_the_table_is_the_tables(both, bound):
+    """5 pages of 16 slots: the scratch that is asked for and the call go by 80 slots at most."""
+    mod, slow, seen, mp, _ = both
+    asked = []
+    mq.lib.mquant_paged_attention_workspace_bytes = staticmethod(lambda *a: asked.append(a) or 0)
+    operands, _ = calls()["paged_attention"]
+    cache = mq.PagedCache(Tensor(9, 2, 16, 128), Tensor(9, 2, 16, 128), i32(4, 5))
+    for way in (mod, slow):
+        mp.setattr(mq, "_fast", way)
+        mq.paged_attention(operands["q"], cache, operands["start"], operands["pos"], 6, 2, bound, out=operands["qo"])
+    assert [a[-1] for a in asked] == [min(bound, 80)] * 2 and [s[1][10] for s in seen] == [min(bound, 80)] * 2

@@ -415,3 +415,15 @@ def test_large_logits_that_differ_by_single_steps(mq, seqs, hq, hkv, slope, rows
         err = np.abs(got - ref)[mine] - tol[mine]
         worst = np.unravel_index(err.argmax(), err.shape)
         assert (err <= 0).all(), f"high {high}: {(err + tol[mine])[worst]:.3e} > {tol[mine][worst]:.3e} at {worst}"
+
+
+@pytest.mark.parametrize("seqs,hq,hkv", [([(1, 1 + 5 * i % 60) for i in range(128)], 8, 8), ([(1, 300), (3, 40)], 28, 4), ([(40, 300), (1, 9)], 8, 8)])
+def test_bounds_beyond_the_table(mq, seqs, hq, hkv):
+    """Bounds up to the largest number: the same bits as with the table's own slots."""
+    st = make_step(np.random.default_rng(len(seqs)), seqs, hq, hkv, 16)
+    t = device_step(mq, st)
+    want = mq.paged_attention(*t, 0, t[1].slots)
+    check(st, want, what="the table's slots")
+    mine = torch.from_numpy(np.concatenate([np.arange(a, b) for a, b in zip(st["start"], st["start"][1:])])).cuda()
+    for max_kv in (0, t[1].slots + 1, 2 ** 31 - 128, 2 ** 31 - 1, 2 ** 33):
+        assert torch.equal(mq.paged_attention(*t, 0, max_kv)[mine], want[mine])

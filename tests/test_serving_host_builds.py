@@ -37,3 +37,14 @@ def test_lds_limits_of_the_serving_kernels_on_every_device(tmp_path):
                     os.path.join(ROOT, "tests", "lds_limit_serving_driver.c"), "-o", exe, "-ldl"], check=True)
     r = subprocess.run([exe, mq.LIB_PATH], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
     assert r.returncode == 0, r.stdout
+
+
+def test_grids_and_scratch_for_any_host_bounds(tmp_path):
+    """Bounds from 0 to the largest number: no empty or oversized grid, and one beyond the table is the table's."""
+    if shutil.which("gcc") is None:
+        pytest.skip("no gcc")
+    exe = str(tmp_path / "serving_grid_driver")
+    subprocess.run(["gcc", "-std=gnu11", "-O1", "-rdynamic", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "tests"),
+                    os.path.join(ROOT, "tests", "serving_grid_driver.c"), "-o", exe, "-ldl"], check=True)
+    r = subprocess.run([exe, mq.LIB_PATH], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout
