@@ -552,7 +552,8 @@ int mquant_kv_append(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ld
 
 /* Workspace of mquant_paged_attention for the same sizes and bounds (max_kv: table_pages * page_size where the call
  * passes 0 or more than that; asked with more it may be far larger, and does as well): 0 where no sequence's keys are
- * split. */
+ * split.  It depends on how they are split and does not grow with each size: scratch for a step of more rows or longer
+ * sequences need not do for a smaller one, so take the largest over the steps that share it. */
 int64_t mquant_paged_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
                                                int32_t head_dim, int32_t max_rows, int32_t max_kv);
 
@@ -581,7 +582,8 @@ int mquant_paged_attention(const void *q_dev, int64_t ldq, const mquant_paged_ca
                            int32_t n_q_heads, int32_t max_rows, int32_t max_kv, void *workspace_dev,
                            int64_t workspace_bytes, mquant_stream_t stream);
 
-/* Workspace of mquant_lora_apply (the rank-sized intermediate in fp32).  Negative status on a bad shape or rank. */
+/* Workspace of mquant_lora_apply (the rank-sized intermediate in fp32).  It grows with T, K and rank: scratch for the
+ * largest of each does for any smaller call.  Negative status on a bad shape or rank. */
 int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t rank);
 
 /*

@@ -603,12 +603,29 @@ int64_t few_slices(int32_t K)
 // 128 with 2 / 3 / 4 slices: 2889 rows 40.0 / 40.2 / 39.3, 4096 48.6 / 48.6 / 54.1, 1000 29.4 / 27.2 / 25.5 and 28.2 with 8).
 constexpr int32_t kManyRank = 64;          // ranks of a part
 int64_t rank_parts(int32_t rank) { return rank > kManyRank ? 2 : 1; }
+int64_t wanted_slices(int32_t K, int64_t parts)
+{
+    return static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)) / static_cast<double>(parts))));
+}
 int64_t many_slices(int32_t T, int32_t K, int32_t rank)
 {
-    int64_t s = static_cast<int64_t>(ceil(sqrt(2.0 * static_cast<double>(ceil_div(K, kStage)) / static_cast<double>(rank_parts(rank)))));
+    int64_t s = wanted_slices(K, rank_parts(rank));
     const int64_t most = kNumCU / (ceil_div(T, kRows) * rank_parts(rank));
     if (s > most) s = most;
     return s < 1 ? 1 : s;
+}
+
+// The most that T rows or fewer have of rows times slices: s slices go with up to kNumCU / (s parts) tiles.
+int64_t most_row_slices(int32_t T, int32_t K, int64_t parts)
+{
+    int64_t most = 0, s = wanted_slices(K, parts);
+    if (s > kNumCU / parts) s = kNumCU / parts;
+    for (; s > 1; --s) {
+        const int64_t rows = static_cast<int32_t>(kNumCU) / static_cast<int32_t>(s * parts) * kRows;
+        if (T <= rows) break;
+        if (s * rows > most) most = s * rows;
+    }
+    return s * T > most ? s * T : most;
 }
 
 // Tiles of 16 rows or of 64: 64 where they are full.  Tiles of 64 / of 16, shrink + expansion in us, K = 3584, N = 4608, rank 16 and 64, 4 adapters:
@@ -664,9 +681,14 @@ extern "C" int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t ran
     if (T < 0 || K < 0 || rank < 1) return MQUANT_ERR_BAD_SHAPE;
     if (K == 0 || K % 8 != 0 || rank % 8 != 0 || rank > 128) return MQUANT_ERR_UNSUPPORTED;
     if (T == 0) return 0;
-    int64_t slices = many_slices(T, K, rank);
-    if (T <= kFewMax && few_slices(K) > slices) slices = few_slices(K);        // whichever the number of adapters asks for
-    return ceil_div(slices * T * rank * 4, 256) * 256;
+    // whichever way the number of adapters chooses, and no less than fewer rows or lower ranks take: scratch for the largest step does for all
+    const int64_t few = few_slices(K) * (T < kFewMax ? T : kFewMax), many = most_row_slices(T, K, rank_parts(rank));
+    int64_t floats = (few > many ? few : many) * rank;
+    if (rank > kManyRank) {
+        const int64_t lower = most_row_slices(T, K, 1) * kManyRank;
+        if (lower > floats) floats = lower;
+    }
+    return ceil_div(floats * 4, 256) * 256;
 }
 
 extern "C" int mquant_lora_apply(const void *x, int64_t ldx, const int32_t *perm, const int32_t *adapter, const void *a, const void *b,

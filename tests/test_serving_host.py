@@ -138,3 +138,17 @@ def test_binding_refuses_host_tensors():
     with pytest.raises(mq.MQuantError) as e:
         mq.PagedCache(pages[0], pages[0], table)
     assert e.value.status == mq.ERR_BAD_SHAPE
+
+
+@pytest.mark.parametrize("K", [8, 512, 3584, 18944, 29568, 1 << 20])
+def test_scratch_of_the_adapters_grows_with_rows_channels_and_rank(K):
+    """Scratch for the largest step does for every smaller one."""
+    size = L.mquant_lora_workspace_bytes
+    rows = sorted({*range(1, 300), *range(300, 5000, 61), *(64 * i + d for i in range(1, 80) for d in (0, 1)), 16384, 16385, 100000, 1 << 24})
+    for rank in (8, 16, 64, 72, 128):
+        sizes = [size(T, K, rank) for T in rows]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), rank
+        assert all(s >= T * rank * 4 for s, T in zip(sizes, rows))
+    for T in rows[::7]:
+        by_rank = [size(T, K, r) for r in range(8, 129, 8)]
+        assert by_rank == sorted(by_rank) and size(T, K, 64) <= size(T, K + 8, 64) and size(T, K, 128) <= size(T, K + 512, 128)
