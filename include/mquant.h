@@ -521,7 +521,7 @@ typedef struct {
  * in fp32 (angles in double), rounded to fp16 once.  mquant_rope_apply is the same without the norm, in place.
  *   q_dev, k_dev         : fp16 [T, n_heads * head_dim], leading dimensions multiples of 8, 16-byte aligned
  *   q_out_dev, k_out_dev : the same layout (written); q_out_dev == q_dev with the same leading dimension
- *                          works in place, likewise k; no other overlap of an output with an input or output
+ *                          (of a single row: any) works in place, likewise k; no other overlap of an output with an input or output
  *   q_weight_dev, k_weight_dev : fp16 [head_dim], 16-byte aligned, or NULL: no norm
  *   eps                  : finite, >= 0
  *   n_q_heads, n_kv_heads: >= 0, not both 0; the pointers of a side without heads are not read

@@ -125,13 +125,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
     }
 }
 
-int check_side(const void *x, int64_t ldx, const void *out, int64_t ldo, int32_t heads)
+int check_side(const void *x, int64_t ldx, const void *out, int64_t ldo, int32_t T, int32_t heads)
 {
     if (heads == 0) return MQUANT_OK;
     if (!x || !out) return MQUANT_ERR_NULL;
     const int64_t w = static_cast<int64_t>(heads) * kD;
     if (ldx < w || ldo < w) return MQUANT_ERR_BAD_SHAPE;
-    if (x == out && ldx != ldo) return MQUANT_ERR_BAD_SHAPE;
+    if (x == out && ldx != ldo && T > 1) return MQUANT_ERR_BAD_SHAPE;         // of a single row it says nothing
     if (ldx % 8 != 0 || ldo % 8 != 0 || !aligned_to(x, 16) || !aligned_to(out, 16)) return MQUANT_ERR_ALIGNMENT;
     return MQUANT_OK;
 }
@@ -182,8 +182,8 @@ extern "C" int mquant_qk_norm_rope(const void *q, int64_t ldq, void *q_out, int6
     if (T == 0) return MQUANT_OK;
     if (!pos) return MQUANT_ERR_NULL;
     if (!aligned_to(pos, 4)) return MQUANT_ERR_ALIGNMENT;
-    if (const int st = check_side(q, ldq, q_out, ldqo, n_q_heads); st != MQUANT_OK) return st;
-    if (const int st = check_side(k, ldk, k_out, ldko, n_kv_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(q, ldq, q_out, ldqo, T, n_q_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(k, ldk, k_out, ldko, T, n_kv_heads); st != MQUANT_OK) return st;
     const Rows a = {static_cast<const __half *>(q), static_cast<const __half *>(k), nullptr, static_cast<__half *>(q_out),
                     static_cast<__half *>(k_out), ldq, ldqo, ldk, ldko, 0, static_cast<const __half *>(q_weight),
                     static_cast<const __half *>(k_weight), pos, nullptr, nullptr, eps, T, n_q_heads, n_kv_heads};
@@ -201,9 +201,9 @@ extern "C" int mquant_kv_append(const void *q, int64_t ldq, void *q_out, int64_t
     if (T == 0 || cache->n_seq == 0) return MQUANT_OK;
     if (!row_start || !pos) return MQUANT_ERR_NULL;
     if (!aligned_to(row_start, 4) || !aligned_to(pos, 4) || !aligned_to(rope_pos, 4)) return MQUANT_ERR_ALIGNMENT;
-    if (const int st = check_side(q, ldq, q_out, ldqo, n_q_heads); st != MQUANT_OK) return st;
-    if (const int st = check_side(k, ldk, cache->k_pages_dev, ldk, cache->n_kv_heads); st != MQUANT_OK) return st;
-    if (const int st = check_side(v, ldv, cache->v_pages_dev, ldv, cache->n_kv_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(q, ldq, q_out, ldqo, T, n_q_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(k, ldk, cache->k_pages_dev, ldk, T, cache->n_kv_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(v, ldv, cache->v_pages_dev, ldv, T, cache->n_kv_heads); st != MQUANT_OK) return st;
     const Rows a = {static_cast<const __half *>(q), static_cast<const __half *>(k), static_cast<const __half *>(v),
                     static_cast<__half *>(q_out), nullptr, ldq, ldqo, ldk, 0, ldv, static_cast<const __half *>(q_weight),
                     static_cast<const __half *>(k_weight), pos, rope_pos, row_start, eps, T, n_q_heads, cache->n_kv_heads};

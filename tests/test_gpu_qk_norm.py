@@ -195,3 +195,24 @@ def test_append_captured(mq, T):
         ref = orc.qk_norm_rope_f64(host(q), w.cpu().numpy(), pos.cpu().numpy(), hq)
         check(host(o)[:T - rep], ref[:T - rep], f"replay {rep}")
         assert bool(vp.any()) and not bool(o[T - rep:].any())
+
+
+def test_a_single_row_in_place_whatever_its_width(mq):
+    """A row alone is written where it was read from, also where the two views of it end elsewhere."""
+    rng = np.random.default_rng(21)
+    hq, hkv = 6, 2
+    x = rng.standard_normal((1, (hq + 2 * hkv) * D)).astype(np.float16)
+    pos = np.array([9], dtype=np.int32)
+    want_q, want_k = orc.qk_norm_rope_f64(x[:, :hq * D], None, pos, hq), orc.qk_norm_rope_f64(x[:, hq * D:(hq + hkv) * D], None, pos, hkv)
+    b = dev(x)
+    mq.qk_norm_rope(b, b[:, hq * D:], None, None, dev(pos), hq, hkv, q_out=b[:, :hq * D], k_out=b[:, hq * D:(hq + hkv) * D])
+    check(host(b)[:, :hq * D], want_q, "q")
+    check(host(b)[:, hq * D:(hq + hkv) * D], want_k, "k")
+    assert torch.equal(b[:, (hq + hkv) * D:], dev(x)[:, (hq + hkv) * D:])
+    b = dev(x)
+    cache = mq.PagedCache(*(torch.zeros((2, hkv, 16, D), dtype=torch.float16, device="cuda") for _ in range(2)),
+                          dev(np.array([[1]], dtype=np.int32)))
+    mq.kv_append(b, b[:, hq * D:], b[:, (hq + hkv) * D:], cache, dev(np.array([0, 1], dtype=np.int32)), dev(pos), hq, q_out=b[:, :hq * D])
+    check(host(b)[:, :hq * D], want_q, "q")
+    assert torch.equal(b[:, hq * D:], dev(x)[:, hq * D:])
+    check(host(cache.k_pages[1, :, 9]).reshape(1, -1), want_k, "k page")
