@@ -525,7 +525,8 @@ typedef struct {
  *   q_weight_dev, k_weight_dev : fp16 [head_dim], 16-byte aligned, or NULL: no norm
  *   eps                  : finite, >= 0
  *   n_q_heads, n_kv_heads: >= 0, not both 0; the pointers of a side without heads are not read
- * Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED (head_dim != 128), ERR_ALIGNMENT.
+ * Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED (head_dim != 128, 2^26 rows and more of up to 16 heads, 2^25 of up to
+ *         32 ...: sizes beyond the grid), ERR_ALIGNMENT.
  */
 int mquant_qk_norm_rope(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ldqo, const void *k_dev, int64_t ldk,
                         void *k_out_dev, int64_t ldko, const void *q_weight_dev, const void *k_weight_dev, float eps,

@@ -40,7 +40,6 @@ constexpr int kChunkQ = 128;               // queries of a work-group (32 a wave
 constexpr int kChunkK = 64;                // slots of a tile
 constexpr int kTileBytes = kChunkK * 256;
 constexpr int kChunkLds = 4 * kTileBytes;  // two key and two value tiles
-constexpr int64_t kMaxThreads = 0xffffffffll;              // of a launch along one dimension
 constexpr int kAhead = 4;                  // LDS fragment reads in flight ahead of the MFMA that uses them
 
 // The running maximum that the sums are scaled to follows the true one lazily: only when some query's has grown by more

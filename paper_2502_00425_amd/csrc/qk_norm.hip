@@ -161,7 +161,7 @@ int launch(const Rows &a, const PagedCache &c, double base, hipStream_t stream)
     const bool few = a.T * groups < 6000;
     if (few) waves = groups;
     const int64_t blocks = ceil_div(a.T * waves, 4);
-    if (blocks > 0x7fffffff || heads > 1 << 20) return MQUANT_ERR_UNSUPPORTED;
+    if (blocks > kMaxThreads / 256 || heads > 1 << 20) return MQUANT_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(blocks));
     const int32_t per = static_cast<int32_t>(ceil_div(groups, waves)), n = static_cast<int32_t>(waves);
     if (few) MQ_LAUNCH((qk_norm_rope_kernel<APPEND, 1>), grid, dim3(256), 0, stream, a, c, inv, n, per);

@@ -9,6 +9,7 @@
 namespace mquant {
 
 constexpr int kCacheHeadDim = 128;
+constexpr int64_t kMaxThreads = 0xffffffffll;              // of a launch along one dimension
 
 struct PagedCache {
     __half *k, *v;

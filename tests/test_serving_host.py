@@ -152,3 +152,12 @@ def test_scratch_of_the_adapters_grows_with_rows_channels_and_rank(K):
     for T in rows[::7]:
         by_rank = [size(T, K, r) for r in range(8, 129, 8)]
         assert by_rank == sorted(by_rank) and size(T, K, 64) <= size(T, K + 8, 64) and size(T, K, 128) <= size(T, K + 512, 128)
+
+
+def test_rows_beyond_a_grid_are_refused():
+    """2^32 threads are more than a launch takes: a wave of 64 to a row of up to 16 heads."""
+    keep, address = cache(k=Q + 65536, v=Q + 131072)
+    for T, heads in ((1 << 26, 1), (1 << 26, 16), (1 << 25, 17), (2 ** 31 - 1, 1)):
+        w = heads * 128
+        assert L.mquant_qk_norm_rope(P, w, Q, w, None, 0, None, 0, None, None, 1e-6, P, T, heads, 0, 128, 1e4, None) == mq.ERR_UNSUPPORTED
+        assert L.mquant_kv_append(P, w, Q, w, P, 512, P, 512, None, None, 1e-6, P, P, None, T, heads, 1e4, address, None) == mq.ERR_UNSUPPORTED
