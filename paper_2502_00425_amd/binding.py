@@ -584,13 +584,15 @@ def w4g128_gemm(x, w_prepacked, N: int, out=None):
 
 # ----------------------------------------------------------- serving step
 
-def _operand(t, dtype, what: str, shape=None):
+def _operand(t, dtype, what: str, shape=None, counted: bool = True):
     """A device operand of the serving entries: on the current device, of this type, and of `shape` (contiguous) or
-    2-D with unit column stride, whose leading dimension is returned."""
+    2-D with unit column stride, whose leading dimension is returned.  The ABI counts in 32 bits (scratch aside)."""
     if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected a tensor on the current device")
     if t.dtype is not dtype:
         raise MQuantError(ERR_UNSUPPORTED, f"{what}: expected {dtype}, got {t.dtype}")
+    if counted and max(t.shape, default=0) > 0x7fffffff:
+        raise MQuantError(ERR_UNSUPPORTED, f"{what}: a size of {tuple(t.shape)} is beyond 32 bits")
     if shape is None:
         ld = 0 if t.dim() == 2 and t.shape[0] == 0 else _rows(t, what)
         return ld if t.shape[0] > 1 else t.shape[1] + -t.shape[1] % 8       # the stride of a single row, or of none, says nothing
@@ -636,7 +638,7 @@ def _step(cache, row_start_dev, pos_dev, T: int) -> None:
 
 def _workspace(ws) -> None:
     if ws is not None:
-        _operand(ws, ws.dtype, "workspace", tuple(ws.shape))
+        _operand(ws, ws.dtype, "workspace", tuple(ws.shape), counted=False)
 
 
 def _weight(w, head_dim: int, what: str) -> None:

@@ -180,3 +180,34 @@ def test_a_bound_beyond_the_table_is_the_tables(both, bound):
         mp.setattr(mq, "_fast", way)
         mq.paged_attention(operands["q"], cache, operands["start"], operands["pos"], 6, 2, bound, out=operands["qo"])
     assert [a[-1] for a in asked] == [min(bound, 80)] * 2 and [s[1][10] for s in seen] == [min(bound, 80)] * 2
+
+
+def test_sizes_beyond_32_bits_call_nothing(both):
+    """Rows, channels, columns, sequences and pages whose lowest 32 bits would make sense."""
+    mod, slow, seen, mp, _ = both
+    far = 1 << 32
+    mq.lib.mquant_lora_workspace_bytes = mq.lib.mquant_paged_attention_workspace_bytes = staticmethod(lambda *a: 256)
+    for way in (mod, slow):
+        mp.setattr(mq, "_fast", way)
+        for name in TYPES:                                                    # rows
+            operands, call = calls(rows=far + 3)[name]
+            with pytest.raises(mq.MQuantError) as e:
+                call(**operands)
+            assert e.value.status == mq.ERR_UNSUPPORTED
+        operands, call = calls()["lora_apply"]
+        for other in (dict(x=Tensor(3, far + 64), a=Tensor(3, 16, far + 64)),
+                      dict(base=Tensor(3, far + 40), b=Tensor(3, far + 40, 16), out=Tensor(3, far + 40)),
+                      dict(a=Tensor(far + 3, 16, 64), b=Tensor(far + 3, 40, 16), scale=Tensor(far + 3, dtype=torch.float32))):
+            with pytest.raises(mq.MQuantError) as e:
+                call(**{**operands, **other})
+            assert e.value.status == mq.ERR_UNSUPPORTED
+        for pages, table in (((far + 9, 2, 16, 128), (4, 5)), ((9, 2, 16, 128), (far + 4, 5)), ((9, 2, 16, 128), (4, far + 5))):
+            with pytest.raises(mq.MQuantError) as e:
+                mq.PagedCache(Tensor(*pages), Tensor(*pages), i32(*table))
+            assert e.value.status == mq.ERR_UNSUPPORTED
+    assert not seen
+    operands, call = calls()["lora_apply"]                                    # scratch may be as large as it likes
+    for way in (mod, slow):
+        mp.setattr(mq, "_fast", way)
+        call(**{**operands, "ws": Tensor(far + 4096, dtype=torch.uint8)})
+    assert [s[1][-2] for s in seen] == [far + 4096] * 2
