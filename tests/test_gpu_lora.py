@@ -245,3 +245,16 @@ def test_many_rows_replayed(mq):
         g.replay()
         torch.cuda.synchronize()
         check(c, out, what=f"replay {rep}")
+
+
+@pytest.mark.parametrize("T,N", [(5, 264), (256, 130), (900, 264), (900, 16392), (1300, 264)])
+def test_many_more_adapters_than_rows_use(mq, T, N):
+    """Five of five hundred in use."""
+    rng = np.random.default_rng(T + N)
+    used = np.array([0, 17, 255, 256, 499])
+    c = make(rng, T, 136, N, 16, 500, ids=np.where(np.arange(T) % 7 == 6, 500, used[np.arange(T) * 3 % 5]))
+    got = call(mq, c)
+    five = {**c, "a": c["a"][used], "b": c["b"][used], "scale": c["scale"][used]}
+    five["ids"] = np.where(c["ids"] == 500, -1, np.searchsorted(used, c["ids"])).astype(np.int32)
+    check(five, got, what=f"{T} {N}")
+    check(five, call(mq, five), what=f"{T} {N}, five")

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from oracle import mquant_oracle as orc
-from serving import D
+from serving import D, attention_bound
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -77,3 +77,54 @@ def test_prompt_in_chunks_then_tokens():
     wo = mq.w4_prepack(dev(rng.integers(0, 256, (K, hq * D // 2), dtype=np.uint8)))
     oq = mq.hadamard_quant_act(o, 0, 0.05, 0.05, 128)
     assert torch.isfinite(mq.w4a8_gemm(oq, wo, wscale[:K].contiguous(), K, 0, 0.05, 0.05)).all()
+
+
+def test_later_steps_see_every_slot_of_earlier_ones():
+    """Three sequences over several steps, the last of them in the pages that the first has given back: keys and values in the pages
+    against fp64 (2^-11 |y|, 2^-25, and 2^-19 of a pair's magnitude before the rounding), what a step does not write as it was, and
+    attention over the pages as they are, from the queries that the append wrote, within serving.attention_bound."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2502_00425_amd import binding as mq
+    rng = np.random.default_rng(3)
+    hq, hkv, page, n_pages = 14, 2, 16, 40
+    pages = rng.permutation(n_pages).astype(np.int32)
+    table = np.full((3, 14), -3, dtype=np.int32)
+    table[0, :8], table[1] = pages[:8], pages[8:22]
+    kp = torch.full((n_pages, hkv, page, D), float("nan"), dtype=torch.float16, device="cuda")
+    vp = torch.full_like(kp, float("inf"))
+    wq, wk = (rng.uniform(0.5, 1.5, D).astype(np.float16) for _ in range(2))
+    have = [0, 0, 0]
+    steps = [((70, [(10, 40)]), (33, []), (0, [])), ((41, []), (50, [(0, 30)]), (0, [])), ((1, []), (1, []), (0, [])), ((5, []), (1, []), (0, [])),
+             ((0, []), (90, [(7, 60)]), (100, [(3, 90)])), ((0, []), (1, []), (1, [])), ((0, []), (4, []), (2, []))]
+    for number, counts in enumerate(steps):
+        if number == 4:
+            table[2, :8], table[0] = table[0, :8], -3                  # the first sequence is done
+        T = sum(n for n, _ in counts)
+        start = np.concatenate([[0], np.cumsum([n for n, _ in counts])]).astype(np.int32)
+        pos = np.concatenate([have[s] + orc.aifs_build_perm(n, spans)[0] for s, (n, spans) in enumerate(counts)]).astype(np.int32)
+        have = [h + n for h, (n, _) in zip(have, counts)]
+        qkv = rng.standard_normal((T, (hq + 2 * hkv) * D)).astype(np.float16)
+        k0, v0 = kp.cpu().numpy(), vp.cpu().numpy()
+        x = dev(qkv)
+        q, k, v = x[:, :hq * D], x[:, hq * D:(hq + hkv) * D], x[:, (hq + hkv) * D:]
+        cache = mq.PagedCache(kp, vp, dev(table))
+        mq.kv_append(q, k, v, cache, dev(start), dev(pos), hq, dev(wq), dev(wk), q_out=q)
+        o = mq.paged_attention(q, cache, dev(start), dev(pos), hq, max(n for n, _ in counts), int(pos.max()) + 1).cpu().numpy()
+        k1, v1 = kp.cpu().numpy(), vp.cpu().numpy()
+        k64 = orc.qk_norm_rope_f64(qkv[:, hq * D:(hq + hkv) * D], wk, pos, hkv)
+        new = np.zeros((n_pages, page), dtype=bool)
+        for s, rows in orc.sequence_rows(start, T):
+            for i in rows:
+                p, r = orc.cache_slot(table, page, s, int(pos[i]), n_pages)
+                new[p, r] = True
+                pair = np.repeat(np.abs(k64[i]).reshape(-1, 2).sum(axis=1), 2)
+                tol = 2.0 ** -11 * np.abs(k64[i]) + 2.0 ** -25 + 2.0 ** -19 * np.sqrt(2) * pair
+                assert (np.abs(k1[p, :, r].reshape(-1).astype(np.float64) - k64[i]) <= tol).all()
+                assert np.array_equal(v1[p, :, r].reshape(-1), qkv[i, (hq + hkv) * D:])
+        for before, after in ((k0, k1), (v0, v1)):
+            was, now = (a.view(np.uint16).transpose(0, 2, 1, 3)[~new] for a in (before, after))
+            assert np.array_equal(was, now)
+        st = {"T": T, "hq": hq, "hkv": hkv, "q": q.cpu().numpy(), "kp": k1, "vp": v1, "table": table, "start": start, "pos": pos}
+        ref = orc.paged_attention_f64(st["q"], k1, v1, table, start, pos, hq)
+        assert (np.abs(o.astype(np.float64) - ref) <= attention_bound(st, ref)).all(), number
