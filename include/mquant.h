@@ -563,8 +563,10 @@ int64_t mquant_paged_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t
  * tokens) or a whole chunk of a prompt, mixed in one call as they come:
  *     o[i] = softmax(q[i] k[j]^T / sqrt(head_dim)) v[j] over the slots j <= pos[i] of row i's sequence
  * per head (query head h reads key/value head h / (n_q_heads / n_kv_heads)); fp32 softmax statistics, fp16
- * MFMA operands.  The rows' own keys and values are in the cache already (mquant_kv_append).  A row that
- * sees no slot (pos[i] < 0) gets zeros.  Positions beyond the table count as its last slot.
+ * MFMA operands.  Probabilities are such operands: each is off by 2^-11 of itself, and one below 2^-25 of the row's
+ * largest counts as nothing, so that a flat tail behind a peak can lose slots * 2^-25 of the sum.  The rows' own keys and
+ * values are in the cache already (mquant_kv_append).  A row that sees no slot (pos[i] < 0) gets zeros.  Positions beyond
+ * the table count as its last slot.
  *   q_dev, o_dev   : fp16 [T, n_q_heads * head_dim]; ldq a multiple of 8, ldo of 4; q 16-byte aligned, o 8-byte
  *   max_rows       : most rows a sequence has in this call, max_kv: largest pos + 1.  They choose the kernel and how keys
  *                    are split over work-groups, so that host values are enough to capture the call;
@@ -591,7 +593,10 @@ int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t rank);
  * DEVICE.  Low-rank adapters of many requests beside a shared linear: with base the linear's output (of
  * mquant_w4a8_gemm, mquant_w4g128_gemm ... on the same x) and a = adapter[i],
  *     h[i] = x[perm[i]] A_a^T,   y[i, n] = fp16( base[i, n] + scale[a] * sum_r h[i, r] B_a[n, r] )
- * sums and h in fp32 or better.  Rows with adapter[i] outside [0, n_adapters) have none: y = base.
+ * h is summed in fp32; into the second product, whose sums are fp32 too, it goes as two fp16 parts, which lose at most
+ * 2^-22 of the row's largest h.  Rows with adapter[i] outside [0, n_adapters) have none: y = base.  What is not finite in
+ * x, A or B shows in the rows (of B: in the columns of the rows) that use it, as NaN also where the formula has an
+ * infinity, and nowhere else.
  *   x_dev       : fp16 [T, K], leading dimension ldx (multiple of 8), 16-byte aligned: the linear's input BEFORE
  *                 rotation and quantization
  *   perm_dev    : NULL, or int32 [T]: row i of y belongs to row perm[i] of x (an entry outside [0, T) reads row 0)
@@ -604,7 +609,8 @@ int64_t mquant_lora_workspace_bytes(int32_t T, int32_t K, int32_t rank);
  *   workspace_dev : mquant_lora_workspace_bytes(T, K, rank) bytes, 256-byte aligned; scratch, concurrent
  *                 calls must not share it
  * rank: a multiple of 8 up to 128, K a multiple of 8, K and N at most 2^30, T at most 65535 * 256 (ERR_UNSUPPORTED
- * otherwise).  Rows of one adapter next to each other are the fast case; any order is right.
+ * otherwise).  Rows of one adapter next to each other are the fast case; any order is right.  n_adapters chooses the
+ * grids: many more of them than the rows use cost time.
  * T == 0 or N == 0 is a no-op.  Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_ALIGNMENT.
  */
 int mquant_lora_apply(const void *x_dev, int64_t ldx, const int32_t *perm_dev, const int32_t *adapter_dev,

@@ -631,6 +631,9 @@ int64_t most_row_slices(int32_t T, int32_t K, int64_t parts)
 // Tiles of 16 rows or of 64: 64 where they are full.  Tiles of 64 / of 16, shrink + expansion in us, K = 3584, N = 4608, rank 16 and 64, 4 adapters:
 // 128 rows 10.2 / 9.6 and 14.5 / 13.4, 256 10.6 / 10.9 and 14.9 / 16.5, 512 11.3 / 13.2 and 16.6 / 22.1; 64 adapters, each row another:
 // 128 rows 52.4 / 35.8 and 61.0 / 42.7, 512 89 / 61 and 111 / 73, 1024 108 / 107 and 141 / 132.
+// The host knows how many adapters there are, not how many the rows use, and takes the one for the other, here and for the tiles of the grids.  Where far
+// more are loaded than used that is wrong (K = 3584, N = 4608, rank 64, us): 4096 rows of 5 adapters, 5 / 500 loaded, 34.5 / 104 (26 times the
+// work-groups, nearly all of which find no tile), 256 rows of 5 16.3 / 27.8, 1000 rows of one, 1 / 64 loaded, 20.0 / 36.1; up to 48 rows no difference.
 constexpr int32_t kFewMax = 1024;
 bool few_rows(int32_t T, int32_t n_adapters) { return T <= 128 || (T <= kFewMax && n_adapters >= T / 16); }
 

@@ -258,3 +258,18 @@ def test_many_more_adapters_than_rows_use(mq, T, N):
     five["ids"] = np.where(c["ids"] == 500, -1, np.searchsorted(used, c["ids"])).astype(np.int32)
     check(five, got, what=f"{T} {N}")
     check(five, call(mq, five), what=f"{T} {N}, five")
+
+
+@pytest.mark.parametrize("T", [21, 400])
+def test_adapters_that_are_not_finite_stay_by_themselves(mq, T):
+    """An infinity in A shows in every column of the rows that use it, one in B in its own column of them, and nowhere else."""
+    rng = np.random.default_rng(T + 1)
+    c = make(rng, T, 264, 200, 24, 4, ids=np.arange(T) % 5 - 1)
+    want = call(mq, c)
+    c["a"][1, 5, 263], c["b"][2, 77, 3] = np.inf, -np.inf
+    got = call(mq, c)
+    ids = torch.from_numpy(c["ids"]).cuda()
+    odd = torch.zeros((T, 200), dtype=torch.bool, device="cuda")
+    odd[:, 77] = ids == 2
+    odd[ids == 1] = True
+    assert not torch.isfinite(got[odd]).any() and torch.equal(got[~odd], want[~odd])
