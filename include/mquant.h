@@ -619,6 +619,165 @@ int mquant_lora_apply(const void *x_dev, int64_t ldx, const int32_t *perm_dev, c
                       void *workspace_dev, int64_t workspace_bytes, mquant_stream_t stream);
 
 /* -------------------------------------------------------------------------
+ * The serving loop around the layers: a step's rows, pages and positions from the lengths of its sequences, the rotations
+ * of models whose channels, positions or contexts are not those of mquant_kv_append, attention of sequences that begin with the
+ * same tokens, and the next token of every row of logits.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * DEVICE.  The bookkeeping of a step: which rows the sequences get, their pages, positions and slots, all from arrays in
+ * device memory, so that a captured loop needs no host.  A sequence with rows[s] < 0 has ended: its pages behind the first
+ * shared[s] go to the end of the free pages, and its length becomes 0.  Then, in the order of the sequences,
+ *     r[s]    = rows[s], or 0 where rows[s] <= 0 or length[s] + rows[s] is more than the table holds
+ *     need[s] = ceil((length[s] + r[s]) / page_size) - ceil(length[s] / page_size)
+ * and a sequence is served while r[0] + .. + r[s] <= T and need[0] + .. + need[s] <= the free pages there are (those given back in
+ * this call among them); from the first that is not, no sequence gets rows.  Served sequences take pages from the front of
+ * the free pages, length becomes length + r, and row i = row_start[s] + j gets
+ *     pos[i] = length[s] + order[i] (order NULL: j),   slot[i] = page_table[s][pos / page_size] * page_size + pos % page_size.
+ * Rows from row_start[n_seq] on, and rows whose order is outside [0, r[s]), get pos -1 and slot -1; so does the slot of a page
+ * id outside [0, n_pages).  row_start, pos and the table are what mquant_kv_append and the attention entries take.
+ *   length_dev, length_out_dev : int32 [n_seq], tokens cached before and with the step; negative lengths count as 0.
+ *                     length_out_dev == length_dev works in place
+ *   rows_dev        : int32 [n_seq], new rows asked for
+ *   shared_dev      : NULL (none), or int32 [n_seq]: leading pages of a sequence that are not its own
+ *   order_dev       : NULL, or int32 [T]: the place of row i among its sequence's new tokens (AIFS order: the
+ *                     permutation of mquant_aifs_build_perm)
+ *   page_table_dev  : int32 [n_seq, table_pages], contiguous; entries of the pages taken are written
+ *   free_pages_dev  : int32 [n_pages], a ring of page ids; free_state_dev, free_state_out_dev: int32 [2], where the ring
+ *                     begins and how many ids it holds, before and behind the call (both may be the same array)
+ *   row_start_dev   : int32 [n_seq + 1] (written); pos_dev int32 [T], slot_dev int64 [T] (written; slot_dev may be NULL)
+ * A state outside [0, n_pages) counts as its remainder, a count above n_pages as n_pages.  No other overlap of arrays.  T == 0 serves
+ * no rows and gives pages back all the same; n_seq == 0 writes row_start, the state and -1.
+ * Errors: ERR_NULL, ERR_BAD_SHAPE (negative sizes, n_pages or table_pages < 1 where there are sequences), ERR_UNSUPPORTED
+ *         (page_size not a power of two in 16 .. 4096, table beyond 2^31 slots, n_seq > 2^20), ERR_ALIGNMENT (of the types).
+ */
+int mquant_step_plan(const int32_t *length_dev, const int32_t *rows_dev, const int32_t *shared_dev, const int32_t *order_dev,
+                     int32_t n_seq, int32_t *page_table_dev, int32_t table_pages, int32_t page_size, int32_t *free_pages_dev,
+                     int32_t n_pages, const int32_t *free_state_dev, int32_t *free_state_out_dev, int32_t *length_out_dev,
+                     int32_t *row_start_dev, int32_t *pos_dev, int64_t *slot_dev, int32_t T, mquant_stream_t stream);
+
+typedef enum {
+    MQUANT_ROTARY_INTERLEAVED = 0,  /* pair j: channels 2j and 2j + 1 */
+    MQUANT_ROTARY_HALVES = 1        /* pair j: channels j and j + rot_dim / 2 */
+} mquant_rotary_layout_t;
+
+typedef enum {
+    MQUANT_ROTARY_NONE = 0,         /* f[j] = base^(-2j/rot_dim) */
+    MQUANT_ROTARY_LINEAR = 1,       /* f[j] / factor: positions as if divided by it */
+    MQUANT_ROTARY_BASE = 2,         /* f[j] of the base base * factor^(rot_dim/(rot_dim - 2)): the slowest pair is stretched by factor, the
+                                       fastest not */
+    MQUANT_ROTARY_TURNS = 3         /* by the turns n = trained_len * f[j] / 2 pi that a pair makes in the trained context:
+                                       f[j] where n >= high_turns, f[j] / factor where n <= low_turns, linear in n between */
+} mquant_rotary_scaling_t;
+
+/* A rotation (host descriptor, read during the call).  The first rot_dim channels of a head are turned in pairs, pair j by the angle
+ * (position on its axis) * freq[j]; cosine and sine are multiplied by `scale`; the other channels stay.  Pairs 0 ..
+ * section[0] - 1 take their positions from axis 0, the next section[1] from axis 1, the next section[2] from axis 2. */
+typedef struct {
+    int32_t layout;                 /* mquant_rotary_layout_t */
+    int32_t rot_dim;                /* a multiple of 16, 16 .. 128 */
+    int32_t n_axes;                 /* 1 .. 3 */
+    int32_t section[3];             /* >= 0; of the first n_axes, the sum is rot_dim / 2 */
+    float scale;                    /* finite */
+    int32_t reserved;               /* 0 */
+    double freq[64];                /* radians a position, rot_dim / 2 of them, finite */
+} mquant_rotary_t;
+
+/*
+ * HOST.  Fills a descriptor: one axis, scale 1, freq by the scaling above.  Axes, sections, scale and single
+ * frequencies may be changed in it afterwards.  base > 1, factor >= 1; trained_len > 0 and high_turns > low_turns are looked at for
+ * MQUANT_ROTARY_TURNS only.  Errors: ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED (rot_dim; rot_dim 16 .. 128 by 16).
+ */
+int mquant_rotary_init(mquant_rotary_t *rot_host, int32_t layout, int32_t rot_dim, double base, int32_t scaling, double factor,
+                       double trained_len, double low_turns, double high_turns);
+
+/*
+ * DEVICE.  mquant_qk_norm_rope with the rotation of a descriptor: norm (u = x where the weight is NULL), then
+ *     y[first] = scale * (u[first] cos a - u[second] sin a),  y[second] = scale * (u[first] sin a + u[second] cos a)
+ * for the pairs, y = u for the channels behind rot_dim; fp32 (angles in double), rounded to fp16 once.
+ *   pos_dev : int32 [n_axes, T], contiguous
+ * Everything else, in-place use and the errors too, as in mquant_qk_norm_rope; ERR_NULL (rot), ERR_BAD_SHAPE (its fields),
+ * ERR_UNSUPPORTED (rot_dim).
+ */
+int mquant_rotary_apply(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ldqo, const void *k_dev, int64_t ldk,
+                        void *k_out_dev, int64_t ldko, const void *q_weight_dev, const void *k_weight_dev, float eps,
+                        const int32_t *pos_dev, int32_t T, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                        const mquant_rotary_t *rot, mquant_stream_t stream);
+
+/*
+ * DEVICE.  mquant_kv_append with the rotation of a descriptor.
+ *   rope_pos_dev : NULL: every axis takes pos; else int32 [n_axes, T], contiguous
+ * Everything else as in mquant_kv_append.
+ */
+int mquant_rotary_append(const void *q_dev, int64_t ldq, void *q_out_dev, int64_t ldqo, const void *k_dev, int64_t ldk,
+                         const void *v_dev, int64_t ldv, const void *q_weight_dev, const void *k_weight_dev, float eps,
+                         const int32_t *row_start_dev, const int32_t *pos_dev, const int32_t *rope_pos_dev, int32_t T,
+                         int32_t n_q_heads, const mquant_rotary_t *rot, const mquant_paged_cache_t *cache, mquant_stream_t stream);
+
+/* Workspace of mquant_paged_attention_shared for the same sizes and bounds; like that of mquant_paged_attention it does not grow
+ * with each size. */
+int64_t mquant_paged_attention_shared_workspace_bytes(int32_t T, int32_t n_seq, int32_t n_groups, int32_t n_q_heads,
+                                                      int32_t n_kv_heads, int32_t head_dim, int32_t max_rows, int32_t max_prefix,
+                                                      int32_t max_suffix);
+
+/*
+ * DEVICE.  mquant_paged_attention where groups of sequences begin with the same tokens (a system prompt, an image, a document):
+ * the sequences group_start[g] .. group_start[g + 1] - 1 have the same keys and values in their slots 0 .. prefix[g] - 1, which
+ * are read once for the rows of all of them, through the page table of the group's first sequence.  The formula, the
+ * roundings and what is said of rows, positions and page ids there hold here too.
+ *   group_start_dev : int32 [n_groups + 1], not decreasing; sequences before group_start[0] or from group_start[n_groups] on
+ *                     share nothing
+ *   prefix_dev      : int32 [n_groups]; 0 and less: nothing shared; more than the table holds: all of it
+ *   max_rows, max_prefix, max_suffix : most rows of a sequence, longest prefix, most slots of a sequence behind its prefix.  They
+ *                     choose how the work is split; data beyond them still get right results.  0: not known (T, the table's slots)
+ *   workspace_dev   : mquant_paged_attention_shared_workspace_bytes(...) bytes, 256-byte aligned; scratch, concurrent calls must
+ *                     not share it
+ * Pages that lie wholly inside a prefix are looked up in the first sequence's table only; where a prefix ends inside a
+ * page, that page is each sequence's own and holds the prefix's last tokens in each.
+ * n_groups may be 0.  Errors: as mquant_paged_attention; ERR_BAD_SHAPE (n_groups < 0), ERR_NULL (the groups' arrays).
+ */
+int mquant_paged_attention_shared(const void *q_dev, int64_t ldq, const mquant_paged_cache_t *cache, const int32_t *row_start_dev,
+                                  const int32_t *pos_dev, const int32_t *group_start_dev, const int32_t *prefix_dev,
+                                  int32_t n_groups, void *o_dev, int64_t ldo, int32_t T, int32_t n_q_heads, int32_t max_rows,
+                                  int32_t max_prefix, int32_t max_suffix, void *workspace_dev, int64_t workspace_bytes,
+                                  mquant_stream_t stream);
+
+typedef enum {
+    MQUANT_F16 = 0,
+    MQUANT_F32 = 1
+} mquant_float_t;
+
+/* Workspace of mquant_sample.  It grows with rows and V: scratch for the largest of each does for any smaller call. */
+int64_t mquant_sample_workspace_bytes(int32_t rows, int32_t V);
+
+/*
+ * DEVICE.  The next token of every row of logits l by the row's settings, from a given random number u.  With m the largest
+ * logit and t the temperature, token i has the weight w[i] = exp((l[i] - m) / t).  Tokens are ranked by their logit, equal ones by
+ * their number (lowest first); kept are
+ *     the first top_k of them (top_k <= 0: all), with the sum M of their weights,
+ *     of these the tokens with less than top_p * M before them in the ranking, the first one always (top_p >= 1: all),
+ *     and of these the tokens with w[i] >= min_p, the first one always (min_p <= 0: all).
+ * With S the kept weights' sum, the token is the first one in the order of the vocabulary up to which the kept weights add to more
+ * than u * S.  Its log-probability is (l - m) / t - ln S.  Temperatures that are not above 0 take the first token of the ranking,
+ * with log-probability 0.
+ * Weights are computed in double and summed as whole multiples of 2^-43, so that results do not depend on how the work is split;
+ * a token with a weight below 2^-44 is never drawn.
+ *   logits_dev      : fp16 or fp32 (type) [rows, V], ld >= V elements apart; aligned to the type.  -inf and NaN are tokens that
+ *                     cannot be chosen; where +inf occurs, only such tokens can.  Up to 15 bytes before and behind a row are
+ *                     read (within the 16-byte blocks that hold it) and not used.
+ *   temperature_dev, top_k_dev, top_p_dev, min_p_dev : fp32, int32, fp32, fp32 [rows]; NULL: 1, 0, 1, 0.  NaN in top_p or min_p: all
+ *   u_dev           : fp32 [rows], in [0, 1): below it or NaN counts as 0, 1 and above as the last kept token
+ *   token_dev       : int32 [rows] (written); -1 where no token can be chosen
+ *   logprob_dev     : NULL, or fp32 [rows] (written); -inf where no token can be chosen
+ *   workspace_dev   : mquant_sample_workspace_bytes(rows, V) bytes, 256-byte aligned; scratch, concurrent calls must not share it
+ * V <= 2^20.  rows == 0 is a no-op.  Errors: ERR_NULL, ERR_BAD_SHAPE (V < 1, ld < V, type), ERR_UNSUPPORTED (V, rows beyond the
+ * grid), ERR_WORKSPACE, ERR_ALIGNMENT.
+ */
+int mquant_sample(const void *logits_dev, int32_t type, int64_t ld, const float *temperature_dev, const int32_t *top_k_dev,
+                  const float *top_p_dev, const float *min_p_dev, const float *u_dev, int32_t *token_dev, float *logprob_dev,
+                  int32_t rows, int32_t V, void *workspace_dev, int64_t workspace_bytes, mquant_stream_t stream);
+
+/* -------------------------------------------------------------------------
  * Tuning hook (tests and tuning runs; not needed for normal use).
  * ---------------------------------------------------------------------- */
 

@@ -627,3 +627,110 @@ def lora_f64(x, perm, adapter, a, b, scale, base) -> np.ndarray:
             h = np.asarray(a[r], dtype=np.float64) @ np.asarray(x[at], dtype=np.float64)
             y[i] += float(scale[r]) * (np.asarray(b[r], dtype=np.float64) @ h)
     return y
+
+
+# --------------------------------------------------------------------------
+# The serving loop: a step's bookkeeping, rotations of a descriptor, the next token
+# --------------------------------------------------------------------------
+
+def step_plan(length, rows, table, page_size: int, ring, state, T: int, shared=None, order=None):
+    """One step's bookkeeping, sequence by sequence and page by page.  table and ring are changed in place; returns
+    (row_start, pos, slots, new length, new state).  A page id that no page has gives slot -1."""
+    n_pages, (n_seq, table_pages) = len(ring), table.shape
+    head, count = int(state[0]) % n_pages, min(max(int(state[1]), 0), n_pages)
+    most = table_pages * page_size
+    length = [min(max(int(n), 0), most) for n in length]
+    own = [max(0, int(shared[s])) if shared is not None else 0 for s in range(n_seq)]
+    pages = lambda n: -(-n // page_size)
+    for s in range(n_seq):
+        if rows[s] < 0:
+            for page in range(own[s], pages(length[s])):
+                if count < n_pages:
+                    ring[(head + count) % n_pages] = table[s, page]
+                    count += 1
+    pos, slots = np.full(T, -1, dtype=np.int32), np.full(T, -1, dtype=np.int64)
+    start, new, room, taken = [0], [], True, 0
+    for s in range(n_seq):
+        r = int(rows[s]) if rows[s] > 0 and length[s] + int(rows[s]) <= most else 0
+        first, last = pages(length[s]), pages(length[s] + r)
+        room = room and start[-1] + r <= T and taken + last - first <= count
+        if not room:
+            r, last = 0, first
+        for page in range(first, last):
+            table[s, page] = ring[(head + taken) % n_pages]
+            taken += 1
+        for j in range(r):
+            i = start[-1] + j
+            o = j if order is None else int(order[i])
+            if 0 <= o < r:
+                pos[i] = length[s] + o
+                at = cache_slot(table, page_size, s, int(pos[i]), n_pages)
+                slots[i] = -1 if at is None else at[0] * page_size + at[1]
+        start.append(start[-1] + r)
+        new.append(0 if rows[s] < 0 else length[s] + r)
+    return (np.array(start, dtype=np.int32), pos, slots, np.array(new, dtype=np.int32),
+            np.array([(head + taken) % n_pages, count - taken], dtype=np.int32))
+
+
+def rotary_frequencies(rot_dim: int, base: float, scaling: str = "none", factor: float = 1.0, trained: float = 0.0, low: float = 1.0,
+                       high: float = 32.0) -> np.ndarray:
+    """Radians a position of every pair: base^(-2j/rot_dim), stretched."""
+    j = np.arange(rot_dim // 2, dtype=np.float64)
+    if scaling == "base":
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = base ** (-2.0 * j / rot_dim)
+    if scaling == "linear":
+        return f / factor
+    if scaling == "turns":
+        keep = np.clip((trained * f / (2 * math.pi) - low) / (high - low), 0.0, 1.0)
+        return f * keep + f / factor * (1.0 - keep)
+    return f
+
+
+def rotary_f64(x, weight, pos, n_heads: int, freq, halves: bool, sections=None, scale: float = 1.0, eps: float = 1e-6) -> np.ndarray:
+    """Norm of every head's channels (skipped where weight is None), then pairs of its first 2 len(freq) channels turned by
+    pos[axis, row] * freq[pair], cosine and sine times scale; the other channels stay.  x is [T, n_heads*D]; fp64."""
+    x = np.asarray(x, dtype=np.float64)
+    T, half = x.shape[0], len(freq)
+    h = x.reshape(T, n_heads, -1).copy()
+    if weight is not None:
+        h = h / np.sqrt((h * h).mean(axis=2, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)
+    pos = np.asarray(pos).reshape(-1, T)
+    axis = np.repeat(np.arange(len(sections)), sections) if sections is not None else np.zeros(half, dtype=int)
+    angle = pos[axis].T.astype(np.float64) * np.asarray(freq)                   # [T, half]
+    c, s = scale * np.cos(angle)[:, None, :], scale * np.sin(angle)[:, None, :]
+    first = np.arange(half) if halves else np.arange(0, 2 * half, 2)
+    second = first + (half if halves else 1)
+    a, b = h[:, :, first].copy(), h[:, :, second].copy()
+    h[:, :, first], h[:, :, second] = a * c - b * s, a * s + b * c
+    return h.reshape(x.shape)
+
+
+def sample_f64(logits, t: float, k: int, p: float, min_p: float, u: float):
+    """The token that a row of logits gives for u, and its log-probability; (-1, -inf) where no token can be chosen."""
+    z = np.asarray(logits, dtype=np.float64) + 0.0
+    z = np.where(np.isnan(z), -np.inf, z)
+    top = z.max(initial=-np.inf)
+    if top == -np.inf:
+        return -1, -np.inf
+    if not t > 0:
+        return int(np.argmax(z)), 0.0
+    if top == np.inf:
+        z, top = np.where(z == np.inf, 0.0, -np.inf), 0.0
+    can = z > -np.inf
+    w = np.where(can, np.exp(np.where(can, z - top, 0.0) / t), 0.0)
+    ranked = np.argsort(-z, kind="stable")[:int(can.sum())]
+    if k > 0:
+        ranked = ranked[:k]
+    if p < 1:
+        before = np.cumsum(w[ranked]) - w[ranked]
+        ranked = ranked[:max(1, int((before < p * w[ranked].sum()).sum()))]
+    if min_p > 0:
+        ranked = ranked[:max(1, int((w[ranked] >= min_p).sum()))]
+    kept = np.sort(ranked)
+    mass = np.cumsum(w[kept])
+    u = u if u > 0 else 0.0
+    at = min(int(np.searchsorted(mass, u * mass[-1], side="right")), len(kept) - 1)
+    while w[kept[at]] == 0.0:
+        at -= 1
+    return int(kept[at]), float((z[kept[at]] - top) / t - math.log(mass[-1]))

@@ -42,6 +42,8 @@ EXPORTS = (
     "mquant_w4g128_prepacked_bytes", "mquant_w4g128_prepack", "mquant_w4g128_gemm",
     "mquant_qk_norm_rope", "mquant_kv_append", "mquant_paged_attention_workspace_bytes", "mquant_paged_attention",
     "mquant_lora_workspace_bytes", "mquant_lora_apply",
+    "mquant_step_plan", "mquant_rotary_init", "mquant_rotary_apply", "mquant_rotary_append",
+    "mquant_paged_attention_shared_workspace_bytes", "mquant_paged_attention_shared", "mquant_sample_workspace_bytes", "mquant_sample",
 )
 
 OK, ERR_NULL, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_ALIGNMENT = 0, -1, -2, -3, -4, -5, -6
@@ -61,6 +63,11 @@ class PagedCacheStruct(ctypes.Structure):
     _fields_ = [("k_pages_dev", ctypes.c_void_p), ("v_pages_dev", ctypes.c_void_p), ("page_table_dev", ctypes.c_void_p),
                 ("n_seq", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("table_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class RotaryStruct(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("section", ctypes.c_int32 * 3),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("freq", ctypes.c_double * 64)]
 
 
 class Linear(ctypes.Structure):
@@ -124,10 +131,21 @@ def _load() -> ctypes.CDLL:
     lib.mquant_lora_workspace_bytes.restype = i64
     lib.mquant_lora_workspace_bytes.argtypes = [i32, i32, i32]
     lib.mquant_lora_apply.argtypes = [p, i64, p, p, p, p, p, p, i64, p, i64, i32, i32, i32, i32, i32, p, i64, p]
+    lib.mquant_step_plan.argtypes = [p, p, p, p, i32, p, i32, i32, p, i32, p, p, p, p, p, p, i32, p]
+    lib.mquant_rotary_init.argtypes = [p, i32, i32, f64, i32, f64, f64, f64, f64]
+    lib.mquant_rotary_apply.argtypes = [p, i64, p, i64, p, i64, p, i64, p, p, f32, p, i32, i32, i32, i32, p, p]
+    lib.mquant_rotary_append.argtypes = [p, i64, p, i64, p, i64, p, i64, p, p, f32, p, p, p, i32, i32, p, p, p]
+    lib.mquant_paged_attention_shared_workspace_bytes.restype = i64
+    lib.mquant_paged_attention_shared_workspace_bytes.argtypes = [i32] * 9
+    lib.mquant_paged_attention_shared.argtypes = [p, i64, p, p, p, p, p, i32, p, i64, i32, i32, i32, i32, i32, p, i64, p]
+    lib.mquant_sample_workspace_bytes.restype = i64
+    lib.mquant_sample_workspace_bytes.argtypes = [i32, i32]
+    lib.mquant_sample.argtypes = [p, i32, i64, p, p, p, p, p, p, p, i32, i32, p, i64, p]
     for name in EXPORTS:
         if name not in ("mquant_status_string", "mquant_w4_prepacked_bytes", "mquant_aifs_attention_workspace_bytes",
                         "mquant_build_id", "mquant_w4g128_prepacked_bytes",
                         "mquant_paged_attention_workspace_bytes", "mquant_lora_workspace_bytes",
+                        "mquant_paged_attention_shared_workspace_bytes", "mquant_sample_workspace_bytes",
                         "mquant_w4a8_workspace_bytes", "mquant_w4a8_linear_prefill_workspace_bytes",
                         "mquant_version"):
             getattr(lib, name).restype = ctypes.c_int
@@ -755,3 +773,170 @@ def lora_apply(x, adapter_dev, a, b, scale, base, perm_dev=None, out=None, works
                                  _dp(out), ldy, T, N, K, rank, n_adapters, _dp(workspace), ws_bytes, _stream()),
            "mquant_lora_apply")
     return out
+
+
+# ----------------------------------------------------------- serving loop
+
+class Rotary:
+    """A rotation (mquant_rotary_t): the first rot_dim channels of a head in interleaved pairs or in halves, pairs by `sections`
+    on one to three axes of positions, frequencies of `base` by `scaling` ("none", "linear", "base", "turns") or given in
+    `freq` (radians a position), cosine and sine times `scale`."""
+    SCALINGS = {"none": 0, "linear": 1, "base": 2, "turns": 3}
+
+    def __init__(self, rot_dim: int = 128, base: float = 10000.0, halves: bool = False, sections: Optional[Sequence[int]] = None,
+                 scaling: str = "none", factor: float = 1.0, trained: float = 0.0, low: float = 1.0, high: float = 32.0,
+                 scale: float = 1.0, freq: Optional[Sequence[float]] = None):
+        if scaling not in self.SCALINGS:
+            raise MQuantError(ERR_BAD_SHAPE, f"Rotary: scaling {scaling!r} is none of {tuple(self.SCALINGS)}")
+        self.struct = RotaryStruct()
+        self.address = ctypes.addressof(self.struct)
+        _check(lib.mquant_rotary_init(self.address, 1 if halves else 0, rot_dim, base, self.SCALINGS[scaling], factor, trained, low, high),
+               "mquant_rotary_init")
+        if sections is not None:
+            if not 1 <= len(sections) <= 3:
+                raise MQuantError(ERR_BAD_SHAPE, f"Rotary: sections {tuple(sections)}: one to three axes")
+            self.struct.n_axes = len(sections)
+            for i, n in enumerate(sections):
+                self.struct.section[i] = n
+        if freq is not None:
+            if len(freq) != rot_dim // 2:
+                raise MQuantError(ERR_BAD_SHAPE, f"Rotary: {len(freq)} frequencies for {rot_dim // 2} pairs")
+            for i, f in enumerate(freq):
+                self.struct.freq[i] = f
+        self.struct.scale = scale
+        self.n_axes = self.struct.n_axes
+        self.fast = (self.address, self.n_axes)
+
+
+def _axes(pos, rot: Rotary, T: int, what: str) -> None:
+    """Positions of a rotation: [T] of a single axis, [axes, T] of any number."""
+    _operand(pos, torch.int32, what, (T,) if rot.n_axes == 1 and pos.dim() == 1 else (rot.n_axes, T))
+
+
+def rotary_apply(q, k, pos_dev, rot: Rotary, n_q_heads: int, n_kv_heads: int, q_weight=None, k_weight=None, head_dim: int = 128,
+                 eps: float = 1e-6, q_out=None, k_out=None):
+    """q [T, >= Hq*D], k [T, >= Hkv*D] fp16 views, pos [axes, T] (or [T]) -> (q_out, k_out); q_out=q, k_out=k work in place."""
+    T = q.shape[0]
+    if q_out is None:
+        q_out = torch.empty((T, n_q_heads * head_dim), dtype=torch.float16, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((T, n_kv_heads * head_dim), dtype=torch.float16, device=q.device)
+    lds = [_heads(t, n, head_dim, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
+                                                               (k, n_kv_heads, "k"), (k_out, n_kv_heads, "k_out"))]
+    _weight(q_weight, head_dim, "q_weight"), _weight(k_weight, head_dim, "k_weight"), _axes(pos_dev, rot, T, "pos")
+    _check(lib.mquant_rotary_apply(_dp(q), lds[0], _dp(q_out), lds[1], _dp(k), lds[2], _dp(k_out), lds[3], _dp(q_weight),
+                                   _dp(k_weight), eps, _dp(pos_dev), T, n_q_heads, n_kv_heads, head_dim, rot.address, _stream()),
+           "mquant_rotary_apply")
+    return q_out, k_out
+
+
+def rotary_append(q, k, v, cache: PagedCache, row_start_dev, pos_dev, rot: Rotary, n_q_heads: int, q_weight=None, k_weight=None,
+                  eps: float = 1e-6, rope_pos_dev=None, q_out=None):
+    """kv_append with the rotation `rot`; rope_pos [axes, T] (or [T]), None: every axis takes pos -> q_out."""
+    T, D = q.shape[0], cache.head_dim
+    if q_out is None:
+        q_out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
+    lds = [_heads(t, n, D, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
+                                                        (k, cache.n_kv_heads, "k"), (v, cache.n_kv_heads, "v"))]
+    _weight(q_weight, D, "q_weight"), _weight(k_weight, D, "k_weight")
+    _step(cache, row_start_dev, pos_dev, T)
+    if rope_pos_dev is not None:
+        _axes(rope_pos_dev, rot, T, "rope_pos")
+    _check(lib.mquant_rotary_append(_dp(q), lds[0], _dp(q_out), lds[1], _dp(k), lds[2], _dp(v), lds[3], _dp(q_weight), _dp(k_weight),
+                                    eps, _dp(row_start_dev), _dp(pos_dev), _dp(rope_pos_dev), T, n_q_heads, rot.address,
+                                    cache.address, _stream()), "mquant_rotary_append")
+    return q_out
+
+
+def step_plan(length, rows, page_table, page_size: int, free_pages, free_state, T: int, shared_dev=None, order_dev=None,
+              length_out=None, state_out=None, row_start=None, pos=None, slots=None):
+    """The bookkeeping of a step of up to T rows; page_table, free_pages and the outputs are written, length_out=length and
+    state_out=free_state work in place -> (row_start, pos, slots)."""
+    n_seq, dev = rows.shape[0], rows.device
+    new = lambda t, *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device=dev) if t is None else t
+    length_out, state_out = new(length_out, n_seq), new(state_out, 2)
+    row_start, pos, slots = new(row_start, n_seq + 1), new(pos, T), new(slots, T, dtype=torch.int64)
+    for t, what in ((length, "length"), (rows, "rows"), (length_out, "length_out")):
+        _operand(t, torch.int32, what, (n_seq,))
+    _operand(row_start, torch.int32, "row_start", (n_seq + 1,)), _operand(pos, torch.int32, "pos", (T,))
+    _operand(slots, torch.int64, "slots", (T,))
+    if page_table.dim() != 2 or page_table.shape[0] != n_seq:
+        raise MQuantError(ERR_BAD_SHAPE, f"page_table: expected [{n_seq}, pages], got {tuple(page_table.shape)}")
+    _operand(page_table, torch.int32, "page_table", tuple(page_table.shape)), _operand(free_pages, torch.int32, "free_pages", (free_pages.numel(),))
+    _operand(free_state, torch.int32, "free_state", (2,)), _operand(state_out, torch.int32, "state_out", (2,))
+    if shared_dev is not None:
+        _operand(shared_dev, torch.int32, "shared", (n_seq,))
+    if order_dev is not None:
+        _operand(order_dev, torch.int32, "order", (T,))
+    _check(lib.mquant_step_plan(_dp(length), _dp(rows), _dp(shared_dev), _dp(order_dev), n_seq, _dp(page_table), page_table.shape[1],
+                                page_size, _dp(free_pages), free_pages.numel(), _dp(free_state), _dp(state_out), _dp(length_out),
+                                _dp(row_start), _dp(pos), _dp(slots), T, _stream()), "mquant_step_plan")
+    return row_start, pos, slots
+
+
+def paged_attention_shared_workspace_bytes(T: int, cache: PagedCache, n_groups: int, n_q_heads: int, max_rows: int = 0,
+                                           max_prefix: int = 0, max_suffix: int = 0) -> int:
+    bound = lambda n: min(n, cache.slots) if n else cache.slots
+    n = int(lib.mquant_paged_attention_shared_workspace_bytes(T, cache.n_seq, n_groups, n_q_heads, cache.n_kv_heads, cache.head_dim,
+                                                              max_rows, bound(max_prefix), bound(max_suffix)))
+    if n < 0:
+        raise MQuantError(n, "mquant_paged_attention_shared_workspace_bytes")
+    return n
+
+
+def paged_attention_shared(q, cache: PagedCache, row_start_dev, pos_dev, group_start_dev, prefix_dev, n_q_heads: int, max_rows: int = 0,
+                           max_prefix: int = 0, max_suffix: int = 0, out=None, workspace=None):
+    """paged_attention where the sequences group_start[g] .. group_start[g + 1] - 1 share their first prefix[g] slots, which are read
+    once; max_rows, max_prefix, max_suffix: host bounds (0: not known) -> o [T, Hq*D]."""
+    T, D, n_groups = q.shape[0], cache.head_dim, prefix_dev.shape[0]
+    max_prefix, max_suffix = min(max_prefix, cache.slots), min(max_suffix, cache.slots)
+    if out is None:
+        out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(256, paged_attention_shared_workspace_bytes(T, cache, n_groups, n_q_heads, max_rows, max_prefix,
+                                                                                max_suffix)), dtype=torch.uint8, device=q.device)
+    ws_bytes = workspace.numel() * workspace.element_size()
+    ldq, ldo = _heads(q, n_q_heads, D, T, "q"), _heads(out, n_q_heads, D, T, "out")
+    _step(cache, row_start_dev, pos_dev, T), _workspace(workspace)
+    _operand(group_start_dev, torch.int32, "group_start", (n_groups + 1,)), _operand(prefix_dev, torch.int32, "prefix", (n_groups,))
+    _check(lib.mquant_paged_attention_shared(_dp(q), ldq, cache.address, _dp(row_start_dev), _dp(pos_dev), _dp(group_start_dev),
+                                             _dp(prefix_dev), n_groups, _dp(out), ldo, T, n_q_heads, max_rows, max_prefix, max_suffix,
+                                             _dp(workspace), ws_bytes, _stream()), "mquant_paged_attention_shared")
+    return out
+
+
+F16, F32 = 0, 1
+_FLOATS = {torch.float16: F16, torch.float32: F32}
+
+
+def sample_workspace_bytes(rows: int, V: int) -> int:
+    n = int(lib.mquant_sample_workspace_bytes(rows, V))
+    if n < 0:
+        raise MQuantError(n, "mquant_sample_workspace_bytes")
+    return n
+
+
+def sample(logits, temperature, top_k, top_p, min_p, u, out=None, logprob=None, workspace=None):
+    """The next token of every row of logits [rows, V] (fp16 or fp32) from random numbers u [rows]; temperature, top_k, top_p and
+    min_p [rows], None: 1, all, 1, 0 -> (tokens int32 [rows], their log-probabilities fp32 [rows])."""
+    if logits.dtype not in _FLOATS:
+        raise MQuantError(ERR_UNSUPPORTED, f"logits: expected float16 or float32, got {logits.dtype}")
+    ld = _operand(logits, logits.dtype, "logits")
+    rows, V = logits.shape
+    if out is None:
+        out = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    if logprob is None:
+        logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    need = sample_workspace_bytes(rows, V)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    for t, dtype, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
+                           (min_p, torch.float32, "min_p"), (u, torch.float32, "u"), (out, torch.int32, "out"),
+                           (logprob, torch.float32, "logprob")):
+        if t is not None:
+            _operand(t, dtype, what, (rows,))
+    _workspace(workspace)
+    _check(lib.mquant_sample(_dp(logits), _FLOATS[logits.dtype], max(ld, V), _dp(temperature), _dp(top_k), _dp(top_p), _dp(min_p), _dp(u),
+                             _dp(out), _dp(logprob), rows, V, _dp(workspace), ws_bytes, _stream()), "mquant_sample")
+    return out, logprob

@@ -18,7 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libmquant.so")
 SOURCES = ["aifs.hip", "hadamard_quant.hip", "w4a8_gemm.hip", "w4a8_gemv.hip", "w4a8_sliced.hip", "w4a8_wide.hip", "w4a8_small.hip", "w4a8_walk.hip", "attention.hip",
-           "w4g128_gemm.hip", "w4g128_walk.hip", "qk_norm.hip", "paged_attention.hip", "lora.hip"]
+           "w4g128_gemm.hip", "w4g128_walk.hip", "qk_norm.hip", "paged_attention.hip", "lora.hip", "step_plan.hip", "sample.hip"]
 # The benchmark's measurement probes: their own shared object, outside the product's ABI.
 PROBES_LIB = os.path.join(LIB_DIR, "libmquant_probes.so")
 PROBES_SOURCES = ["probes.hip"]

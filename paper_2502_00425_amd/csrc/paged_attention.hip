@@ -9,6 +9,10 @@
 //   paged_chunk_kernel  the others: 128 queries a work-group, 64 slots a tile, bound by the matrix cores.
 // Both split the slots of a sequence into pieces where there are too few work-groups otherwise; the pieces' partial
 // results (unnormalised sums, maximum, denominator, fp32) meet in paged_combine_kernel.
+//
+// Sequences that begin with the same tokens (mquant_paged_attention_shared) are walked by the same kernels in two parts: the rows of a group lie
+// behind one another, so its shared slots are those of one sequence with all the group's rows (Part::kPrefix), read once for
+// them; the slots behind the prefix are walked sequence by sequence (Part::kSuffix).  All pieces of both parts meet in shared_combine_kernel.
 #include <climits>
 #include <cmath>
 
@@ -48,6 +52,14 @@ constexpr int kAhead = 4;                  // LDS fragment reads in flight ahead
 // factor matters), under one of the maxima's own they would be up to 2^(1/8) apart.  No product is contracted into an addition here (-ffp-contract=off).
 constexpr float kLazy = 8.0f;
 
+enum class Part { kAll, kPrefix, kSuffix };
+
+// Pieces of a part in a call with shared prefixes: at most `split` of them, `piece` slots each, for sequences of few queries and for the others.
+struct Pieces {
+    int32_t few_split, few_piece, chunk_split, chunk_piece;
+    int32_t few_alone, chunk_alone;        // one kernel takes all of them, whatever their rows
+};
+
 struct Step {
     const __half *q;
     int64_t ldq, ldo;
@@ -62,6 +74,11 @@ struct Step {
     int32_t all;                           // this kernel takes every sequence, whatever its rows
     float *part;
     float2 *part_ml;
+    // shared prefixes: the groups, and the pieces of both parts: all of the prefix's ahead of the suffix's, by (piece, row, head)
+    const int32_t *group_start, *prefix;
+    int32_t n_groups;
+    int32_t first_piece;                   // of the part that a kernel walks
+    Pieces in_prefix, in_suffix;
 };
 
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -74,10 +91,26 @@ __device__ __forceinline__ void wait_copies()
     asm volatile("" ::: "memory");
 }
 
-// Rows of a sequence: first and behind the last, inside [0, T).
+// What a kernel walks one after another: sequences, or groups of them.
+template <Part P>
+__device__ __forceinline__ int32_t walked(const Step &a)
+{
+    return P == Part::kPrefix ? a.n_groups : a.c.n_seq;
+}
+
+// First sequence of group g (n_groups: behind the last group), inside [0, n_seq].
+__device__ __forceinline__ int32_t group_begin(const Step &a, int32_t g)
+{
+    const int32_t s = a.group_start[g];
+    return s < 0 ? 0 : s < a.c.n_seq ? s : a.c.n_seq;
+}
+
+// Rows of a sequence or group: first and behind the last, inside [0, T).
+template <Part P = Part::kAll>
 __device__ __forceinline__ int2 rows_of(const Step &a, int32_t seq)
 {
-    const int32_t b = a.row_start[seq], e = a.row_start[seq + 1];
+    const int32_t s0 = P == Part::kPrefix ? group_begin(a, seq) : seq, s1 = P == Part::kPrefix ? group_begin(a, seq + 1) : seq + 1;
+    const int32_t b = a.row_start[s0], e = a.row_start[s1];
     return make_int2(b > 0 ? b : 0, e < a.T ? e : a.T);
 }
 
@@ -88,13 +121,48 @@ __device__ __forceinline__ int32_t limit_of(const Step &a, int32_t row)
     return p < 0 ? -1 : p < last ? p : last;
 }
 
+// Slots that group g shares, inside the table; of no group (-1): none.
+__device__ __forceinline__ int32_t prefix_of(const Step &a, int32_t g)
+{
+    if (g < 0) return 0;
+    const int32_t p = a.prefix[g], most = a.c.table_pages << a.c.page_shift;
+    return p < 0 ? 0 : p < most ? p : most;
+}
+
+// What a part has to know of a sequence or group beside its rows.
+struct Place {
+    int32_t table = 0;                     // whose line of the table has its pages ..
+    int32_t prefix = 0;                    // .. kPrefix: slots to walk; kSuffix: slots ahead of those to walk
+    int32_t front = 0, front_table = 0;    // kSuffix: whole pages of the prefix, and whose line has them
+};
+
+template <Part P>
+__device__ __forceinline__ Place place_of(const Step &a, int32_t seq)
+{
+    Place at;
+    at.table = seq;
+    if constexpr (P == Part::kPrefix) {
+        at.table = group_begin(a, seq);
+        at.prefix = prefix_of(a, seq);
+    }
+    if constexpr (P == Part::kSuffix) {
+        const int32_t g = a.n_groups > 0 ? uniform(sequence_of_row(a.group_start, a.n_groups, seq)) : -1;
+        at.prefix = prefix_of(a, g);
+        at.front = at.prefix >> a.c.page_shift;
+        at.front_table = g < 0 ? seq : group_begin(a, g);
+    }
+    return at;
+}
+
 // The 16 slots block * 16 .. of a sequence, as the number of 4 KiB blocks before them in a page array.  A block behind the table
 // repeats its last one, a page id out of range is page 0: any block is memory of the cache, and what a row does not see
 // is not used.
-__device__ __forceinline__ uint32_t block_at(const Step &a, int32_t seq, int32_t kvh, int32_t block)
+template <Part P>
+__device__ __forceinline__ uint32_t block_at(const Step &a, const Place &place, int32_t kvh, int32_t block)
 {
     const int32_t shift = a.c.page_shift - 4, last = (a.c.table_pages << shift) - 1, b = block < last ? block : last;
-    const int32_t id = a.c.table[static_cast<int64_t>(seq) * a.c.table_pages + (b >> shift)];
+    const int32_t line = P == Part::kSuffix && (b >> shift) < place.front ? place.front_table : place.table;
+    const int32_t id = a.c.table[static_cast<int64_t>(line) * a.c.table_pages + (b >> shift)];
     const uint32_t page = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.c.n_pages) ? id : 0;
     return (page * static_cast<uint32_t>(a.c.n_kv_heads) + kvh) * (1u << shift) + (b & ((1 << shift) - 1));
 }
@@ -109,6 +177,16 @@ __device__ __forceinline__ int32_t pieces_of(const Step &a, int32_t limit)
     if (limit < 0) return 0;
     const int32_t n = limit / a.piece + 1;
     return n < a.n_split ? n : a.n_split;
+}
+
+// Last slot of a part that a row sees, of the part's own slots; -1: none.
+template <Part P>
+__device__ __forceinline__ int32_t limit_in(const Step &a, const Place &place, int32_t row)
+{
+    const int32_t limit = limit_of(a, row);
+    if constexpr (P == Part::kPrefix) return limit < place.prefix ? limit : place.prefix - 1;
+    if constexpr (P == Part::kSuffix) return limit < place.prefix ? -1 : limit;
+    return limit;
 }
 
 // ------------------------------------------------------------------------------------------------ few queries
@@ -126,20 +204,22 @@ __device__ __forceinline__ int32_t pieces_of(const Step &a, int32_t limit)
 // NQ: 16 queries each, all of them computed, whatever a sequence has: skipping by branches those behind the last query cost the
 // others the overlap of their products and exponentials (20.4 against 17.7 us at 8 sequences of 5 rows x 28 heads over 4096 slots), and
 // a form for each number beside one another gave nothing (32 sequences of one row among one of 512, 8000 slots each: 194 and 193 us).
-template <int NQ>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
+template <int NQ, Part P>
+__device__ __forceinline__ void walk_few(const Step &a, int32_t block)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = uniform(tid >> 6);
-    const int32_t units = a.c.n_seq * a.c.n_kv_heads;
-    const int32_t unit = blockIdx.x % units, piece = blockIdx.x / units;
+    const int32_t units = walked<P>(a) * a.c.n_kv_heads;
+    const int32_t unit = block % units, piece = block / units;
     const int32_t seq = unit / a.c.n_kv_heads, kvh = unit % a.c.n_kv_heads;
-    const int2 rows = rows_of(a, seq);
+    const int2 rows = rows_of<P>(a, seq);
     if (rows.x >= rows.y) return;
     const int32_t M = (rows.y - rows.x) * a.group;
     if (!a.all && M > kFew) return;
 
+    const Place place = place_of<P>(a, seq);
+    const int32_t front = P == Part::kSuffix ? place.prefix & ~(kFewSlots - 1) : 0;        // where the part's slots begin, in whole tiles
     const uint32_t k_lds = lds_address(smem) + wave * (2 * kFewSlots * 256), v_lds = k_lds + kFewSlots * 256;
     uint32_t k_off[4], v_off[4];                               // where a lane reads in a block of 16 rows
 #pragma unroll
@@ -150,13 +230,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
     }
     for (int32_t m0 = 0; m0 < M; m0 += 16 * NQ) {
         const int nq = M - m0 < 16 * NQ ? (M - m0 + 15) / 16 : NQ;
-        const bool split = m0 + 16 * NQ <= a.few_stride;       // the others' slots are all in piece 0
+        const bool split = P != Part::kAll || m0 + 16 * NQ <= a.few_stride;    // the others' slots are all in piece 0
         if (!split && piece > 0) return;
         // page ids, queries and positions are on their way together
-        const int32_t begin = split ? piece * a.piece : 0;     // slots, a multiple of kFewStep
+        const int32_t begin = front + (split ? piece * a.piece : 0);           // slots, a multiple of kFewStep behind the front
         const int32_t first = begin / kFewSlots + wave;
         // lane 2 i + b: block b of this wave's tile i; 32 tiles (4096 slots of the work-group) a time
-        auto blocks_from = [&](int32_t tile0) { return block_at(a, seq, kvh, (tile0 + (lane >> 1) * kFewWaves) * 2 + (lane & 1)); };
+        auto blocks_from = [&](int32_t tile0) { return block_at<P>(a, place, kvh, (tile0 + (lane >> 1) * kFewWaves) * 2 + (lane & 1)); };
         uint32_t blocks = blocks_from(first);
         v8h qf[NQ][4];
         int32_t lim[NQ], top = -1, low = INT_MAX;
@@ -167,7 +247,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
             const __half *qp = a.q + row * a.ldq + static_cast<int64_t>(kvh * a.group + mc % a.group) * kD + g * 8;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) qf[u][ks] = *reinterpret_cast<const v8h *>(qp + ks * 32);
-            lim[u] = limit_of(a, row);
+            lim[u] = limit_in<P>(a, place, row);
         }
 #pragma unroll
         for (int u = 0; u < NQ; ++u) {
@@ -237,6 +317,14 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
                                 if (kb * 16 + r > room) s[kb][r] = -INFINITY;
+                    }
+                    if (P == Part::kSuffix && slot0 < place.prefix) {          // slots of the prefix in the first tile
+                        const int32_t skip = place.prefix - slot0 - 4 * g;
+#pragma unroll
+                        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (kb * 16 + r < skip) s[kb][r] = -INFINITY;
                     }
                     float m = m_ref[u];
 #pragma unroll
@@ -333,7 +421,14 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
                     for (int e = 0; e < 8; ++e) f[e] += share * sums[(w * 16 + qi) * kFewPitch + ch + e];
                 }
                 const int32_t row = rows.x + m / a.group, limit = lims[qi];
-                if (!split || pieces_of(a, limit) <= 1) {
+                if constexpr (P != Part::kAll) {
+                    if (limit >= begin) {                      // -1: nothing of this part is seen
+                        const int64_t at = (static_cast<int64_t>(a.first_piece + piece) * a.T + row) * a.n_q + kvh * a.group + m % a.group;
+                        *reinterpret_cast<v4f *>(a.part + at * kD + ch) = v4f{f[0], f[1], f[2], f[3]};
+                        *reinterpret_cast<v4f *>(a.part + at * kD + ch + 4) = v4f{f[4], f[5], f[6], f[7]};
+                        if (ch == 0) a.part_ml[at] = make_float2(top_m, den);
+                    }
+                } else if (!split || pieces_of(a, limit) <= 1) {
                     if (piece == 0) {
                         const float inv = den > 0.0f ? 1.0f / den : 0.0f;       // a row that sees nothing: zeros
                         __half *out = a.o + row * a.ldo + static_cast<int64_t>(kvh * a.group + m % a.group) * kD + ch;
@@ -353,6 +448,18 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
         }
         __syncthreads();
     }
+}
+
+template <int NQ>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
+{
+    walk_few<NQ, Part::kAll>(a, blockIdx.x);
+}
+
+template <int NQ, bool PREFIX>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void shared_few_kernel(Step a)
+{
+    walk_few<NQ, PREFIX ? Part::kPrefix : Part::kSuffix>(a, blockIdx.x);
 }
 
 // ------------------------------------------------------------------------------------------------ chunks
@@ -377,8 +484,8 @@ __device__ __forceinline__ void halves_of(float x, float &lo, float &hi)
 // MFMA 32x32 result register r of lane group g holds row (r/4)*8 + g*4 + r%4.
 __device__ __forceinline__ int acc_row(int r, int g) { return (r >> 2) * 8 + g * 4 + (r & 3); }
 
-template <int KG>
-__global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_t xcds_per_kv)
+template <int KG, Part P>
+__device__ __forceinline__ void walk_chunk(const Step &a, int32_t block, int32_t xcds_per_kv)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];           // KG * kChunkLds
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
@@ -387,12 +494,12 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     // evenly, so that an L2 fetches the tiles its work-groups walk together once.
     int32_t kvh, item;
     if (xcds_per_kv > 0) {
-        const int32_t xcd = blockIdx.x % 8;
+        const int32_t xcd = block % 8;
         kvh = xcd / xcds_per_kv;
-        item = static_cast<int32_t>(blockIdx.x / 8) * xcds_per_kv + xcd % xcds_per_kv;
+        item = block / 8 * xcds_per_kv + xcd % xcds_per_kv;
     } else {
-        kvh = blockIdx.x % a.c.n_kv_heads;
-        item = blockIdx.x / a.c.n_kv_heads;
+        kvh = block % a.c.n_kv_heads;
+        item = block / a.c.n_kv_heads;
     }
     // Query tiles are dealt from the last of a sequence to the first (the later ones see more slots), up to 64 sequences in order of
     // length, so that long work-groups start first.  Where all work-groups are on the chip at once, two to a compute unit, the second half
@@ -402,23 +509,24 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     int32_t left = item / a.n_split;
     int32_t seq = -1, tile = 0;
     int2 rows = make_int2(0, 0);
-    for (int32_t at = 0; at < a.c.n_seq; at += 64) {
-        int32_t s = a.c.n_seq - 1 - at - lane;
+    const int32_t n_walked = walked<P>(a);
+    for (int32_t at = 0; at < n_walked; at += 64) {
+        int32_t s = n_walked - 1 - at - lane;
         int32_t tiles = 0, length = -1;
         int2 r = make_int2(0, 0);
         if (s >= 0) {
-            r = rows_of(a, s);
+            r = rows_of<P>(a, s);
             const int32_t M = r.y > r.x ? (r.y - r.x) * a.group : 0;
             tiles = a.all || M > kFew ? (M + kChunkQ - 1) / kChunkQ : 0;
         }
-        if (a.c.n_seq > 1 && a.c.n_seq <= 64) {
+        if (n_walked > 1 && n_walked <= 64) {
             if (tiles > 0) length = limit_of(a, r.y - 1);
             int32_t rank = 0;
-            for (int32_t j = 0; j < a.c.n_seq; ++j) {
+            for (int32_t j = 0; j < n_walked; ++j) {
                 const int32_t other = __builtin_amdgcn_readlane(length, j);
                 rank += other > length || (other == length && j < lane) ? 1 : 0;
             }
-            if (lane >= a.c.n_seq) rank = lane;                // behind all sequences: where it is
+            if (lane >= n_walked) rank = lane;                // behind all sequences: where it is
             s = __builtin_amdgcn_ds_permute(rank * 4, s);
             tiles = __builtin_amdgcn_ds_permute(rank * 4, tiles);
         }
@@ -429,7 +537,7 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
             if (lane >= x) sum += o;
         }
         const int32_t total = __builtin_amdgcn_readlane(sum, 63);
-        if (KG == 1 && a.c.n_seq <= 64 && a.n_split == 1 && total <= 2 * kNumCU / a.c.n_kv_heads) {
+        if (KG == 1 && n_walked <= 64 && a.n_split == 1 && total <= 2 * kNumCU / a.c.n_kv_heads) {
             const int32_t half = kNumCU / a.c.n_kv_heads;
             if (left >= half && left < total) left = total - 1 - (left - half);
         }
@@ -438,19 +546,20 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
             const int who = __builtin_ctzll(behind);
             seq = __builtin_amdgcn_readlane(s, who);
             tile = __builtin_amdgcn_readlane(sum, who) - 1 - left;
-            const int from = a.c.n_seq - 1 - at - seq;         // the lane that looked at it
+            const int from = n_walked - 1 - at - seq;         // the lane that looked at it
             rows = make_int2(__builtin_amdgcn_readlane(r.x, from), __builtin_amdgcn_readlane(r.y, from));
             break;
         }
         left -= total;
     }
     if (seq < 0) return;
+    const Place place = place_of<P>(a, seq);
     const int32_t M = (rows.y - rows.x) * a.group;
 
     // ---- this lane's query: the slots it sees, Q^T fragments; page ids are on their way with them
     const int32_t m = tile * kChunkQ + wave * 32 + l32, mc = m < M ? m : M - 1;
     const int32_t row = rows.x + mc / a.group, head = kvh * a.group + mc % a.group;
-    const int32_t limit = limit_of(a, row);
+    const int32_t limit = limit_in<P>(a, place, row);
     v8h qf[kD / 16];
     {
         const __half *qp = a.q + row * a.ldq + static_cast<int64_t>(head) * kD + g * 8;
@@ -459,10 +568,10 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     }
     // Key group kg takes the tiles t0 + kg, t0 + kg + KG, ...: tile i of its own.  The groups do the same number of steps: the last tile
     // of one may lie behind the piece, and nothing of it is visible then.
-    const int32_t piece_tiles = a.piece / kChunkK, t0 = piece * piece_tiles;
+    const int32_t piece_tiles = a.piece / kChunkK, t0 = piece * piece_tiles + (P == Part::kSuffix ? place.prefix / kChunkK : 0);
     auto tile_of = [&](int32_t i) { return t0 + kg + KG * i; };
     // lane l: block l % 4 of tile 16 j + l / 4, for the keys' tile and for the values', and the next 16 tiles on their way
-    auto blocks_from = [&](int32_t i) { return block_at(a, seq, kvh, tile_of(i + (lane >> 2)) * 4 + (lane & 3)); };
+    auto blocks_from = [&](int32_t i) { return block_at<P>(a, place, kvh, tile_of(i + (lane >> 2)) * 4 + (lane & 3)); };
     uint32_t k_blocks = blocks_from(0), v_blocks = k_blocks, n_blocks = blocks_from(16);
 
     int32_t top, low = row16_min(limit);
@@ -583,6 +692,15 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
                 for (int r = 0; r < 16; ++r)
                     if (kb * 32 + acc_row(r, 0) > room) s_cur[kb][r] = -INFINITY;
         }
+        if (P == Part::kSuffix && t * kChunkK < place.prefix) { // slots of the prefix in the first tile
+            int32_t skip = place.prefix - t * kChunkK - 4 * g;
+            asm volatile("" : "+v"(skip));
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (kb * 32 + acc_row(r, 0) < skip) s_cur[kb][r] = -INFINITY;
+        }
         float m_new = m_ref;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -683,9 +801,9 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     const float ref = m_ref * scale_log2e;
 
     // ---- lane = query, registers = head channels (4 consecutive per group)
-    const bool partial = a.n_split > 1;
+    const bool partial = P != Part::kAll || a.n_split > 1;
     const bool write = m < M && (!partial || limit >= t0 * kChunkK);
-    const int64_t at = (static_cast<int64_t>(piece) * a.T + row) * a.n_q + head;
+    const int64_t at = (static_cast<int64_t>((P != Part::kAll ? a.first_piece : 0) + piece) * a.T + row) * a.n_q + head;
     __half *out = a.o + row * a.ldo + static_cast<int64_t>(head) * kD;
     auto store4 = [&](int dt, int r4, const v4f &f, float inv_l) {
         if (partial) {
@@ -748,6 +866,18 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
         }
         if (partial && kg == 0 && g == 0) a.part_ml[at] = make_float2(top_m, l_all);
     }
+}
+
+template <int KG>
+__global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_t xcds_per_kv)
+{
+    walk_chunk<KG, Part::kAll>(a, blockIdx.x, xcds_per_kv);
+}
+
+template <int KG, bool PREFIX>
+__global__ __launch_bounds__(KG * 256, 2) void shared_chunk_kernel(Step a, int32_t xcds_per_kv)
+{
+    walk_chunk<KG, PREFIX ? Part::kPrefix : Part::kSuffix>(a, blockIdx.x, xcds_per_kv);
 }
 
 // ------------------------------------------------------------------------------------------------ pieces
@@ -844,6 +974,82 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
     reinterpret_cast<uint2 *>(out)[1] = reinterpret_cast<const uint2 *>(h)[1];
 }
 
+// The same where groups share a prefix: the pieces of the prefix that a row sees, then those of its sequence's own slots.  A row that sees
+// nothing gets zeros.
+__global__ __launch_bounds__(256) void shared_combine_kernel(Step a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + uniform(threadIdx.x >> 6);
+    const int32_t row = static_cast<int32_t>(item / a.n_q), head = static_cast<int32_t>(item % a.n_q);
+    if (row >= a.T) return;
+    const int32_t limit = limit_of(a, row);
+    const int32_t seq = uniform(sequence_of_row(a.row_start, a.c.n_seq, row));
+    if (seq < 0) return;
+    const int32_t g = a.n_groups > 0 ? uniform(sequence_of_row(a.group_start, a.n_groups, seq)) : -1;
+    const int32_t prefix = prefix_of(a, g);
+    // pieces of n slots, as the kernel that took these queries cut them
+    auto pieces = [&](const Pieces &by, const int2 &rows, int32_t n, bool suffix) {
+        const bool few = by.few_alone || (!by.chunk_alone && (rows.y - rows.x) * a.group <= kFew);
+        if (n <= 0) return 0;
+        if (suffix) n += prefix % (few ? kFewSlots : kChunkK);
+        const int32_t k = (n - 1) / (few ? by.few_piece : by.chunk_piece) + 1, most = few ? by.few_split : by.chunk_split;
+        return k < most ? k : most;
+    };
+    int32_t n_pre = 0;
+    if (g >= 0 && prefix > 0) n_pre = pieces(a.in_prefix, rows_of<Part::kPrefix>(a, g), limit < prefix ? limit + 1 : prefix, false);
+    const int32_t n = n_pre + pieces(a.in_suffix, rows_of(a, seq), limit + 1 - prefix, true);
+    const int ch = (lane & 15) * 8, quarter = lane >> 4;
+    const int64_t stride = static_cast<int64_t>(a.T) * a.n_q;
+    float top = -INFINITY, den = 0.0f, f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int kAtOnce = 4;
+    for (int32_t p0 = 0; p0 < n; p0 += 4 * kAtOnce) {
+        v4f v[kAtOnce][2];
+        float2 ml[kAtOnce];
+        float top_p = top;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int32_t p = p0 + i * 4 + quarter, pc = p < n ? p : n - 1;
+            const int64_t from = item + (pc < n_pre ? pc : a.first_piece + pc - n_pre) * stride;
+            ml[i] = a.part_ml[from];
+            v[i][0] = *reinterpret_cast<const v4f *>(a.part + from * kD + ch);
+            v[i][1] = *reinterpret_cast<const v4f *>(a.part + from * kD + ch + 4);
+            if (p >= n) ml[i].x = -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) top_p = fmaxf(top_p, ml[i].x);
+        top_p = fmaxf(top_p, __shfl_xor(top_p, 16, 64));
+        top_p = fmaxf(top_p, __shfl_xor(top_p, 32, 64));
+        const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - top_p);
+        top = top_p;
+        den *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= keep;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (ml[i].x == -INFINITY) continue;
+            const float share = __builtin_amdgcn_exp2f(ml[i].x - top);
+            den = __builtin_fmaf(share, ml[i].y, den);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(share, v[i][e >> 2][e & 3], f[e]);
+        }
+    }
+    den += __shfl_xor(den, 16, 64);
+    den += __shfl_xor(den, 32, 64);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f[e] += __shfl_xor(f[e], 16, 64);
+        f[e] += __shfl_xor(f[e], 32, 64);
+    }
+    if (quarter != 0) return;
+    const float inv = den > 0.0f ? 1.0f / den : 0.0f;
+    __half h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = __float2half_rn(f[e] * inv);
+    __half *out = a.o + row * a.ldo + static_cast<int64_t>(head) * kD + ch;
+    reinterpret_cast<uint2 *>(out)[0] = reinterpret_cast<const uint2 *>(h)[0];
+    reinterpret_cast<uint2 *>(out)[1] = reinterpret_cast<const uint2 *>(h)[1];
+}
+
 // ------------------------------------------------------------------------------------------------ dispatch
 
 int check_sizes(int32_t T, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows, int32_t max_kv)
@@ -870,15 +1076,10 @@ struct Plan {
     }
 };
 
-Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_rows, int32_t max_kv)
+// Pieces for the kernels that p names: T rows of n_seq sequences of at most `most` rows and max_kv slots each.
+void plan_pieces(Plan &p, int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int64_t most, int32_t max_kv)
 {
-    Plan p;
-    if (T == 0 || n_seq == 0) return p;
     const int32_t G = n_q / n_kv;
-    const int64_t most = max_rows > 0 && max_rows < T ? max_rows : T;          // rows of a sequence
-    const int64_t least = T - (n_seq - 1) * most;                              // where no row is outside the sequences
-    p.chunk = most * G > kFew;
-    p.few = !p.chunk || least * G <= kFew;
     const int64_t units = static_cast<int64_t>(n_seq) * n_kv, kv = max_kv > 0 ? max_kv : 1;
     if (p.few) {
         const int64_t m = most * G < kFew ? most * G : kFew;
@@ -927,7 +1128,131 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
         p.chunk_two = groups * p.chunk_split <= kNumCU;
         if (p.chunk_split > 1) p.chunk_part = static_cast<int64_t>(T) * n_q * p.chunk_split;
     }
+}
+
+Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_rows, int32_t max_kv)
+{
+    Plan p;
+    if (T == 0 || n_seq == 0) return p;
+    const int32_t G = n_q / n_kv;
+    const int64_t most = max_rows > 0 && max_rows < T ? max_rows : T;          // rows of a sequence
+    const int64_t least = T - (n_seq - 1) * most;                              // where no row is outside the sequences
+    p.chunk = most * G > kFew;
+    p.few = !p.chunk || least * G <= kFew;
+    plan_pieces(p, T, n_seq, n_q, n_kv, most, max_kv);
     return p;
+}
+
+// What a call with shared prefixes launches.
+struct SharedPlan {
+    Plan pre, suf;
+    int32_t pre_split = 0, suf_split = 0;  // pieces a query has room for
+    int64_t parts = 0;                     // partial results
+    int64_t bytes() const { return parts == 0 ? 0 : ceil_div(parts * kD * 4, 256) * 256 + ceil_div(parts * 8, 256) * 256; }
+};
+
+int32_t split_of(const Plan &p)
+{
+    const int32_t few = p.few ? p.few_split : 0, chunk = p.chunk ? p.chunk_split : 0;
+    return few > chunk ? few : chunk;
+}
+
+Pieces pieces_by(const Plan &p) { return {p.few_split, p.few_piece, p.chunk_split, p.chunk_piece, p.few && !p.chunk, p.chunk && !p.few}; }
+
+SharedPlan make_shared_plan(int32_t T, int32_t n_seq, int32_t n_groups, int32_t n_q, int32_t n_kv, int32_t max_rows, int32_t max_prefix,
+                            int32_t max_suffix)
+{
+    SharedPlan p;
+    if (T == 0 || n_seq == 0) return p;
+    if (n_groups > 0) {
+        // one kernel for all groups, by the rows that they have on average
+        p.pre.chunk = ceil_div(T, n_groups) * (n_q / n_kv) > kFew;
+        p.pre.few = !p.pre.chunk;
+        plan_pieces(p.pre, T, n_groups, n_q, n_kv, T, max_prefix);
+        p.pre_split = split_of(p.pre);
+    }
+    p.suf = make_plan(T, n_seq, n_q, n_kv, max_rows, max_suffix);
+    p.suf_split = split_of(p.suf);
+    p.parts = static_cast<int64_t>(T) * n_q * (p.pre_split + p.suf_split);
+    return p;
+}
+
+template <int KG, Part P>
+auto chunk_kernel()
+{
+    if constexpr (P == Part::kAll) return &paged_chunk_kernel<KG>;
+    else return &shared_chunk_kernel<KG, P == Part::kPrefix>;
+}
+
+template <int NQ, Part P>
+auto few_kernel()
+{
+    if constexpr (P == Part::kAll) return &paged_few_kernel<NQ>;
+    else return &shared_few_kernel<NQ, P == Part::kPrefix>;
+}
+
+template <Part P>
+int launch_chunk(Step a, const Plan &p, hipStream_t stream)
+{
+    a.n_split = p.chunk_split;
+    a.piece = p.chunk_piece;
+    a.all = !p.few;
+    const int32_t n_kv = a.c.n_kv_heads, xcds_per_kv = 8 % n_kv == 0 ? 8 / n_kv : 0;
+    const int64_t items = static_cast<int64_t>(p.chunk_tiles) * p.chunk_split;
+    const int64_t groups = xcds_per_kv > 0 ? 8 * ceil_div(items, xcds_per_kv) : items * n_kv;
+    const int key_groups = p.chunk_two ? 2 : 1;
+    if (groups * key_groups * 256 > kMaxThreads) return MQUANT_ERR_UNSUPPORTED;
+    auto kern = p.chunk_two ? chunk_kernel<2, P>() : chunk_kernel<1, P>();
+    static LdsLimit limits[2];
+    if (const int st = limits[p.chunk_two].raise(reinterpret_cast<const void *>(kern), key_groups * kChunkLds); st != MQUANT_OK) return st;
+    MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(key_groups * 256), key_groups * kChunkLds, stream, a, xcds_per_kv);
+    return launch_status();
+}
+
+template <Part P>
+int launch_few(Step a, const Plan &p, int64_t walked, hipStream_t stream)
+{
+    a.n_split = p.few_split;
+    a.piece = p.few_piece;
+    a.all = !p.chunk;
+    const int64_t groups = walked * a.c.n_kv_heads * p.few_split;
+    auto kern = p.few_nq == 1 ? few_kernel<1, P>() : p.few_nq == 2 ? few_kernel<2, P>() : few_kernel<3, P>();
+    static LdsLimit limits[3];
+    if (const int st = limits[p.few_nq - 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
+    MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(kFewWaves * 64), kFewLds, stream, a);
+    return launch_status();
+}
+
+int check_rows(const void *q, int64_t ldq, const void *o, int64_t ldo, const int32_t *row_start, const int32_t *pos, int32_t n_q_heads)
+{
+    if (!q || !o || !row_start || !pos) return MQUANT_ERR_NULL;
+    const int64_t w = static_cast<int64_t>(n_q_heads) * kD;
+    if (ldq < w || ldo < w) return MQUANT_ERR_BAD_SHAPE;
+    if (ldq % 8 != 0 || ldo % 4 != 0 || !aligned_to(q, 16) || !aligned_to(o, 8) || !aligned_to(pos, 4) || !aligned_to(row_start, 4))
+        return MQUANT_ERR_ALIGNMENT;
+    return MQUANT_OK;
+}
+
+Step step_of(const void *q, int64_t ldq, const mquant_paged_cache_t *cache, const int32_t *row_start, const int32_t *pos, void *o,
+             int64_t ldo, int32_t T, int32_t n_q_heads, void *workspace, int64_t parts)
+{
+    Step a = {};
+    a.q = static_cast<const __half *>(q);
+    a.ldq = ldq;
+    a.ldo = ldo;
+    a.o = static_cast<__half *>(o);
+    a.row_start = row_start;
+    a.pos = pos;
+    a.T = T;
+    a.n_q = n_q_heads;
+    a.group = n_q_heads / cache->n_kv_heads;
+    a.scale_log2e = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(kD)));
+    a.c = cache_args(cache);
+    a.n_split = 1;
+    a.piece = 1 << 30;
+    a.part = static_cast<float *>(workspace);
+    a.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + ceil_div(parts * kD * 4, 256) * 256);
+    return a;
 }
 
 }  // namespace
@@ -947,11 +1272,7 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
     if (const int st = check_sizes(T, cache->n_seq, n_q_heads, cache->n_kv_heads, cache->head_dim, max_rows, max_kv); st != MQUANT_OK)
         return st;
     if (T == 0 || cache->n_seq == 0) return MQUANT_OK;
-    if (!q || !o || !row_start || !pos) return MQUANT_ERR_NULL;
-    const int64_t w = static_cast<int64_t>(n_q_heads) * kD;
-    if (ldq < w || ldo < w) return MQUANT_ERR_BAD_SHAPE;
-    if (ldq % 8 != 0 || ldo % 4 != 0 || !aligned_to(q, 16) || !aligned_to(o, 8) || !aligned_to(pos, 4) || !aligned_to(row_start, 4))
-        return MQUANT_ERR_ALIGNMENT;
+    if (const int st = check_rows(q, ldq, o, ldo, row_start, pos, n_q_heads); st != MQUANT_OK) return st;
     const int32_t n_kv = cache->n_kv_heads;
     const int32_t slots = cache->table_pages * cache->page_size;
     Plan p = make_plan(T, cache->n_seq, n_q_heads, n_kv, max_rows, max_kv > 0 && max_kv < slots ? max_kv : slots);
@@ -962,46 +1283,82 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
     if (need > 0 && !aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
-    Step a = {static_cast<const __half *>(q), ldq, ldo, static_cast<__half *>(o), row_start, pos, T, n_q_heads, n_q_heads / n_kv,
-              static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(kD))), cache_args(cache), 1, 1 << 30, p.few_stride, 0,
-              static_cast<float *>(workspace),
-              reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + ceil_div((p.few_part + p.chunk_part) * kD * 4, 256) * 256)};
+    Step a = step_of(q, ldq, cache, row_start, pos, o, ldo, T, n_q_heads, workspace, p.few_part + p.chunk_part);
+    a.few_stride = p.few_stride;
     if (p.chunk) {
-        a.n_split = p.chunk_split;
-        a.piece = p.chunk_piece;
-        a.all = !p.few;
-        const int32_t xcds_per_kv = 8 % n_kv == 0 ? 8 / n_kv : 0;
-        const int64_t items = static_cast<int64_t>(p.chunk_tiles) * p.chunk_split;
-        const int64_t groups = xcds_per_kv > 0 ? 8 * ceil_div(items, xcds_per_kv) : items * n_kv;
-        const int key_groups = p.chunk_two ? 2 : 1;
-        if (groups * key_groups * 256 > kMaxThreads) return MQUANT_ERR_UNSUPPORTED;
-        auto kern = p.chunk_two ? paged_chunk_kernel<2> : paged_chunk_kernel<1>;
-        static LdsLimit limits[2];
-        if (const int st = limits[p.chunk_two].raise(reinterpret_cast<const void *>(kern), key_groups * kChunkLds); st != MQUANT_OK) return st;
-        MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(key_groups * 256), key_groups * kChunkLds, stream, a, xcds_per_kv);
-        if (const int st = launch_status(); st != MQUANT_OK) return st;
+        if (const int st = launch_chunk<Part::kAll>(a, p, stream); st != MQUANT_OK) return st;
         if (p.chunk_split > 1) {
+            a.n_split = p.chunk_split;
+            a.piece = p.chunk_piece;
+            a.all = !p.few;
             MQ_LAUNCH(paged_combine_kernel<true>, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * n_q_heads, 4))), dim3(256), 0,
                       stream, a);
             if (const int st = launch_status(); st != MQUANT_OK) return st;
         }
     }
     if (p.few) {
-        a.n_split = p.few_split;
-        a.piece = p.few_piece;
-        a.all = !p.chunk;
         a.part += p.chunk_part * kD;
         a.part_ml += p.chunk_part;
-        const int64_t units = static_cast<int64_t>(cache->n_seq) * n_kv, groups = units * p.few_split;
-        auto kern = p.few_nq == 1 ? paged_few_kernel<1> : p.few_nq == 2 ? paged_few_kernel<2> : paged_few_kernel<3>;
-        static LdsLimit limits[3];
-        if (const int st = limits[p.few_nq - 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
-        MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(kFewWaves * 64), kFewLds, stream, a);
-        if (const int st = launch_status(); st != MQUANT_OK) return st;
+        if (const int st = launch_few<Part::kAll>(a, p, cache->n_seq, stream); st != MQUANT_OK) return st;
         if (p.few_split > 1) {
-            MQ_LAUNCH(paged_combine_kernel<false>, dim3(static_cast<unsigned>(ceil_div(units * p.few_stride, 4))), dim3(256), 0, stream, a);
+            a.n_split = p.few_split;
+            a.piece = p.few_piece;
+            a.all = !p.chunk;
+            const int64_t queries = static_cast<int64_t>(cache->n_seq) * n_kv * p.few_stride;
+            MQ_LAUNCH(paged_combine_kernel<false>, dim3(static_cast<unsigned>(ceil_div(queries, 4))), dim3(256), 0, stream, a);
             return launch_status();
         }
     }
     return MQUANT_OK;
+}
+
+extern "C" int64_t mquant_paged_attention_shared_workspace_bytes(int32_t T, int32_t n_seq, int32_t n_groups, int32_t n_q_heads,
+                                                                 int32_t n_kv_heads, int32_t head_dim, int32_t max_rows,
+                                                                 int32_t max_prefix, int32_t max_suffix)
+{
+    if (const int st = check_sizes(T, n_seq, n_q_heads, n_kv_heads, head_dim, max_rows, max_suffix); st != MQUANT_OK) return st;
+    if (const int st = check_sizes(T, n_groups, n_q_heads, n_kv_heads, head_dim, max_rows, max_prefix); st != MQUANT_OK) return st;
+    return make_shared_plan(T, n_seq, n_groups, n_q_heads, n_kv_heads, max_rows, max_prefix, max_suffix).bytes();
+}
+
+extern "C" int mquant_paged_attention_shared(const void *q, int64_t ldq, const mquant_paged_cache_t *cache, const int32_t *row_start,
+                                             const int32_t *pos, const int32_t *group_start, const int32_t *prefix, int32_t n_groups,
+                                             void *o, int64_t ldo, int32_t T, int32_t n_q_heads, int32_t max_rows, int32_t max_prefix,
+                                             int32_t max_suffix, void *workspace, int64_t workspace_bytes, mquant_stream_t stream_)
+{
+    if (const int st = check_cache(cache); st != MQUANT_OK) return st;
+    const int32_t n_kv = cache->n_kv_heads;
+    if (const int st = check_sizes(T, cache->n_seq, n_q_heads, n_kv, cache->head_dim, max_rows, max_suffix); st != MQUANT_OK) return st;
+    if (const int st = check_sizes(T, n_groups, n_q_heads, n_kv, cache->head_dim, max_rows, max_prefix); st != MQUANT_OK) return st;
+    if (T == 0 || cache->n_seq == 0) return MQUANT_OK;
+    if (const int st = check_rows(q, ldq, o, ldo, row_start, pos, n_q_heads); st != MQUANT_OK) return st;
+    if (n_groups > 0 && (!group_start || !prefix)) return MQUANT_ERR_NULL;
+    if (n_groups > 0 && (!aligned_to(group_start, 4) || !aligned_to(prefix, 4))) return MQUANT_ERR_ALIGNMENT;
+    const int32_t slots = cache->table_pages * cache->page_size;
+    auto in_table = [&](int32_t bound) { return bound > 0 && bound < slots ? bound : slots; };
+    SharedPlan p = make_shared_plan(T, cache->n_seq, n_groups, n_q_heads, n_kv, max_rows, in_table(max_prefix), in_table(max_suffix));
+    // scratch that was asked for with bounds beyond the table may be another size: then those bounds' pieces are taken
+    if ((max_prefix > slots || max_suffix > slots) && workspace_bytes < p.bytes())
+        p = make_shared_plan(T, cache->n_seq, n_groups, n_q_heads, n_kv, max_rows, max_prefix > 0 ? max_prefix : slots,
+                             max_suffix > 0 ? max_suffix : slots);
+    const int64_t need = p.bytes();
+    if (!workspace || workspace_bytes < need) return MQUANT_ERR_WORKSPACE;
+    if (!aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
+    hipStream_t stream = static_cast<hipStream_t>(stream_);
+
+    Step a = step_of(q, ldq, cache, row_start, pos, o, ldo, T, n_q_heads, workspace, p.parts);
+    a.group_start = group_start;
+    a.prefix = prefix;
+    a.n_groups = n_groups;
+    a.in_prefix = pieces_by(p.pre);
+    a.in_suffix = pieces_by(p.suf);
+    int st = MQUANT_OK;
+    if (p.pre.chunk) st = launch_chunk<Part::kPrefix>(a, p.pre, stream);
+    if (p.pre.few) st = launch_few<Part::kPrefix>(a, p.pre, n_groups, stream);
+    a.first_piece = p.pre_split;
+    if (st == MQUANT_OK && p.suf.chunk) st = launch_chunk<Part::kSuffix>(a, p.suf, stream);
+    if (st == MQUANT_OK && p.suf.few) st = launch_few<Part::kSuffix>(a, p.suf, cache->n_seq, stream);
+    if (st != MQUANT_OK) return st;
+    MQ_LAUNCH(shared_combine_kernel, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * n_q_heads, 4))), dim3(256), 0, stream, a);
+    return launch_status();
 }

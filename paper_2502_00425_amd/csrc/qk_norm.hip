@@ -1,5 +1,6 @@
 // Norms of queries and keys per head with the rotary embedding, and with the write of keys and values to
-// their pages, in one pass, for gfx950.
+// their pages, in one pass, for gfx950: qk_norm_rope_kernel for whole heads in interleaved pairs, rotary_kernel for the rotation
+// of a descriptor (either channel order, part of a head, positions on up to three axes, given frequencies).
 //
 // For a head x of 128 channels and position p:
 //   u = x * w * (sum(x^2) / 128 + eps)^(-1/2)     (no weight: u = x)
@@ -125,6 +126,132 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(Rows a, PagedCache c,
     }
 }
 
+// The rotation of a descriptor.  Pair j takes the position of its axis and the frequency that the host gives in turns a position;
+// lane l forms the angle of pair l for the whole wave, as above.
+struct Turn {
+    double turns[kD / 2];
+    int32_t axis1, axis2, half_lanes;      // first pairs of axis 1 and 2; lanes of 8 channels in half of those that are turned
+    float scale;
+};
+
+// Channels 8 l .. 8 l + 7 of a head are in lane l of its 16.  In interleaved order a lane holds four whole pairs.  In halves the
+// partner of a channel is half_lanes further or back: the lane gets the partner's eight channels as they came, and their weights with
+// them, and works out its own eight results.  WHOLE: all 128 channels are turned, the partner's lane is 8 away.
+// A wave's rows, heads and stores as in qk_norm_rope_kernel.
+template <bool APPEND, bool HALVES, bool WHOLE, int U>
+__global__ __launch_bounds__(256) void rotary_kernel(Rows a, PagedCache c, Turn turn, int32_t waves, int32_t per)
+{
+    constexpr int kPairs = HALVES ? 8 : 4;                     // angles a lane works with
+    const int lane = threadIdx.x & 63, l16 = lane & 15;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t i = static_cast<int32_t>(item / waves);
+    if (i >= a.T) return;
+    const int32_t part = static_cast<int32_t>(item % waves);
+    const int32_t first = part * per * 4 + (lane >> 4), all = a.n_q + a.n_k * (APPEND ? 2 : 1);
+    const int32_t heads = all < (part + 1) * per * 4 ? all : (part + 1) * per * 4;         // this wave's end
+    const int ch = l16 * 8;
+    const int32_t p = APPEND ? a.pos[i] : 0;
+    const int32_t axis = lane >= turn.axis2 ? 2 : lane >= turn.axis1 ? 1 : 0;
+    const int32_t angle_pos = !APPEND || a.rope_pos ? a.rope_pos[static_cast<int64_t>(axis) * a.T + i] : p;
+    v8h x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t h = first + u * 4;
+        const __half *row = h < a.n_q ? a.q + i * a.ldq + static_cast<int64_t>(h) * kD
+                            : h < a.n_q + a.n_k ? a.k + i * a.ldk + static_cast<int64_t>(h - a.n_q) * kD
+                                                : a.v + i * a.ldv + static_cast<int64_t>(h - a.n_q - a.n_k) * kD;
+        x[u] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
+        if (h < heads) x[u] = *reinterpret_cast<const v8h *>(row + ch);
+    }
+    const int32_t seq = APPEND ? sequence_of_row(a.row_start, c.n_seq, i) : 0;
+    if (seq < 0) return;
+    int64_t slot = -1;                                          // halves from a page array's start to head 0's row
+    int32_t head_stride = 0;
+    if constexpr (APPEND) {
+        head_stride = kD << c.page_shift;
+        const int32_t page_at = p >> c.page_shift;
+        if (p >= 0 && page_at < c.table_pages) {
+            const int32_t page = c.table[static_cast<int64_t>(seq) * c.table_pages + page_at];
+            if (page >= 0 && page < c.n_pages)
+                slot = page * c.page_halves + static_cast<int64_t>(p & ((1 << c.page_shift) - 1)) * kD;
+        }
+    }
+    const double turns = static_cast<double>(angle_pos) * turn.turns[lane];
+    float sn, cs, co[kPairs], si[kPairs];
+    sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
+    sn *= turn.scale;
+    cs *= turn.scale;
+    // this lane's pairs, and in halves its partner and the sign of the partner's share
+    const int half = WHOLE ? 8 : turn.half_lanes;
+    const bool second = HALVES && l16 >= half;
+    const bool turned = WHOLE || l16 < 2 * half;
+    const int partner = HALVES && turned ? (second ? lane - half : lane + half) : lane;
+    const int pair0 = !turned ? 0 : HALVES ? (second ? l16 - half : l16) * 8 : l16 * 4;
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) {
+        co[e] = __shfl(cs, pair0 + e, 64);
+        si[e] = __shfl(sn, pair0 + e, 64);
+        if (second) si[e] = -si[e];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t h = first + u * 4;
+        if (U > 1 && u >= per) break;
+        const bool is_q = h < a.n_q && h < heads, is_v = APPEND && h >= a.n_q + a.n_k;
+        const __half *w = is_q ? a.q_weight : a.k_weight;
+        const bool normed = w && h < heads && !is_v;
+        float f[8], sum = 0.0f, r = 1.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f[e] = static_cast<float>(x[u][e]);
+            sum = __builtin_fmaf(f[e], f[e], sum);
+        }
+        sum = row16_sum(sum);
+        if (normed) {
+            r = 1.0f / sqrtf(sum * (1.0f / kD) + a.eps);
+            const v8h wt = *reinterpret_cast<const v8h *>(w + ch);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] *= r * static_cast<float>(wt[e]);
+        }
+        v8h y;
+        if constexpr (HALVES) {
+            union {
+                v8h h8;
+                int32_t w4[4];
+            } mine, other;
+            mine.h8 = x[u];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                other.w4[e] = WHOLE ? __builtin_amdgcn_update_dpp(mine.w4[e], mine.w4[e], 0x128, 0xf, 0xf, false)
+                                    : __builtin_amdgcn_ds_bpermute(partner * 4, mine.w4[e]);
+            float g[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = static_cast<float>(other.h8[e]);
+            if (normed) {
+                const v8h wt = *reinterpret_cast<const v8h *>(w + (partner & 15) * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] *= r * static_cast<float>(wt[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = static_cast<_Float16>(turned ? f[e] * co[e] - g[e] * si[e] : f[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[2 * e] = static_cast<_Float16>(turned ? f[2 * e] * co[e] - f[2 * e + 1] * si[e] : f[2 * e]);
+                y[2 * e + 1] = static_cast<_Float16>(turned ? f[2 * e] * si[e] + f[2 * e + 1] * co[e] : f[2 * e + 1]);
+            }
+        }
+        if (is_q) {
+            put<(U > 1)>(a.q_out + i * a.ldqo + static_cast<int64_t>(h) * kD + ch, y);
+        } else if (!APPEND) {
+            if (h < heads) put<(U > 1)>(a.k_out + i * a.ldko + static_cast<int64_t>(h - a.n_q) * kD + ch, y);
+        } else if (h < heads && slot >= 0) {
+            if (is_v) put<(U > 1)>(c.v + slot + static_cast<int64_t>(h - a.n_q - a.n_k) * head_stride + ch, x[u]);
+            else put<(U > 1)>(c.k + slot + static_cast<int64_t>(h - a.n_q) * head_stride + ch, y);
+        }
+    }
+}
+
 int check_side(const void *x, int64_t ldx, const void *out, int64_t ldo, int32_t T, int32_t heads)
 {
     if (heads == 0) return MQUANT_OK;
@@ -136,11 +263,53 @@ int check_side(const void *x, int64_t ldx, const void *out, int64_t ldo, int32_t
     return MQUANT_OK;
 }
 
-int check_norm(const void *q_weight, const void *k_weight, float eps, double base)
+int check_norm(const void *q_weight, const void *k_weight, float eps, double base = 1e4)
 {
     if (!(eps >= 0.0f) || !std::isfinite(eps) || !(base > 1.0) || !std::isfinite(base)) return MQUANT_ERR_BAD_SHAPE;
     if (!aligned_to(q_weight, 16) || !aligned_to(k_weight, 16)) return MQUANT_ERR_ALIGNMENT;
     return MQUANT_OK;
+}
+
+// Pointers and strides of an append, checked, as the kernels take them.
+int append_rows(const void *q, int64_t ldq, void *q_out, int64_t ldqo, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                const void *q_weight, const void *k_weight, float eps, const int32_t *row_start, const int32_t *pos,
+                const int32_t *rope_pos, int32_t T, int32_t n_q_heads, const mquant_paged_cache_t *cache, Rows &a)
+{
+    if (!row_start || !pos) return MQUANT_ERR_NULL;
+    if (!aligned_to(row_start, 4) || !aligned_to(pos, 4) || !aligned_to(rope_pos, 4)) return MQUANT_ERR_ALIGNMENT;
+    if (const int st = check_side(q, ldq, q_out, ldqo, T, n_q_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(k, ldk, cache->k_pages_dev, ldk, T, cache->n_kv_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(v, ldv, cache->v_pages_dev, ldv, T, cache->n_kv_heads); st != MQUANT_OK) return st;
+    a = {static_cast<const __half *>(q), static_cast<const __half *>(k), static_cast<const __half *>(v),
+         static_cast<__half *>(q_out), nullptr, ldq, ldqo, ldk, 0, ldv, static_cast<const __half *>(q_weight),
+         static_cast<const __half *>(k_weight), pos, rope_pos, row_start, eps, T, n_q_heads, cache->n_kv_heads};
+    return MQUANT_OK;
+}
+
+// How rows and heads are dealt to waves.
+struct Grid {
+    dim3 grid;
+    int32_t waves, per;                    // waves of a row, groups of four heads a wave
+    bool few;
+};
+
+// A wave takes four heads where rows are few, since what such a launch waits for is the way of one wave, else up to 16.  Waves of 4 /
+// of up to 16 heads, 32 heads: 512 rows 4.1 / 4.7 us, 700 5.0 / 5.0, 1024 5.8 / 5.3, 4096 15.0 / 11.6; 72 heads: 256 4.4 / 5.0, 512 6.2 / 6.0.
+// (Up to 12 heads at 72 of 16384 rows 102.4 us, 16 101.1: 6.0 TB/s, 20 103.6, 40 107.3; 32 of 4096 12.8, 11.6, 12.3, 12.2.)
+constexpr int kGroups = 4;
+
+bool grid_of(int64_t heads, int32_t T, Grid &g)
+{
+    const int64_t groups = ceil_div(heads, 4);
+    int64_t waves = ceil_div(groups, kGroups);
+    g.few = T * groups < 6000;
+    if (g.few) waves = groups;
+    const int64_t blocks = ceil_div(T * waves, 4);
+    if (blocks > kMaxThreads / 256 || heads > 1 << 20) return false;
+    g.grid = dim3(static_cast<unsigned>(blocks));
+    g.per = static_cast<int32_t>(ceil_div(groups, waves));
+    g.waves = static_cast<int32_t>(waves);
+    return true;
 }
 
 template <bool APPEND>
@@ -152,20 +321,57 @@ int launch(const Rows &a, const PagedCache &c, double base, hipStream_t stream)
     const long double ratio = powl(static_cast<long double>(base), -2.0L / kD);
     long double f = 0.159154943091895335768883763372514362L;
     for (int j = 0; j < kD / 2; ++j, f *= ratio) inv.f[j] = static_cast<double>(f);
-    // A wave takes four heads where rows are few, since what such a launch waits for is the way of one wave, else up to 16.  Waves of 4 /
-    // of up to 16 heads, 32 heads: 512 rows 4.1 / 4.7 us, 700 5.0 / 5.0, 1024 5.8 / 5.3, 4096 15.0 / 11.6; 72 heads: 256 4.4 / 5.0, 512 6.2 / 6.0.
-    // (Up to 12 heads at 72 of 16384 rows 102.4 us, 16 101.1: 6.0 TB/s, 20 103.6, 40 107.3; 32 of 4096 12.8, 11.6, 12.3, 12.2.)
-    constexpr int U = 4;
-    const int64_t groups = ceil_div(heads, 4);
-    int64_t waves = ceil_div(groups, U);
-    const bool few = a.T * groups < 6000;
-    if (few) waves = groups;
-    const int64_t blocks = ceil_div(a.T * waves, 4);
-    if (blocks > kMaxThreads / 256 || heads > 1 << 20) return MQUANT_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(blocks));
-    const int32_t per = static_cast<int32_t>(ceil_div(groups, waves)), n = static_cast<int32_t>(waves);
-    if (few) MQ_LAUNCH((qk_norm_rope_kernel<APPEND, 1>), grid, dim3(256), 0, stream, a, c, inv, n, per);
-    else MQ_LAUNCH((qk_norm_rope_kernel<APPEND, U>), grid, dim3(256), 0, stream, a, c, inv, n, per);
+    Grid g;
+    if (!grid_of(heads, a.T, g)) return MQUANT_ERR_UNSUPPORTED;
+    if (g.few) MQ_LAUNCH((qk_norm_rope_kernel<APPEND, 1>), g.grid, dim3(256), 0, stream, a, c, inv, g.waves, g.per);
+    else MQ_LAUNCH((qk_norm_rope_kernel<APPEND, kGroups>), g.grid, dim3(256), 0, stream, a, c, inv, g.waves, g.per);
+    return launch_status();
+}
+
+int check_rotary(const mquant_rotary_t *rot)
+{
+    if (!rot) return MQUANT_ERR_NULL;
+    if (rot->rot_dim < 16 || rot->rot_dim > kD || rot->rot_dim % 16 != 0) return MQUANT_ERR_UNSUPPORTED;
+    if (rot->layout != MQUANT_ROTARY_INTERLEAVED && rot->layout != MQUANT_ROTARY_HALVES) return MQUANT_ERR_BAD_SHAPE;
+    if (rot->n_axes < 1 || rot->n_axes > 3 || !std::isfinite(rot->scale)) return MQUANT_ERR_BAD_SHAPE;
+    int64_t pairs = 0;
+    for (int i = 0; i < rot->n_axes; ++i) {
+        if (rot->section[i] < 0) return MQUANT_ERR_BAD_SHAPE;
+        pairs += rot->section[i];
+    }
+    if (pairs != rot->rot_dim / 2) return MQUANT_ERR_BAD_SHAPE;
+    for (int j = 0; j < rot->rot_dim / 2; ++j)
+        if (!std::isfinite(rot->freq[j])) return MQUANT_ERR_BAD_SHAPE;
+    return MQUANT_OK;
+}
+
+template <bool APPEND, bool HALVES, bool WHOLE>
+void launch_rotary(const Grid &g, const Rows &a, const PagedCache &c, const Turn &turn, hipStream_t stream)
+{
+    if (g.few) MQ_LAUNCH((rotary_kernel<APPEND, HALVES, WHOLE, 1>), g.grid, dim3(256), 0, stream, a, c, turn, g.waves, g.per);
+    else MQ_LAUNCH((rotary_kernel<APPEND, HALVES, WHOLE, kGroups>), g.grid, dim3(256), 0, stream, a, c, turn, g.waves, g.per);
+}
+
+template <bool APPEND>
+int launch(const Rows &a, const PagedCache &c, const mquant_rotary_t &rot, hipStream_t stream)
+{
+    Grid g;
+    if (!grid_of(a.n_q + static_cast<int64_t>(a.n_k) * (APPEND ? 2 : 1), a.T, g)) return MQUANT_ERR_UNSUPPORTED;
+    Turn turn = {};
+    constexpr double kTurnsOfRadian = 0.15915494309189533577;
+    for (int j = 0; j < rot.rot_dim / 2; ++j) turn.turns[j] = rot.freq[j] * kTurnsOfRadian;
+    turn.axis1 = rot.n_axes > 1 ? rot.section[0] : kD;         // behind the last pair: no such axis
+    turn.axis2 = rot.n_axes > 2 ? rot.section[0] + rot.section[1] : kD;
+    turn.half_lanes = rot.rot_dim / 16;
+    turn.scale = rot.scale;
+    const bool whole = rot.rot_dim == kD;
+    if (rot.layout == MQUANT_ROTARY_HALVES) {
+        if (whole) launch_rotary<APPEND, true, true>(g, a, c, turn, stream);
+        else launch_rotary<APPEND, true, false>(g, a, c, turn, stream);
+    } else {
+        if (whole) launch_rotary<APPEND, false, true>(g, a, c, turn, stream);
+        else launch_rotary<APPEND, false, false>(g, a, c, turn, stream);
+    }
     return launch_status();
 }
 
@@ -199,13 +405,80 @@ extern "C" int mquant_kv_append(const void *q, int64_t ldq, void *q_out, int64_t
     if (const int st = check_cache(cache); st != MQUANT_OK) return st;
     if (const int st = check_norm(q_weight, k_weight, eps, base); st != MQUANT_OK) return st;
     if (T == 0 || cache->n_seq == 0) return MQUANT_OK;
-    if (!row_start || !pos) return MQUANT_ERR_NULL;
-    if (!aligned_to(row_start, 4) || !aligned_to(pos, 4) || !aligned_to(rope_pos, 4)) return MQUANT_ERR_ALIGNMENT;
-    if (const int st = check_side(q, ldq, q_out, ldqo, T, n_q_heads); st != MQUANT_OK) return st;
-    if (const int st = check_side(k, ldk, cache->k_pages_dev, ldk, T, cache->n_kv_heads); st != MQUANT_OK) return st;
-    if (const int st = check_side(v, ldv, cache->v_pages_dev, ldv, T, cache->n_kv_heads); st != MQUANT_OK) return st;
-    const Rows a = {static_cast<const __half *>(q), static_cast<const __half *>(k), static_cast<const __half *>(v),
-                    static_cast<__half *>(q_out), nullptr, ldq, ldqo, ldk, 0, ldv, static_cast<const __half *>(q_weight),
-                    static_cast<const __half *>(k_weight), pos, rope_pos, row_start, eps, T, n_q_heads, cache->n_kv_heads};
+    Rows a;
+    if (const int st = append_rows(q, ldq, q_out, ldqo, k, ldk, v, ldv, q_weight, k_weight, eps, row_start, pos, rope_pos, T, n_q_heads, cache, a);
+        st != MQUANT_OK)
+        return st;
     return launch<true>(a, cache_args(cache), base, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int mquant_rotary_init(mquant_rotary_t *rot, int32_t layout, int32_t rot_dim, double base, int32_t scaling, double factor,
+                                  double trained_len, double low_turns, double high_turns)
+{
+    if (!rot) return MQUANT_ERR_NULL;
+    if (rot_dim < 16 || rot_dim > kD || rot_dim % 16 != 0) return MQUANT_ERR_UNSUPPORTED;
+    if (layout != MQUANT_ROTARY_INTERLEAVED && layout != MQUANT_ROTARY_HALVES) return MQUANT_ERR_BAD_SHAPE;
+    if (scaling < MQUANT_ROTARY_NONE || scaling > MQUANT_ROTARY_TURNS) return MQUANT_ERR_BAD_SHAPE;
+    if (!(base > 1.0) || !std::isfinite(base) || !(factor >= 1.0) || !std::isfinite(factor)) return MQUANT_ERR_BAD_SHAPE;
+    if (scaling == MQUANT_ROTARY_TURNS &&
+        (!(trained_len > 0.0) || !std::isfinite(trained_len) || !(high_turns > low_turns) || !std::isfinite(high_turns) || !std::isfinite(low_turns)))
+        return MQUANT_ERR_BAD_SHAPE;
+    if (scaling == MQUANT_ROTARY_BASE) base *= pow(factor, static_cast<double>(rot_dim) / (rot_dim - 2));
+    if (!std::isfinite(base)) return MQUANT_ERR_BAD_SHAPE;
+    mquant_rotary_t r = {};
+    r.layout = layout;
+    r.rot_dim = rot_dim;
+    r.n_axes = 1;
+    r.section[0] = rot_dim / 2;
+    r.scale = 1.0f;
+    for (int j = 0; j < rot_dim / 2; ++j) {
+        const double f = pow(base, -2.0 * j / rot_dim);
+        r.freq[j] = f;
+        if (scaling == MQUANT_ROTARY_LINEAR) r.freq[j] = f / factor;
+        if (scaling == MQUANT_ROTARY_TURNS) {
+            const double turns = trained_len * f * 0.15915494309189533577;
+            double keep = (turns - low_turns) / (high_turns - low_turns);
+            keep = keep < 0.0 ? 0.0 : keep < 1.0 ? keep : 1.0;
+            r.freq[j] = f / factor * (1.0 - keep) + f * keep;
+        }
+    }
+    *rot = r;
+    return MQUANT_OK;
+}
+
+extern "C" int mquant_rotary_apply(const void *q, int64_t ldq, void *q_out, int64_t ldqo, const void *k, int64_t ldk, void *k_out,
+                                   int64_t ldko, const void *q_weight, const void *k_weight, float eps, const int32_t *pos, int32_t T,
+                                   int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const mquant_rotary_t *rot,
+                                   mquant_stream_t stream)
+{
+    if (T < 0 || n_q_heads < 0 || n_kv_heads < 0 || (n_q_heads == 0 && n_kv_heads == 0)) return MQUANT_ERR_BAD_SHAPE;
+    if (head_dim != kD) return MQUANT_ERR_UNSUPPORTED;
+    if (const int st = check_rotary(rot); st != MQUANT_OK) return st;
+    if (const int st = check_norm(q_weight, k_weight, eps); st != MQUANT_OK) return st;
+    if (T == 0) return MQUANT_OK;
+    if (!pos) return MQUANT_ERR_NULL;
+    if (!aligned_to(pos, 4)) return MQUANT_ERR_ALIGNMENT;
+    if (const int st = check_side(q, ldq, q_out, ldqo, T, n_q_heads); st != MQUANT_OK) return st;
+    if (const int st = check_side(k, ldk, k_out, ldko, T, n_kv_heads); st != MQUANT_OK) return st;
+    const Rows a = {static_cast<const __half *>(q), static_cast<const __half *>(k), nullptr, static_cast<__half *>(q_out),
+                    static_cast<__half *>(k_out), ldq, ldqo, ldk, ldko, 0, static_cast<const __half *>(q_weight),
+                    static_cast<const __half *>(k_weight), nullptr, pos, nullptr, eps, T, n_q_heads, n_kv_heads};
+    return launch<false>(a, PagedCache{}, *rot, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int mquant_rotary_append(const void *q, int64_t ldq, void *q_out, int64_t ldqo, const void *k, int64_t ldk, const void *v,
+                                    int64_t ldv, const void *q_weight, const void *k_weight, float eps, const int32_t *row_start,
+                                    const int32_t *pos, const int32_t *rope_pos, int32_t T, int32_t n_q_heads,
+                                    const mquant_rotary_t *rot, const mquant_paged_cache_t *cache, mquant_stream_t stream)
+{
+    if (T < 0 || n_q_heads < 0) return MQUANT_ERR_BAD_SHAPE;
+    if (const int st = check_cache(cache); st != MQUANT_OK) return st;
+    if (const int st = check_rotary(rot); st != MQUANT_OK) return st;
+    if (const int st = check_norm(q_weight, k_weight, eps); st != MQUANT_OK) return st;
+    if (T == 0 || cache->n_seq == 0) return MQUANT_OK;
+    Rows a;
+    if (const int st = append_rows(q, ldq, q_out, ldqo, k, ldk, v, ldv, q_weight, k_weight, eps, row_start, pos, rope_pos, T, n_q_heads, cache, a);
+        st != MQUANT_OK)
+        return st;
+    return launch<true>(a, cache_args(cache), *rot, static_cast<hipStream_t>(stream));
 }
