@@ -247,6 +247,9 @@ def _load_fast():
     mod.setup_serving(torch.float16, torch.float32, torch.int32, *(
         ctypes.cast(getattr(lib, "mquant_" + f), ctypes.c_void_p).value
         for f in ("qk_norm_rope", "kv_append", "paged_attention", "lora_apply")))
+    mod.setup_loop(torch.int64, *(
+        ctypes.cast(getattr(lib, "mquant_" + f), ctypes.c_void_p).value
+        for f in ("step_plan", "rotary_apply", "rotary_append", "paged_attention_shared", "sample")))
     return mod
 
 
@@ -821,6 +824,10 @@ def rotary_apply(q, k, pos_dev, rot: Rotary, n_q_heads: int, n_kv_heads: int, q_
         q_out = torch.empty((T, n_q_heads * head_dim), dtype=torch.float16, device=q.device)
     if k_out is None:
         k_out = torch.empty((T, n_kv_heads * head_dim), dtype=torch.float16, device=q.device)
+    st = _fast.rotary(q, k, pos_dev, rot.fast, n_q_heads, n_kv_heads, q_weight, k_weight, head_dim, eps, q_out, k_out)
+    if st is not NotImplemented:
+        _check(st, "mquant_rotary_apply")
+        return q_out, k_out
     lds = [_heads(t, n, head_dim, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
                                                                (k, n_kv_heads, "k"), (k_out, n_kv_heads, "k_out"))]
     _weight(q_weight, head_dim, "q_weight"), _weight(k_weight, head_dim, "k_weight"), _axes(pos_dev, rot, T, "pos")
@@ -836,6 +843,10 @@ def rotary_append(q, k, v, cache: PagedCache, row_start_dev, pos_dev, rot: Rotar
     T, D = q.shape[0], cache.head_dim
     if q_out is None:
         q_out = torch.empty((T, n_q_heads * D), dtype=torch.float16, device=q.device)
+    st = _fast.rotary_append(q, k, v, cache.fast, row_start_dev, pos_dev, rot.fast, n_q_heads, q_weight, k_weight, eps, rope_pos_dev, q_out)
+    if st is not NotImplemented:
+        _check(st, "mquant_rotary_append")
+        return q_out
     lds = [_heads(t, n, D, T, what) for t, n, what in ((q, n_q_heads, "q"), (q_out, n_q_heads, "q_out"),
                                                         (k, cache.n_kv_heads, "k"), (v, cache.n_kv_heads, "v"))]
     _weight(q_weight, D, "q_weight"), _weight(k_weight, D, "k_weight")
@@ -856,6 +867,11 @@ def step_plan(length, rows, page_table, page_size: int, free_pages, free_state, 
     new = lambda t, *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device=dev) if t is None else t
     length_out, state_out = new(length_out, n_seq), new(state_out, 2)
     row_start, pos, slots = new(row_start, n_seq + 1), new(pos, T), new(slots, T, dtype=torch.int64)
+    st = _fast.plan(length, rows, page_table, page_size, free_pages, free_state, T, shared_dev, order_dev, length_out, state_out, row_start, pos,
+                    slots)
+    if st is not NotImplemented:
+        _check(st, "mquant_step_plan")
+        return row_start, pos, slots
     for t, what in ((length, "length"), (rows, "rows"), (length_out, "length_out")):
         _operand(t, torch.int32, what, (n_seq,))
     _operand(row_start, torch.int32, "row_start", (n_seq + 1,)), _operand(pos, torch.int32, "pos", (T,))
@@ -896,6 +912,11 @@ def paged_attention_shared(q, cache: PagedCache, row_start_dev, pos_dev, group_s
         workspace = torch.empty(max(256, paged_attention_shared_workspace_bytes(T, cache, n_groups, n_q_heads, max_rows, max_prefix,
                                                                                 max_suffix)), dtype=torch.uint8, device=q.device)
     ws_bytes = workspace.numel() * workspace.element_size()
+    st = _fast.shared(q, cache.fast, row_start_dev, pos_dev, group_start_dev, prefix_dev, n_q_heads, max_rows, max_prefix, max_suffix, out,
+                      workspace, ws_bytes)
+    if st is not NotImplemented:
+        _check(st, "mquant_paged_attention_shared")
+        return out
     ldq, ldo = _heads(q, n_q_heads, D, T, "q"), _heads(out, n_q_heads, D, T, "out")
     _step(cache, row_start_dev, pos_dev, T), _workspace(workspace)
     _operand(group_start_dev, torch.int32, "group_start", (n_groups + 1,)), _operand(prefix_dev, torch.int32, "prefix", (n_groups,))
@@ -919,24 +940,28 @@ def sample_workspace_bytes(rows: int, V: int) -> int:
 def sample(logits, temperature, top_k, top_p, min_p, u, out=None, logprob=None, workspace=None):
     """The next token of every row of logits [rows, V] (fp16 or fp32) from random numbers u [rows]; temperature, top_k, top_p and
     min_p [rows], None: 1, all, 1, 0 -> (tokens int32 [rows], their log-probabilities fp32 [rows])."""
-    if logits.dtype not in _FLOATS:
+    kind = _FLOATS.get(logits.dtype)
+    if kind is None:
         raise MQuantError(ERR_UNSUPPORTED, f"logits: expected float16 or float32, got {logits.dtype}")
-    ld = _operand(logits, logits.dtype, "logits")
     rows, V = logits.shape
     if out is None:
         out = torch.empty(rows, dtype=torch.int32, device=logits.device)
     if logprob is None:
         logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    need = sample_workspace_bytes(rows, V)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is None:
+        workspace = torch.empty(max(256, sample_workspace_bytes(rows, V)), dtype=torch.uint8, device=logits.device)
+    ws_bytes = workspace.numel() * workspace.element_size()
+    st = _fast.sample(logits, kind, temperature, top_k, top_p, min_p, u, out, logprob, workspace, ws_bytes)
+    if st is not NotImplemented:
+        _check(st, "mquant_sample")
+        return out, logprob
+    ld = _operand(logits, logits.dtype, "logits")
     for t, dtype, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
                            (min_p, torch.float32, "min_p"), (u, torch.float32, "u"), (out, torch.int32, "out"),
                            (logprob, torch.float32, "logprob")):
         if t is not None:
             _operand(t, dtype, what, (rows,))
     _workspace(workspace)
-    _check(lib.mquant_sample(_dp(logits), _FLOATS[logits.dtype], max(ld, V), _dp(temperature), _dp(top_k), _dp(top_p), _dp(min_p), _dp(u),
+    _check(lib.mquant_sample(_dp(logits), kind, max(ld, V), _dp(temperature), _dp(top_k), _dp(top_p), _dp(min_p), _dp(u),
                              _dp(out), _dp(logprob), rows, V, _dp(workspace), ws_bytes, _stream()), "mquant_sample")
     return out, logprob

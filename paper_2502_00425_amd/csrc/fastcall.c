@@ -40,6 +40,13 @@ typedef struct {
     __typeof__(&mquant_kv_append) append;
     __typeof__(&mquant_paged_attention) attention;
     __typeof__(&mquant_lora_apply) lora;
+    // setup_loop(): torch.int64 and the entries of the serving loop
+    PyObject *i64;
+    __typeof__(&mquant_step_plan) plan;
+    __typeof__(&mquant_rotary_apply) rotary;
+    __typeof__(&mquant_rotary_append) rotary_append;
+    __typeof__(&mquant_paged_attention_shared) shared;
+    __typeof__(&mquant_sample) sample;
 } State;
 
 // ---- readers: 1 on success, 0 where the slow way has to look.  An interrupt, an exit and exhausted memory are nobody's
@@ -458,6 +465,158 @@ static PyObject *lora(PyObject *self, PyObject *const *a, Py_ssize_t n)
     LAUNCH(m->lora(x, ldx, perm, id, pa, pb, scale, base, ldb, y, ldy, T32, N32, K32, rank32, n32, work, bytes, s));
 }
 
+// Rotary.fast: (address of its descriptor, axes)
+static int read_rotary(PyObject *t, const mquant_rotary_t **r, int64_t *axes)
+{
+    if (!PyTuple_CheckExact(t) || PyTuple_GET_SIZE(t) != 2 || !read_i64(PyTuple_GET_ITEM(t, 1), axes)) return 0;
+    *r = PyLong_AsVoidPtr(PyTuple_GET_ITEM(t, 0));
+    return PyErr_Occurred() ? no() : 1;
+}
+
+// Positions [axes, T], or [T] of a single axis.
+static int read_axes(const State *m, PyObject *t, int64_t dev, int64_t axes, int64_t T, int may_miss, void **p)
+{
+    int64_t both[2] = {axes, T};
+    if (read_placed(t, m->i32, dev, 2, both, may_miss, p)) return 1;
+    int64_t one = T;
+    return !PyErr_Occurred() && axes == 1 && read_placed(t, m->i32, dev, 1, &one, may_miss, p);
+}
+
+static PyObject *rotary(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // q, k, pos, rotary, n_q_heads, n_kv_heads, q_weight, k_weight, head_dim, eps, q_out, k_out
+    void *q, *k, *qw, *kw, *pos, *qo, *ko;
+    const mquant_rotary_t *rot;
+    int64_t dev, T = -1, ldq, ldk, ldqo, ldko, w, axes;
+    int32_t T32, n_q, n_kv, D;
+    float eps;
+    mquant_stream_t s;
+    if (n != 12 || !m->i64 || !read_place(m, &dev, &s) || !read_rotary(a[3], &rot, &axes) || !read_i32(a[4], &n_q) || !read_i32(a[5], &n_kv) ||
+        !read_i32(a[8], &D) || n_q < 1 || n_kv < 1 || D < 1 || !read_f32(a[9], &eps))
+        SLOW_WAY;
+    int64_t one = D;
+    if (!read_placed_rows(m, a[0], dev, &T, (int64_t)n_q * D, &q, &ldq, &w) ||
+        !read_placed_rows(m, a[1], dev, &T, (int64_t)n_kv * D, &k, &ldk, &w) ||
+        !read_placed_rows(m, a[10], dev, &T, (int64_t)n_q * D, &qo, &ldqo, &w) ||
+        !read_placed_rows(m, a[11], dev, &T, (int64_t)n_kv * D, &ko, &ldko, &w) || !read_size(T, &T32) ||
+        !read_placed(a[6], m->f16, dev, 1, &one, 1, &qw) || !read_placed(a[7], m->f16, dev, 1, &one, 1, &kw) ||
+        !read_axes(m, a[2], dev, axes, T, 0, &pos))
+        SLOW_WAY;
+    LAUNCH(m->rotary(q, ldq, qo, ldqo, k, ldk, ko, ldko, qw, kw, eps, pos, T32, n_q, n_kv, D, rot, s));
+}
+
+static PyObject *rotary_append(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // q, k, v, cache, row_start, pos, rotary, n_q_heads, q_weight, k_weight, eps, rope_pos, q_out
+    void *q, *k, *v, *qw, *kw, *start, *pos, *rope, *qo;
+    const mquant_paged_cache_t *c;
+    const mquant_rotary_t *rot;
+    int64_t dev, T = -1, ldq, ldk, ldv, ldqo, w, n_seq, n_kv, D, axes;
+    int32_t T32, n_q;
+    float eps;
+    mquant_stream_t s;
+    if (n != 13 || !m->i64 || !read_place(m, &dev, &s) || !read_cache(a[3], dev, &c, &n_seq, &n_kv, &D) || !read_rotary(a[6], &rot, &axes) ||
+        !read_i32(a[7], &n_q) || n_q < 1 || !read_f32(a[10], &eps))
+        SLOW_WAY;
+    int64_t starts = n_seq + 1, one = D;
+    if (!read_placed_rows(m, a[0], dev, &T, n_q * D, &q, &ldq, &w) || !read_placed_rows(m, a[1], dev, &T, n_kv * D, &k, &ldk, &w) ||
+        !read_placed_rows(m, a[2], dev, &T, n_kv * D, &v, &ldv, &w) || !read_placed_rows(m, a[12], dev, &T, n_q * D, &qo, &ldqo, &w) ||
+        !read_size(T, &T32) || !read_placed(a[4], m->i32, dev, 1, &starts, 0, &start) || !read_placed(a[5], m->i32, dev, 1, &T, 0, &pos) ||
+        !read_placed(a[8], m->f16, dev, 1, &one, 1, &qw) || !read_placed(a[9], m->f16, dev, 1, &one, 1, &kw) ||
+        !read_axes(m, a[11], dev, axes, T, 1, &rope))
+        SLOW_WAY;
+    LAUNCH(m->rotary_append(q, ldq, qo, ldqo, k, ldk, v, ldv, qw, kw, eps, start, pos, rope, T32, n_q, rot, c, s));
+}
+
+static PyObject *plan(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // length, rows, page_table, page_size, free_pages, free_state, T, shared, order, length_out, state_out, row_start, pos, slots
+    void *length, *rows, *table, *ring, *state, *shared, *order, *length_out, *state_out, *start, *pos, *slots;
+    int64_t dev, n_seq = -1, n_pages = -1, T64, two = 2;
+    int32_t seq32, pages32, width32, page, T;
+    mquant_stream_t s;
+    if (n != 14 || !m->i64 || !read_place(m, &dev, &s) || !read_i32(a[3], &page) || !read_i32(a[6], &T) || T < 0) SLOW_WAY;
+    T64 = T;
+    if (!read_placed(a[1], m->i32, dev, 1, &n_seq, 0, &rows) || !read_placed(a[0], m->i32, dev, 1, &n_seq, 0, &length)) SLOW_WAY;
+    int64_t shape[2] = {n_seq, -1}, starts = n_seq + 1;
+    if (!read_placed(a[2], m->i32, dev, 2, shape, 0, &table) || !read_placed(a[4], m->i32, dev, 1, &n_pages, 0, &ring) ||
+        !read_placed(a[5], m->i32, dev, 1, &two, 0, &state) || !read_placed(a[7], m->i32, dev, 1, &n_seq, 1, &shared) ||
+        !read_placed(a[8], m->i32, dev, 1, &T64, 1, &order) || !read_placed(a[9], m->i32, dev, 1, &n_seq, 0, &length_out) ||
+        !read_placed(a[10], m->i32, dev, 1, &two, 0, &state_out) || !read_placed(a[11], m->i32, dev, 1, &starts, 0, &start) ||
+        !read_placed(a[12], m->i32, dev, 1, &T64, 0, &pos) || !read_placed(a[13], m->i64, dev, 1, &T64, 1, &slots) ||
+        !read_size(n_seq, &seq32) || !read_size(n_pages, &pages32) || !read_size(shape[1], &width32))
+        SLOW_WAY;
+    LAUNCH(m->plan(length, rows, shared, order, seq32, table, width32, page, ring, pages32, state, state_out, length_out, start, pos, slots, T, s));
+}
+
+static PyObject *shared(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // q, cache, row_start, pos, group_start, prefix, n_q_heads, max_rows, max_prefix, max_suffix, out, workspace, its bytes
+    void *q, *start, *pos, *groups, *prefix, *o, *work;
+    const mquant_paged_cache_t *c;
+    int64_t dev, T = -1, ldq, ldo, w, n_seq, n_kv, D, bytes, n_groups = -1;
+    int32_t T32, groups32, n_q, max_rows, max_prefix, max_suffix;
+    mquant_stream_t s;
+    if (n != 13 || !m->i64 || !read_place(m, &dev, &s) || !read_cache(a[1], dev, &c, &n_seq, &n_kv, &D) || !read_i32(a[6], &n_q) || n_q < 1 ||
+        !read_i32(a[7], &max_rows) || !read_i32(a[8], &max_prefix) || !read_i32(a[9], &max_suffix) || !read_i64(a[12], &bytes))
+        SLOW_WAY;
+    int64_t starts = n_seq + 1;
+    if (!read_placed_rows(m, a[0], dev, &T, n_q * D, &q, &ldq, &w) || !read_placed_rows(m, a[10], dev, &T, n_q * D, &o, &ldo, &w) ||
+        !read_size(T, &T32) || !read_placed(a[2], m->i32, dev, 1, &starts, 0, &start) || !read_placed(a[3], m->i32, dev, 1, &T, 0, &pos) ||
+        !read_placed(a[5], m->i32, dev, 1, &n_groups, 0, &prefix) || !read_size(n_groups, &groups32) || !read_workspace(a[11], dev, &work))
+        SLOW_WAY;
+    int64_t group_starts = n_groups + 1;
+    if (!read_placed(a[4], m->i32, dev, 1, &group_starts, 0, &groups)) SLOW_WAY;
+    LAUNCH(m->shared(q, ldq, c, start, pos, groups, prefix, groups32, o, ldo, T32, n_q, max_rows, max_prefix, max_suffix, work, bytes, s));
+}
+
+static PyObject *sample(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const State *m = PyModule_GetState(self);
+    // logits, type, temperature, top_k, top_p, min_p, u, out, logprob, workspace, its bytes
+    void *l, *t, *k, *p, *min_p, *u, *o, *lp, *work;
+    int64_t dev, rows, V, ld, bytes;
+    int32_t type, rows32, V32;
+    mquant_stream_t s;
+    if (n != 11 || !m->i64 || !read_place(m, &dev, &s) || !read_i32(a[1], &type) || !read_i64(a[10], &bytes) ||
+        !read_rows(a[0], &l, &ld, &rows, &V) || rows < 1 || !placed(a[0], type == MQUANT_F16 ? m->f16 : m->f32, dev))
+        SLOW_WAY;
+    if (rows == 1 || ld < V) ld = V;                           // the stride of a single row says nothing
+    if (!read_size(rows, &rows32) || !read_size(V, &V32) || !read_placed(a[2], m->f32, dev, 1, &rows, 1, &t) ||
+        !read_placed(a[3], m->i32, dev, 1, &rows, 1, &k) || !read_placed(a[4], m->f32, dev, 1, &rows, 1, &p) ||
+        !read_placed(a[5], m->f32, dev, 1, &rows, 1, &min_p) || !read_placed(a[6], m->f32, dev, 1, &rows, 0, &u) ||
+        !read_placed(a[7], m->i32, dev, 1, &rows, 0, &o) || !read_placed(a[8], m->f32, dev, 1, &rows, 1, &lp) || !read_workspace(a[9], dev, &work))
+        SLOW_WAY;
+    LAUNCH(m->sample(l, type, ld, t, k, p, min_p, u, o, lp, rows32, V32, work, bytes, s));
+}
+
+// setup_loop(int64, addresses of the five entries in the order of State), behind setup_serving()
+static PyObject *setup_loop(PyObject *self, PyObject *args)
+{
+    PyObject *i64, *addr[5];
+    if (!PyArg_ParseTuple(args, "OO!O!O!O!O!", &i64, &PyLong_Type, &addr[0], &PyLong_Type, &addr[1], &PyLong_Type, &addr[2], &PyLong_Type,
+                          &addr[3], &PyLong_Type, &addr[4]))
+        return NULL;
+    void *p[5];
+    for (int i = 0; i < 5; ++i) {
+        p[i] = PyLong_AsVoidPtr(addr[i]);
+        if (PyErr_Occurred()) return NULL;
+    }
+    State *m = PyModule_GetState(self);
+    *(void **)&m->plan = p[0];
+    *(void **)&m->rotary = p[1];
+    *(void **)&m->rotary_append = p[2];
+    *(void **)&m->shared = p[3];
+    *(void **)&m->sample = p[4];
+    Py_INCREF(i64);
+    Py_XSETREF(m->i64, i64);
+    Py_RETURN_NONE;
+}
+
 // setup_serving(float16, float32, int32, addresses of the four entries in the order of State), behind setup()
 static PyObject *setup_serving(PyObject *self, PyObject *args)
 {
@@ -514,7 +673,8 @@ static PyObject *setup(PyObject *self, PyObject *args)
 static PyMethodDef methods[] = {
     ENTRY(prefill), ENTRY(prefill_static), ENTRY(decode), ENTRY(decode_grouped), ENTRY(gemv_grouped), ENTRY(quant),
     ENTRY(weight_only), ENTRY(norm), ENTRY(append), ENTRY(attention), ENTRY(lora), {"setup", setup, METH_VARARGS, NULL},
-    {"setup_serving", setup_serving, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL},
+    {"setup_serving", setup_serving, METH_VARARGS, NULL}, ENTRY(plan), ENTRY(rotary), ENTRY(rotary_append), ENTRY(shared), ENTRY(sample),
+    {"setup_loop", setup_loop, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL},
 };
 
 static int traverse(PyObject *self, visitproc visit, void *arg)
@@ -526,6 +686,7 @@ static int traverse(PyObject *self, visitproc visit, void *arg)
     Py_VISIT(m->f16);
     Py_VISIT(m->f32);
     Py_VISIT(m->i32);
+    Py_VISIT(m->i64);
     return 0;
 }
 
@@ -538,6 +699,7 @@ static int clear(PyObject *self)
     Py_CLEAR(m->f16);
     Py_CLEAR(m->f32);
     Py_CLEAR(m->i32);
+    Py_CLEAR(m->i64);
     return 0;
 }
 

@@ -18,15 +18,12 @@
 #include <cfloat>
 #include <cmath>
 
-#include <hip/hip_fp16.h>
-
-#include "mquant_internal.h"
+#include "serving_common.h"
 
 using namespace mquant;
 
 namespace {
 
-typedef unsigned long long u64;
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxTokens = 1 << 20;
@@ -156,40 +153,7 @@ struct Row {
 // Whether a token with this logit can be chosen: neither -inf nor NaN.
 __device__ __forceinline__ bool there(float l) { return l > -INFINITY; }
 
-// ---- over a wave and the work-group, inside the register file: an exchange of lanes through LDS takes the latency of an LDS read, of
-// which a scan has six, one behind another.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t none)       // lanes that nothing comes to get `none`
-{
-    return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 moved(u64 x, u64 none)
-{
-    return static_cast<u64>(moved<CTRL, ROWS>(static_cast<uint32_t>(x >> 32), static_cast<uint32_t>(none >> 32))) << 32 |
-           moved<CTRL, ROWS>(static_cast<uint32_t>(x), static_cast<uint32_t>(none));
-}
-
-__device__ __forceinline__ u64 from_lane(u64 x, int lane)
-{
-    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), lane);
-    return static_cast<u64>(hi) << 32 | lo;
-}
-__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-
-// Up to and with this lane: inside rows of 16 by shifts, then the last lane of the row (of both rows) ahead.
-template <typename N>
-__device__ __forceinline__ N wave_scan(N x)
-{
-    x += moved<0x111, 0xf>(x, N{0});
-    x += moved<0x112, 0xf>(x, N{0});
-    x += moved<0x114, 0xf>(x, N{0});
-    x += moved<0x118, 0xf>(x, N{0});
-    x += moved<0x142, 0xa>(x, N{0});
-    x += moved<0x143, 0xc>(x, N{0});
-    return x;
-}
-
+// ---- over the work-group
 __device__ __forceinline__ u64 wave_sum(u64 x) { return from_lane(wave_scan(x), 63); }
 
 // Up to and with this thread; `all`: over all threads.  Ends behind a barrier that frees nothing: a barrier has to come before the next use.

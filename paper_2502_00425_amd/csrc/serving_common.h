@@ -1,5 +1,5 @@
-// What the operators of the serving step share (qk_norm.hip, paged_attention.hip): the paged cache as the
-// kernels see it, its checks, and the sequence a row belongs to.
+// What the operators of the serving step and loop share (qk_norm.hip, paged_attention.hip, step_plan.hip, sample.hip): the paged cache as
+// the kernels see it, its checks, the sequence a row belongs to, and sums over a wave.
 #pragma once
 
 #include <hip/hip_fp16.h>
@@ -59,6 +59,41 @@ __device__ __forceinline__ float row16_sum(float x)
 }
 __device__ __forceinline__ int32_t row16_max(int32_t x) { return row16(x, [](int a, int b) { return a > b ? a : b; }); }
 __device__ __forceinline__ int32_t row16_min(int32_t x) { return row16(x, [](int a, int b) { return a < b ? a : b; }); }
+
+// Sums over a wave inside the register file (see row16): a scan has six exchanges, one behind another.
+typedef unsigned long long u64;
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t none)       // lanes that nothing comes to get `none`
+{
+    return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 x, u64 none)
+{
+    return static_cast<u64>(moved<CTRL, ROWS>(static_cast<uint32_t>(x >> 32), static_cast<uint32_t>(none >> 32))) << 32 |
+           moved<CTRL, ROWS>(static_cast<uint32_t>(x), static_cast<uint32_t>(none));
+}
+
+__device__ __forceinline__ u64 from_lane(u64 x, int lane)
+{
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), lane);
+    return static_cast<u64>(hi) << 32 | lo;
+}
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+// Up to and with this lane: inside rows of 16 by shifts, then the last lane of the row (of both rows) ahead.
+template <typename N>
+__device__ __forceinline__ N wave_scan(N x)
+{
+    x += moved<0x111, 0xf>(x, N{0});
+    x += moved<0x112, 0xf>(x, N{0});
+    x += moved<0x114, 0xf>(x, N{0});
+    x += moved<0x118, 0xf>(x, N{0});
+    x += moved<0x142, 0xa>(x, N{0});
+    x += moved<0x143, 0xc>(x, N{0});
+    return x;
+}
 
 // Sequence of row i: the number of sequences that start at or before it, less one; -1 for a row of none.  A wave looks at
 // 64 starts at a time (row_start does not decrease).

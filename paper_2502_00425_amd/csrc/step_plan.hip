@@ -3,7 +3,7 @@
 //
 // With r the rows a sequence may get and need its new pages, everything is a sum along the sequences: a sequence is served while both sums
 // stay inside T and the free pages, which is a condition that never turns true again, so that sums over all of them place the
-// served ones.  plan_kernel, one work-group, walks the sequences 1024 at a time with the sums carried on; pages and rows are dealt to the
+// served ones.  plan_kernel, one work-group, walks the sequences a tile at a time with the sums carried on; pages and rows are dealt to the
 // threads by their number and find their sequence by bisection of the sums.  Many rows are written by plan_rows_kernel instead.
 #include "serving_common.h"
 
@@ -11,10 +11,12 @@ using namespace mquant;
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kMost = 1024;                // threads of plan_kernel: this many, or
+constexpr int kFew = 256;                  // fewer, whose barriers are quicker (one sequence and row 1.5 us, 5.5), for up to
+constexpr int kFewSeqs = 32, kFewRows = 1024;  // so many: more sequences can give back more pages than few threads move quickly
+constexpr int kPagesAhead = 8;             // of a thread, on their way at a time
 constexpr int kRowsHere = 4096;            // rows up to which the one work-group writes them itself
-constexpr int kRowsThread = 4;             // rows of a thread of plan_rows_kernel
-constexpr int kStartsLds = 4096;           // starts of sequences that a work-group of plan_rows_kernel holds in LDS
+constexpr int kStartsLds = 4096;           // sequences whose starts and lengths a work-group of plan_rows_kernel holds in LDS
 
 struct Plan {
     const int32_t *length, *rows, *shared, *order;
@@ -25,32 +27,26 @@ struct Plan {
     int32_t n_seq, table_pages, page_shift, n_pages, T;
 };
 
-__device__ __forceinline__ int64_t shfl_up64(int64_t x, int by)
-{
-    const int lo = __shfl_up(static_cast<int>(x), by, 64), hi = __shfl_up(static_cast<int>(x >> 32), by, 64);
-    return (static_cast<int64_t>(hi) << 32) | static_cast<uint32_t>(lo);
-}
-
-// Sum of x over the threads up to this one; `all`: over all threads.  `room` holds a number per wave and may be used again behind the
-// next barrier.
-__device__ __forceinline__ int64_t scan(int64_t x, int64_t *room, int64_t &all)
+// Sums of x and y over the threads up to and with this one, and over all.  `room` holds two numbers a wave; a barrier has to come before
+// the next use.
+template <int THREADS>
+__device__ __forceinline__ void scan(u64 &x, u64 &y, u64 (&room)[2][THREADS / 64], u64 &all_x, u64 &all_y)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = shfl_up64(x, d);
-        if (lane >= d) x += y;
+    x = wave_scan(x);
+    y = wave_scan(y);
+    if (lane == 63) {
+        room[0][wave] = x;
+        room[1][wave] = y;
     }
     __syncthreads();
-    if (lane == 63) room[wave] = x;
-    __syncthreads();
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-        if (w == wave) x += all;
-        all += room[w];
+    const u64 sx = wave_scan(lane < THREADS / 64 ? room[0][lane] : 0), sy = wave_scan(lane < THREADS / 64 ? room[1][lane] : 0);
+    all_x = from_lane(sx, THREADS / 64 - 1);
+    all_y = from_lane(sy, THREADS / 64 - 1);
+    if (wave > 0) {
+        x += from_lane(sx, __builtin_amdgcn_readfirstlane(wave) - 1);
+        y += from_lane(sy, __builtin_amdgcn_readfirstlane(wave) - 1);
     }
-    return x;
 }
 
 // The first of n rising numbers that is above x (n: none).
@@ -68,91 +64,107 @@ __device__ __forceinline__ int32_t above(const N *v, int32_t n, int64_t x)
 
 __device__ __forceinline__ int32_t slots_of(const Plan &a) { return a.table_pages << a.page_shift; }
 
-__device__ __forceinline__ int32_t length_of(const Plan &a, int32_t s)
+__device__ __forceinline__ int32_t in_table(const Plan &a, int32_t n)
 {
-    const int32_t n = a.length[s], most = slots_of(a);
+    const int32_t most = slots_of(a);
     return n < 0 ? 0 : n < most ? n : most;
 }
 
 __device__ __forceinline__ int32_t pages_of(const Plan &a, int32_t n) { return static_cast<int32_t>((static_cast<uint32_t>(n) + (1u << a.page_shift) - 1) >> a.page_shift); }
 
-// Position and slot of row i, the (i - start)-th of the n new rows of sequence s (n_seq: of none).
-__device__ __forceinline__ void write_row(const Plan &a, int32_t i, int32_t s, int32_t start, int32_t n)
+// Position and slot of row i, new token number o of the n that sequence s gets, which has `end` tokens with them (n = 0: of no sequence).
+__device__ __forceinline__ void write_row(const Plan &a, int32_t i, int32_t s, int32_t o, int32_t n, int32_t end)
 {
     int32_t p = -1;
     int64_t at = -1;
-    if (s < a.n_seq) {
-        const int32_t o = a.order ? a.order[i] : i - start;
-        if (o >= 0 && o < n) {
-            p = a.length_out[s] - n + o;
-            const int32_t page = a.table[static_cast<int64_t>(s) * a.table_pages + (p >> a.page_shift)];
-            if (page >= 0 && page < a.n_pages) at = (static_cast<int64_t>(page) << a.page_shift) + (p & ((1 << a.page_shift) - 1));
-        }
+    if (o >= 0 && o < n) {
+        p = end - n + o;
+        const int32_t page = a.table[static_cast<int64_t>(s) * a.table_pages + (p >> a.page_shift)];
+        if (page >= 0 && page < a.n_pages) at = (static_cast<int64_t>(page) << a.page_shift) + (p & ((1 << a.page_shift) - 1));
     }
     a.pos[i] = p;
     if (a.slot) a.slot[i] = at;
 }
 
-__global__ __launch_bounds__(kThreads) void plan_kernel(Plan a, int32_t write_rows)
+// Bound by trips to memory, one behind another: lengths and requests, the free pages, the table, and a barrier between them.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void plan_kernel(Plan a, int32_t write_rows)
 {
-    __shared__ int64_t room[kThreads / 64], sums[kThreads], served[2];
-    __shared__ int32_t pages0[kThreads], starts[kThreads];
+    __shared__ u64 room[2][2][THREADS / 64], served[2];
+    __shared__ int64_t sums[THREADS];
+    __shared__ int32_t pages0[THREADS], starts[THREADS], ends[THREADS];
     const int tid = threadIdx.x;
-    int32_t head = a.state[0] % a.n_pages, count = a.state[1];
+    int32_t head = a.state[0], count = a.state[1];
+    int32_t asked = 0, length = 0, shared = 0;                 // of this thread's sequence of the first tile
+    auto fetch = [&](int32_t s) {
+        asked = s < a.n_seq ? a.rows[s] : 0;
+        length = s < a.n_seq ? a.length[s] : 0;
+        shared = s < a.n_seq && a.shared ? a.shared[s] : 0;
+    };
+    fetch(tid);
+    head %= a.n_pages;
     if (head < 0) head += a.n_pages;
     count = count < 0 ? 0 : count < a.n_pages ? count : a.n_pages;
-    __syncthreads();                                           // state_out may be the same array
+    if (tid < 2) served[tid] = 0;
+    auto in_ring = [&](int64_t i) {                            // place i < n_pages behind its beginning
+        const int64_t at = head + i;
+        return at < a.n_pages ? at : at - a.n_pages;
+    };
 
     // pages of ended sequences to the ring's end
     int64_t given = 0;
-    for (int32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
-        const int32_t s = s0 + tid;
+    for (int32_t s0 = 0; s0 < a.n_seq; s0 += THREADS) {
+        if (s0 > 0) fetch(s0 + tid);
         int32_t n = 0;
-        if (s < a.n_seq && a.rows[s] < 0) {
-            const int32_t own = a.shared && a.shared[s] > 0 ? a.shared[s] : 0;
-            n = pages_of(a, length_of(a, s)) - own;
+        if (asked < 0) {
+            n = pages_of(a, in_table(a, length)) - (shared > 0 ? shared : 0);
             n = n > 0 ? n : 0;
         }
-        int64_t all;
-        sums[tid] = scan(n, room, all);
-        if (all > 0) {
+        if (__syncthreads_or(n > 0)) {
+            u64 x = n, y = 0, all, none;
+            scan<THREADS>(x, y, room[0], all, none);
+            sums[tid] = static_cast<int64_t>(x);
+            starts[tid] = shared > 0 ? shared : 0;
             __syncthreads();
-            const int32_t tile = a.n_seq - s0 < kThreads ? a.n_seq - s0 : kThreads;
-            for (int64_t i = tid; i < all; i += kThreads) {
-                const int32_t j = above(sums, tile, i);
-                const int64_t first = j > 0 ? sums[j - 1] : 0;
-                const int32_t own = a.shared && a.shared[s0 + j] > 0 ? a.shared[s0 + j] : 0;
-                const int32_t id = a.table[static_cast<int64_t>(s0 + j) * a.table_pages + own + (i - first)];
-                // more pages than the ring holds can only be pages given back twice: they are not written over others
-                if (count + given + i < a.n_pages) a.ring[(static_cast<int64_t>(head) + count + given + i) % a.n_pages] = id;
+            const int32_t tile = a.n_seq - s0 < THREADS ? a.n_seq - s0 : THREADS;
+            for (int64_t i0 = tid; i0 < static_cast<int64_t>(all); i0 += THREADS * kPagesAhead) {
+                int32_t id[kPagesAhead];
+#pragma unroll
+                for (int u = 0; u < kPagesAhead; ++u) {
+                    const int64_t i = i0 + u * THREADS < static_cast<int64_t>(all) ? i0 + u * THREADS : i0;
+                    const int32_t j = above(sums, tile, i);
+                    id[u] = a.table[static_cast<int64_t>(s0 + j) * a.table_pages + starts[j] + (i - (j > 0 ? sums[j - 1] : 0))];
+                }
+#pragma unroll
+                for (int u = 0; u < kPagesAhead; ++u) {
+                    const int64_t i = i0 + u * THREADS, at = count + given + i;
+                    // more pages than the ring holds can only be pages given back twice: they are not written over others
+                    if (i < static_cast<int64_t>(all) && at < a.n_pages) a.ring[in_ring(at)] = id[u];
+                }
             }
+            given += static_cast<int64_t>(all);
         }
-        given += all;
-        __syncthreads();
     }
     const int64_t there = count + given < a.n_pages ? count + given : a.n_pages;
+    if (a.n_seq > THREADS) fetch(tid);
+    __syncthreads();
 
     // rows and pages of the others
-    if (tid < 2) served[tid] = 0;
     int64_t rows_before = 0, need_before = 0;                  // sums over the sequences behind us, served or not
-    for (int32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
-        const int32_t s = s0 + tid;
-        int32_t r = 0, before = 0, need = 0;
-        bool ended = false;
-        if (s < a.n_seq) {
-            r = a.rows[s];
-            before = length_of(a, s);
-            ended = r < 0;
-            if (ended || static_cast<int64_t>(before) + r > slots_of(a)) r = 0;
-            pages0[tid] = pages_of(a, before);
-            need = pages_of(a, before + r) - pages0[tid];
-        }
-        int64_t all_rows, all_need;
-        const int64_t my_rows = rows_before + scan(r, room, all_rows);
-        const int64_t my_need = need_before + scan(need, room, all_need);
+    for (int32_t s0 = 0, odd = 0; s0 < a.n_seq; s0 += THREADS, odd ^= 1) {
+        if (s0 > 0) fetch(s0 + tid);
+        const int32_t s = s0 + tid, before = in_table(a, length);
+        const bool ended = asked < 0;
+        const int32_t r = ended || static_cast<int64_t>(before) + asked > slots_of(a) ? 0 : asked;
+        const int32_t have = pages_of(a, before);
+        pages0[tid] = have;
+        u64 my_rows = r, my_need = pages_of(a, before + r) - have, all_rows, all_need;
+        scan<THREADS>(my_rows, my_need, room[odd], all_rows, all_need);
+        my_rows += rows_before;
+        my_need += need_before;
         const int64_t need_first = served[1];                  // where this tile's pages begin
-        const bool ok = s < a.n_seq && my_rows <= a.T && my_need <= there;
-        sums[tid] = my_need;
+        const bool ok = s < a.n_seq && my_rows <= static_cast<u64>(a.T) && my_need <= static_cast<u64>(there);
+        sums[tid] = static_cast<int64_t>(my_need);
         const int n_ok = __syncthreads_count(ok);              // they are the tile's first ones
         if (tid == n_ok - 1) {
             served[0] = my_rows;
@@ -160,62 +172,74 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Plan a, int32_t write_ro
         }
         __syncthreads();
         if (s < a.n_seq) {
-            const int32_t start = static_cast<int32_t>(ok ? my_rows - r : served[0]);
+            const int32_t start = static_cast<int32_t>(ok ? my_rows - r : served[0]), end = ended ? 0 : ok ? before + r : before;
             a.row_start[s] = start;
+            a.length_out[s] = end;
             starts[tid] = start;                               // of the last tile, which is the only one where they are used
-            a.length_out[s] = ended ? 0 : ok ? before + r : before;
+            ends[tid] = end;
         }
-        for (int64_t i = need_first + tid; i < served[1]; i += kThreads) {
-            const int32_t j = above(sums, n_ok, i);
-            const int64_t first = j > 0 ? sums[j - 1] : need_before;
-            a.table[static_cast<int64_t>(s0 + j) * a.table_pages + pages0[j] + (i - first)] = a.ring[(head + i) % a.n_pages];
+        const int64_t need_end = static_cast<int64_t>(served[1]);
+        for (int64_t i0 = need_first + tid; i0 < need_end; i0 += THREADS * kPagesAhead) {
+            int32_t id[kPagesAhead];
+#pragma unroll
+            for (int u = 0; u < kPagesAhead; ++u) id[u] = a.ring[in_ring(i0 + u * THREADS < need_end ? i0 + u * THREADS : i0)];
+#pragma unroll
+            for (int u = 0; u < kPagesAhead; ++u) {
+                const int64_t i = i0 + u * THREADS;
+                if (i >= need_end) break;
+                const int32_t j = above(sums, n_ok, i);
+                a.table[static_cast<int64_t>(s0 + j) * a.table_pages + pages0[j] + (i - (j > 0 ? sums[j - 1] : need_before))] = id[u];
+            }
         }
-        rows_before += all_rows;
-        need_before += all_need;
+        rows_before += static_cast<int64_t>(all_rows);
+        need_before += static_cast<int64_t>(all_need);
         __syncthreads();
     }
-    if (a.n_seq == 0) __syncthreads();
     const int32_t rows = static_cast<int32_t>(served[0]);
     if (tid == 0) {
         a.row_start[a.n_seq] = rows;
-        a.state_out[0] = static_cast<int32_t>((head + served[1]) % a.n_pages);
-        a.state_out[1] = static_cast<int32_t>(there - served[1]);
+        a.state_out[0] = static_cast<int32_t>(served[1] < static_cast<u64>(a.n_pages) ? in_ring(static_cast<int64_t>(served[1])) : head);
+        a.state_out[1] = static_cast<int32_t>(there - static_cast<int64_t>(served[1]));
     }
     if (!write_rows) return;
-    for (int32_t i = tid; i < a.T; i += kThreads) {
-        int32_t s = a.n_seq, start = 0, end = 0;
+    const bool here = a.n_seq <= THREADS;
+    for (int32_t i = tid; i < a.T; i += THREADS) {
+        int32_t s = 0, o = -1, n = 0, end = 0;
         if (i < rows) {
-            const int32_t *v = a.n_seq <= kThreads ? starts : a.row_start;
+            const int32_t *v = here ? starts : a.row_start;
             s = above(v, a.n_seq, i) - 1;
-            start = v[s];
-            end = s + 1 < a.n_seq ? v[s + 1] : rows;
+            n = (s + 1 < a.n_seq ? v[s + 1] : rows) - v[s];
+            o = a.order ? a.order[i] : i - v[s];
+            end = here ? ends[s] : a.length_out[s];
         }
-        write_row(a, i, s, start, end - start);
+        write_row(a, i, s, o, n, end);
     }
 }
 
-// Rows by the thread, sequences found by bisection of the starts (in LDS, where they fit).
+// Rows by the thread, sequences found by bisection of the starts (in LDS, where they fit).  134302 rows of 700 sequences: three trips to memory.
 __global__ __launch_bounds__(256) void plan_rows_kernel(Plan a)
 {
-    __shared__ int32_t lds[kStartsLds];
-    const bool here = a.n_seq < kStartsLds;
-    if (here)
-        for (int32_t s = threadIdx.x; s <= a.n_seq; s += 256) lds[s] = a.row_start[s];
-    __syncthreads();
-    const int32_t *v = here ? lds : a.row_start;
-    const int32_t rows = v[a.n_seq];
-#pragma unroll
-    for (int u = 0; u < kRowsThread; ++u) {
-        const int64_t i = (static_cast<int64_t>(blockIdx.x) * kRowsThread + u) * 256 + threadIdx.x;
-        if (i >= a.T) return;
-        int32_t s = a.n_seq, start = 0, end = 0;
-        if (i < rows) {
-            s = above(v, a.n_seq, i) - 1;
-            start = v[s];
-            end = v[s + 1];
+    __shared__ int32_t starts[kStartsLds + 1], ends[kStartsLds];
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    int32_t o = a.order && i < a.T ? a.order[i] : 0;
+    const bool here = a.n_seq <= kStartsLds;
+    if (here) {
+        for (int32_t s = threadIdx.x; s <= a.n_seq; s += 256) {
+            starts[s] = a.row_start[s];
+            if (s < a.n_seq) ends[s] = a.length_out[s];
         }
-        write_row(a, static_cast<int32_t>(i), s, start, end - start);
     }
+    __syncthreads();
+    if (i >= a.T) return;
+    const int32_t *v = here ? starts : a.row_start;
+    int32_t s = 0, n = 0, end = 0;
+    if (i < v[a.n_seq]) {
+        s = above(v, a.n_seq, i) - 1;
+        n = v[s + 1] - v[s];
+        end = here ? ends[s] : a.length_out[s];
+        if (!a.order) o = static_cast<int32_t>(i) - v[s];
+    }
+    write_row(a, static_cast<int32_t>(i), s, o, n, end);
 }
 
 }  // namespace
@@ -244,8 +268,9 @@ extern "C" int mquant_step_plan(const int32_t *length, const int32_t *rows, cons
                     n_seq, table_pages, __builtin_ctz(static_cast<unsigned>(page_size)), n_pages, T};
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     const bool here = T <= kRowsHere;
-    MQ_LAUNCH(plan_kernel, dim3(1), dim3(kThreads), 0, stream, a, here ? 1 : 0);
+    if (n_seq <= kFewSeqs && T <= kFewRows) MQ_LAUNCH(plan_kernel<kFew>, dim3(1), dim3(kFew), 0, stream, a, 1);
+    else MQ_LAUNCH(plan_kernel<kMost>, dim3(1), dim3(kMost), 0, stream, a, here ? 1 : 0);
     if (const int st = launch_status(); st != MQUANT_OK || here) return st;
-    MQ_LAUNCH(plan_rows_kernel, dim3(static_cast<unsigned>(ceil_div(T, 256 * kRowsThread))), dim3(256), 0, stream, a);
+    MQ_LAUNCH(plan_rows_kernel, dim3(static_cast<unsigned>(ceil_div(T, 256))), dim3(256), 0, stream, a);
     return launch_status();
 }
