@@ -14,7 +14,7 @@ namespace {
 constexpr int kMost = 1024;                // threads of plan_kernel: this many, or
 constexpr int kFew = 256;                  // fewer, whose barriers are quicker (one sequence and row 1.5 us, 5.5), for up to
 constexpr int kFewSeqs = 32, kFewRows = 1024;  // so many: more sequences can give back more pages than few threads move quickly
-constexpr int kPagesAhead = 8;             // of a thread, on their way at a time
+constexpr int kPagesAhead = 4;             // of a thread, on their way at a time
 constexpr int kRowsHere = 4096;            // rows up to which the one work-group writes them itself
 constexpr int kStartsLds = 4096;           // sequences whose starts and lengths a work-group of plan_rows_kernel holds in LDS
 
@@ -50,17 +50,18 @@ __device__ __forceinline__ void scan(u64 &x, u64 &y, u64 (&room)[2][THREADS / 64
 }
 
 // The first of n rising numbers that is above x (n: none).
-template <typename N>
-__device__ __forceinline__ int32_t above(const N *v, int32_t n, int64_t x)
+__device__ __forceinline__ int32_t above(const int32_t *v, int32_t n, int32_t x)
 {
     int32_t lo = 0, hi = n;
     while (lo < hi) {
         const int32_t mid = (lo + hi) >> 1;
-        if (static_cast<int64_t>(v[mid]) > x) hi = mid;
+        if (v[mid] > x) hi = mid;
         else lo = mid + 1;
     }
     return lo;
 }
+
+__device__ __forceinline__ int32_t up_to_int(u64 x) { return x < 0x7fffffff ? static_cast<int32_t>(x) : 0x7fffffff; }
 
 __device__ __forceinline__ int32_t slots_of(const Plan &a) { return a.table_pages << a.page_shift; }
 
@@ -91,8 +92,7 @@ template <int THREADS>
 __global__ __launch_bounds__(THREADS) void plan_kernel(Plan a, int32_t write_rows)
 {
     __shared__ u64 room[2][2][THREADS / 64], served[2];
-    __shared__ int64_t sums[THREADS];
-    __shared__ int32_t pages0[THREADS], starts[THREADS], ends[THREADS];
+    __shared__ int32_t sums[THREADS], pages0[THREADS], starts[THREADS], ends[THREADS];
     const int tid = threadIdx.x;
     int32_t head = a.state[0], count = a.state[1];
     int32_t asked = 0, length = 0, shared = 0;                 // of this thread's sequence of the first tile
@@ -121,26 +121,28 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(Plan a, int32_t write_row
             n = n > 0 ? n : 0;
         }
         if (__syncthreads_or(n > 0)) {
-            u64 x = n, y = 0, all, none;
-            scan<THREADS>(x, y, room[0], all, none);
-            sums[tid] = static_cast<int64_t>(x);
-            starts[tid] = shared > 0 ? shared : 0;
+            u64 x = n, y = n > 0 ? 1 : 0, all, n_ended;
+            scan<THREADS>(x, y, room[0], all, n_ended);
+            if (n > 0) {                                       // those that give some, next to each other
+                sums[y - 1] = up_to_int(x);
+                starts[y - 1] = shared > 0 ? shared : 0;
+                ends[y - 1] = s0 + tid;
+            }
             __syncthreads();
-            const int32_t tile = a.n_seq - s0 < THREADS ? a.n_seq - s0 : THREADS;
-            for (int64_t i0 = tid; i0 < static_cast<int64_t>(all); i0 += THREADS * kPagesAhead) {
+            // more pages than the ring holds can only be pages given back twice: they are not written over others
+            const int64_t left = a.n_pages - count - given;
+            const int32_t n_pages = left <= 0 ? 0 : static_cast<int64_t>(all) < left ? static_cast<int32_t>(all) : static_cast<int32_t>(left);
+            for (int64_t i0 = tid; i0 < n_pages; i0 += THREADS * kPagesAhead) {
                 int32_t id[kPagesAhead];
 #pragma unroll
                 for (int u = 0; u < kPagesAhead; ++u) {
-                    const int64_t i = i0 + u * THREADS < static_cast<int64_t>(all) ? i0 + u * THREADS : i0;
-                    const int32_t j = above(sums, tile, i);
-                    id[u] = a.table[static_cast<int64_t>(s0 + j) * a.table_pages + starts[j] + (i - (j > 0 ? sums[j - 1] : 0))];
+                    const int32_t i = static_cast<int32_t>(i0 + u * THREADS < n_pages ? i0 + u * THREADS : i0);
+                    const int32_t j = above(sums, static_cast<int32_t>(n_ended), i);
+                    id[u] = a.table[static_cast<int64_t>(ends[j]) * a.table_pages + starts[j] + (i - (j > 0 ? sums[j - 1] : 0))];
                 }
 #pragma unroll
-                for (int u = 0; u < kPagesAhead; ++u) {
-                    const int64_t i = i0 + u * THREADS, at = count + given + i;
-                    // more pages than the ring holds can only be pages given back twice: they are not written over others
-                    if (i < static_cast<int64_t>(all) && at < a.n_pages) a.ring[in_ring(at)] = id[u];
-                }
+                for (int u = 0; u < kPagesAhead; ++u)
+                    if (i0 + u * THREADS < n_pages) a.ring[in_ring(count + given + i0 + u * THREADS)] = id[u];
             }
             given += static_cast<int64_t>(all);
         }
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(Plan a, int32_t write_row
         my_need += need_before;
         const int64_t need_first = served[1];                  // where this tile's pages begin
         const bool ok = s < a.n_seq && my_rows <= static_cast<u64>(a.T) && my_need <= static_cast<u64>(there);
-        sums[tid] = static_cast<int64_t>(my_need);
+        sums[tid] = up_to_int(my_need);
         const int n_ok = __syncthreads_count(ok);              // they are the tile's first ones
         if (tid == n_ok - 1) {
             served[0] = my_rows;
@@ -187,8 +189,8 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(Plan a, int32_t write_row
             for (int u = 0; u < kPagesAhead; ++u) {
                 const int64_t i = i0 + u * THREADS;
                 if (i >= need_end) break;
-                const int32_t j = above(sums, n_ok, i);
-                a.table[static_cast<int64_t>(s0 + j) * a.table_pages + pages0[j] + (i - (j > 0 ? sums[j - 1] : need_before))] = id[u];
+                const int32_t j = above(sums, n_ok, static_cast<int32_t>(i));
+                a.table[static_cast<int64_t>(s0 + j) * a.table_pages + pages0[j] + (i - (j > 0 ? sums[j - 1] : need_first))] = id[u];
             }
         }
         rows_before += static_cast<int64_t>(all_rows);
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(Plan a)
     const int32_t *v = here ? starts : a.row_start;
     int32_t s = 0, n = 0, end = 0;
     if (i < v[a.n_seq]) {
-        s = above(v, a.n_seq, i) - 1;
+        s = above(v, a.n_seq, static_cast<int32_t>(i)) - 1;
         n = v[s + 1] - v[s];
         end = here ? ends[s] : a.length_out[s];
         if (!a.order) o = static_cast<int32_t>(i) - v[s];
