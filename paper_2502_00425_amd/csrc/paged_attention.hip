@@ -10,9 +10,11 @@
 // Both split the slots of a sequence into pieces where there are too few work-groups otherwise; the pieces' partial
 // results (unnormalised sums, maximum, denominator, fp32) meet in paged_combine_kernel.
 //
-// Sequences that begin with the same tokens (mquant_paged_attention_shared) are walked by the same kernels in two parts: the rows of a group lie
-// behind one another, so its shared slots are those of one sequence with all the group's rows (Part::kPrefix), read once for
-// them; the slots behind the prefix are walked sequence by sequence (Part::kSuffix).  All pieces of both parts meet in shared_combine_kernel.
+// Sequences that begin with the same tokens (mquant_paged_attention_shared) are walked by the same kernels.  Where they have few rows, in two parts:
+// the rows of a group lie behind one another, so its shared slots are those of one sequence with all the group's rows
+// (Part::kPrefix), read once for them; the slots behind the prefix are walked sequence by sequence (Part::kSuffix), by work-groups of the same
+// launch; all pieces of both parts meet in shared_combine_kernel.  Where every sequence fills work-groups by itself the parts would only
+// cost their partial results: then each is walked as a whole, its shared pages by the first sequence's table (Part::kWhole).
 #include <climits>
 #include <cmath>
 
@@ -52,7 +54,8 @@ constexpr int kAhead = 4;                  // LDS fragment reads in flight ahead
 // factor matters), under one of the maxima's own they would be up to 2^(1/8) apart.  No product is contracted into an addition here (-ffp-contract=off).
 constexpr float kLazy = 8.0f;
 
-enum class Part { kAll, kPrefix, kSuffix };
+enum class Part { kAll, kPrefix, kSuffix, kWhole };
+constexpr bool in_parts(Part p) { return p == Part::kPrefix || p == Part::kSuffix; }
 
 // Pieces of a part in a call with shared prefixes: at most `split` of them, `piece` slots each, for sequences of few queries and for the others.
 struct Pieces {
@@ -133,7 +136,7 @@ __device__ __forceinline__ int32_t prefix_of(const Step &a, int32_t g)
 struct Place {
     int32_t table = 0;                     // whose line of the table has its pages ..
     int32_t prefix = 0;                    // .. kPrefix: slots to walk; kSuffix: slots ahead of those to walk
-    int32_t front = 0, front_table = 0;    // kSuffix: whole pages of the prefix, and whose line has them
+    int32_t front = 0, front_table = 0;    // kSuffix, kWhole: whole pages of the prefix, and whose line has them
 };
 
 template <Part P>
@@ -145,10 +148,10 @@ __device__ __forceinline__ Place place_of(const Step &a, int32_t seq)
         at.table = group_begin(a, seq);
         at.prefix = prefix_of(a, seq);
     }
-    if constexpr (P == Part::kSuffix) {
-        const int32_t g = a.n_groups > 0 ? uniform(sequence_of_row(a.group_start, a.n_groups, seq)) : -1;
-        at.prefix = prefix_of(a, g);
-        at.front = at.prefix >> a.c.page_shift;
+    if constexpr (P == Part::kSuffix || P == Part::kWhole) {
+        const int32_t g = a.n_groups > 0 ? uniform(sequence_of_row(a.group_start, a.n_groups, seq)) : -1, prefix = prefix_of(a, g);
+        if (P == Part::kSuffix) at.prefix = prefix;
+        at.front = prefix >> a.c.page_shift;
         at.front_table = g < 0 ? seq : group_begin(a, g);
     }
     return at;
@@ -161,7 +164,7 @@ template <Part P>
 __device__ __forceinline__ uint32_t block_at(const Step &a, const Place &place, int32_t kvh, int32_t block)
 {
     const int32_t shift = a.c.page_shift - 4, last = (a.c.table_pages << shift) - 1, b = block < last ? block : last;
-    const int32_t line = P == Part::kSuffix && (b >> shift) < place.front ? place.front_table : place.table;
+    const int32_t line = (P == Part::kSuffix || P == Part::kWhole) && (b >> shift) < place.front ? place.front_table : place.table;
     const int32_t id = a.c.table[static_cast<int64_t>(line) * a.c.table_pages + (b >> shift)];
     const uint32_t page = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.c.n_pages) ? id : 0;
     return (page * static_cast<uint32_t>(a.c.n_kv_heads) + kvh) * (1u << shift) + (b & ((1 << shift) - 1));
@@ -230,7 +233,7 @@ __device__ __forceinline__ void walk_few(const Step &a, int32_t block)
     }
     for (int32_t m0 = 0; m0 < M; m0 += 16 * NQ) {
         const int nq = M - m0 < 16 * NQ ? (M - m0 + 15) / 16 : NQ;
-        const bool split = P != Part::kAll || m0 + 16 * NQ <= a.few_stride;    // the others' slots are all in piece 0
+        const bool split = in_parts(P) || m0 + 16 * NQ <= a.few_stride;    // the others' slots are all in piece 0
         if (!split && piece > 0) return;
         // page ids, queries and positions are on their way together
         const int32_t begin = front + (split ? piece * a.piece : 0);           // slots, a multiple of kFewStep behind the front
@@ -421,7 +424,7 @@ __device__ __forceinline__ void walk_few(const Step &a, int32_t block)
                     for (int e = 0; e < 8; ++e) f[e] += share * sums[(w * 16 + qi) * kFewPitch + ch + e];
                 }
                 const int32_t row = rows.x + m / a.group, limit = lims[qi];
-                if constexpr (P != Part::kAll) {
+                if constexpr (in_parts(P)) {
                     if (limit >= begin) {                      // -1: nothing of this part is seen
                         const int64_t at = (static_cast<int64_t>(a.first_piece + piece) * a.T + row) * a.n_q + kvh * a.group + m % a.group;
                         *reinterpret_cast<v4f *>(a.part + at * kD + ch) = v4f{f[0], f[1], f[2], f[3]};
@@ -456,10 +459,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void paged_few_kernel(Step a)
     walk_few<NQ, Part::kAll>(a, blockIdx.x);
 }
 
-template <int NQ, bool PREFIX>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void shared_few_kernel(Step a)
+// Both parts where groups have few queries: work-groups of the prefixes ahead of the others.
+template <int NQ>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void shared_few_kernel(Step prefix, Step suffix, int32_t prefix_groups)
 {
-    walk_few<NQ, PREFIX ? Part::kPrefix : Part::kSuffix>(a, blockIdx.x);
+    const int32_t block = blockIdx.x;
+    if (block < prefix_groups) walk_few<NQ, Part::kPrefix>(prefix, block);
+    else walk_few<NQ, Part::kSuffix>(suffix, block - prefix_groups);
 }
 
 // ------------------------------------------------------------------------------------------------ chunks
@@ -801,9 +807,9 @@ __device__ __forceinline__ void walk_chunk(const Step &a, int32_t block, int32_t
     const float ref = m_ref * scale_log2e;
 
     // ---- lane = query, registers = head channels (4 consecutive per group)
-    const bool partial = P != Part::kAll || a.n_split > 1;
+    const bool partial = in_parts(P) || a.n_split > 1;
     const bool write = m < M && (!partial || limit >= t0 * kChunkK);
-    const int64_t at = (static_cast<int64_t>((P != Part::kAll ? a.first_piece : 0) + piece) * a.T + row) * a.n_q + head;
+    const int64_t at = (static_cast<int64_t>((in_parts(P) ? a.first_piece : 0) + piece) * a.T + row) * a.n_q + head;
     __half *out = a.o + row * a.ldo + static_cast<int64_t>(head) * kD;
     auto store4 = [&](int dt, int r4, const v4f &f, float inv_l) {
         if (partial) {
@@ -874,10 +880,24 @@ __global__ __launch_bounds__(KG * 256, 2) void paged_chunk_kernel(Step a, int32_
     walk_chunk<KG, Part::kAll>(a, blockIdx.x, xcds_per_kv);
 }
 
-template <int KG, bool PREFIX>
-__global__ __launch_bounds__(KG * 256, 2) void shared_chunk_kernel(Step a, int32_t xcds_per_kv)
+// Groups of many queries, sequences of few: the work-groups of the prefixes, bound by the matrix cores, share compute units with those behind
+// them, bound by the bytes of the cache.
+template <int NQ>
+__global__ __launch_bounds__(256, 2) void shared_both_kernel(Step prefix, Step suffix, int32_t prefix_groups, int32_t xcds_per_kv)
 {
-    walk_chunk<KG, PREFIX ? Part::kPrefix : Part::kSuffix>(a, blockIdx.x, xcds_per_kv);
+    static_assert(kFewWaves == 4 && kFewLds == kChunkLds, "one kind of work-group");
+    const int32_t block = blockIdx.x;
+    if (block < prefix_groups) walk_chunk<1, Part::kPrefix>(prefix, block, xcds_per_kv);
+    else walk_few<NQ, Part::kSuffix>(suffix, block - prefix_groups);
+}
+
+// Sequences of many queries in parts, for steps that mix them with others.
+__global__ __launch_bounds__(256, 2) void shared_suffix_kernel(Step a, int32_t xcds_per_kv) { walk_chunk<1, Part::kSuffix>(a, blockIdx.x, xcds_per_kv); }
+
+template <int KG>
+__global__ __launch_bounds__(KG * 256, 2) void shared_whole_kernel(Step a, int32_t xcds_per_kv)
+{
+    walk_chunk<KG, Part::kWhole>(a, blockIdx.x, xcds_per_kv);
 }
 
 // ------------------------------------------------------------------------------------------------ pieces
@@ -982,11 +1002,30 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(Step a)
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + uniform(threadIdx.x >> 6);
     const int32_t row = static_cast<int32_t>(item / a.n_q), head = static_cast<int32_t>(item % a.n_q);
     if (row >= a.T) return;
+    // The row's sequence, its group and what they have, from starts that are on their way together where a wave holds them.
     const int32_t limit = limit_of(a, row);
-    const int32_t seq = uniform(sequence_of_row(a.row_start, a.c.n_seq, row));
-    if (seq < 0) return;
-    const int32_t g = a.n_groups > 0 ? uniform(sequence_of_row(a.group_start, a.n_groups, seq)) : -1;
-    const int32_t prefix = prefix_of(a, g);
+    int32_t seq, g, prefix;
+    int2 rows, group_rows = make_int2(0, 0);
+    if (a.c.n_seq < 64 && a.n_groups < 64) {
+        const int32_t start = a.row_start[lane < a.c.n_seq ? lane : a.c.n_seq], first = group_begin(a, lane < a.n_groups ? lane : a.n_groups),
+                      shared = prefix_of(a, lane < a.n_groups ? lane : -1);
+        seq = __builtin_popcountll(__ballot(lane <= a.c.n_seq && start <= row)) - 1;
+        if (seq < 0 || seq == a.c.n_seq) return;
+        auto start_of = [&](int32_t s) { return __builtin_amdgcn_readlane(start, s); };
+        auto inside = [&](int32_t b, int32_t e) { return make_int2(b > 0 ? b : 0, e < a.T ? e : a.T); };
+        rows = inside(start_of(seq), start_of(seq + 1));
+        g = __builtin_popcountll(__ballot(lane <= a.n_groups && first <= seq)) - 1;
+        if (g == a.n_groups) g = -1;
+        prefix = g < 0 ? 0 : __builtin_amdgcn_readlane(shared, g);
+        if (g >= 0) group_rows = inside(start_of(__builtin_amdgcn_readlane(first, g)), start_of(__builtin_amdgcn_readlane(first, g + 1)));
+    } else {
+        seq = uniform(sequence_of_row(a.row_start, a.c.n_seq, row));
+        if (seq < 0) return;
+        rows = rows_of(a, seq);
+        g = uniform(sequence_of_row(a.group_start, a.n_groups, seq));
+        prefix = prefix_of(a, g);
+        if (g >= 0) group_rows = rows_of<Part::kPrefix>(a, g);
+    }
     // pieces of n slots, as the kernel that took these queries cut them
     auto pieces = [&](const Pieces &by, const int2 &rows, int32_t n, bool suffix) {
         const bool few = by.few_alone || (!by.chunk_alone && (rows.y - rows.x) * a.group <= kFew);
@@ -996,8 +1035,8 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(Step a)
         return k < most ? k : most;
     };
     int32_t n_pre = 0;
-    if (g >= 0 && prefix > 0) n_pre = pieces(a.in_prefix, rows_of<Part::kPrefix>(a, g), limit < prefix ? limit + 1 : prefix, false);
-    const int32_t n = n_pre + pieces(a.in_suffix, rows_of(a, seq), limit + 1 - prefix, true);
+    if (prefix > 0) n_pre = pieces(a.in_prefix, group_rows, limit < prefix ? limit + 1 : prefix, false);
+    const int32_t n = n_pre + pieces(a.in_suffix, rows, limit + 1 - prefix, true);
     const int ch = (lane & 15) * 8, quarter = lane >> 4;
     const int64_t stride = static_cast<int64_t>(a.T) * a.n_q;
     float top = -INFINITY, den = 0.0f, f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -1145,7 +1184,8 @@ Plan make_plan(int32_t T, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t max_
 
 // What a call with shared prefixes launches.
 struct SharedPlan {
-    Plan pre, suf;
+    bool whole = false;
+    Plan pre, suf;                         // of the parts; whole: suf
     int32_t pre_split = 0, suf_split = 0;  // pieces a query has room for
     int64_t parts = 0;                     // partial results
     int64_t bytes() const { return parts == 0 ? 0 : ceil_div(parts * kD * 4, 256) * 256 + ceil_div(parts * 8, 256) * 256; }
@@ -1164,62 +1204,113 @@ SharedPlan make_shared_plan(int32_t T, int32_t n_seq, int32_t n_groups, int32_t 
 {
     SharedPlan p;
     if (T == 0 || n_seq == 0) return p;
-    if (n_groups > 0) {
+    const int64_t G = n_q / n_kv, queries = T * G, tiles = ceil_div(queries, kChunkQ);
+    // As a whole where sequences of about equal rows fill their work-groups nearly as well as their group would: 12 sequences of 29 to 150 rows x
+    // 28 heads behind 6001 slots 152 us in parts.
+    const int64_t each = ceil_div(queries, n_seq);
+    p.whole = max_rows > 0 && max_rows * G <= 2 * each && n_seq * ceil_div(each, kChunkQ) * 4 <= tiles * 5;
+    if (p.whole) {
+        p.suf.chunk = true;
+        const int64_t kv = static_cast<int64_t>(max_prefix) + max_suffix;
+        plan_pieces(p.suf, T, n_seq, n_q, n_kv, T, kv < 0x7fffffc0 ? static_cast<int32_t>(kv) : 0x7fffffc0);
+        // that counts a tile more for every sequence: two key groups also where the tiles of equal rows leave a compute unit to each
+        // (252 work-groups, 103 tiles: 148 us with one group, which then has nobody beside it)
+        if (p.suf.chunk_split == 1 && n_seq * ceil_div(each, kChunkQ) * n_kv * 21 <= kNumCU * 20) p.suf.chunk_two = true;
+        p.suf_split = p.suf.chunk_split > 1 ? p.suf.chunk_split : 0;
+    } else {
         // one kernel for all groups, by the rows that they have on average
-        p.pre.chunk = ceil_div(T, n_groups) * (n_q / n_kv) > kFew;
+        p.pre.chunk = ceil_div(T, n_groups) * G > kFew;
         p.pre.few = !p.pre.chunk;
-        plan_pieces(p.pre, T, n_groups, n_q, n_kv, T, max_prefix);
+        if (p.pre.few) {
+            plan_pieces(p.pre, T, n_groups, n_q, n_kv, T, max_prefix);
+        } else {
+            // a work-group to a compute unit, whose other half is for the slots behind the prefixes
+            p.pre.chunk_tiles = static_cast<int32_t>(n_groups == 1 ? tiles : queries / kChunkQ + n_groups);
+            const int64_t items = static_cast<int64_t>(p.pre.chunk_tiles) * n_kv, slot_tiles = ceil_div(max_prefix > 0 ? max_prefix : 1, kChunkK);
+            int64_t split = kNumCU / items;
+            if (split > slot_tiles / 2) split = slot_tiles / 2;
+            if (split > 1) {
+                const int64_t piece = ceil_div(slot_tiles, split);
+                p.pre.chunk_piece = static_cast<int32_t>(piece * kChunkK);
+                p.pre.chunk_split = static_cast<int32_t>(ceil_div(slot_tiles, piece));
+            }
+        }
         p.pre_split = split_of(p.pre);
+        p.suf = make_plan(T, n_seq, n_q, n_kv, max_rows, max_suffix);
+        p.suf_split = split_of(p.suf);
     }
-    p.suf = make_plan(T, n_seq, n_q, n_kv, max_rows, max_suffix);
-    p.suf_split = split_of(p.suf);
     p.parts = static_cast<int64_t>(T) * n_q * (p.pre_split + p.suf_split);
     return p;
 }
 
-template <int KG, Part P>
-auto chunk_kernel()
+// A kernel's arguments for its pieces.
+Step walking(Step a, const Plan &p, bool chunk)
 {
-    if constexpr (P == Part::kAll) return &paged_chunk_kernel<KG>;
-    else return &shared_chunk_kernel<KG, P == Part::kPrefix>;
+    a.n_split = chunk ? p.chunk_split : p.few_split;
+    a.piece = chunk ? p.chunk_piece : p.few_piece;
+    a.all = chunk ? !p.few : !p.chunk;
+    return a;
 }
 
-template <int NQ, Part P>
-auto few_kernel()
+// Work-groups of a chunk kernel, and how they are dealt to the XCDs.
+int64_t chunk_groups(const Plan &p, int32_t n_kv, int32_t &xcds_per_kv)
 {
-    if constexpr (P == Part::kAll) return &paged_few_kernel<NQ>;
-    else return &shared_few_kernel<NQ, P == Part::kPrefix>;
-}
-
-template <Part P>
-int launch_chunk(Step a, const Plan &p, hipStream_t stream)
-{
-    a.n_split = p.chunk_split;
-    a.piece = p.chunk_piece;
-    a.all = !p.few;
-    const int32_t n_kv = a.c.n_kv_heads, xcds_per_kv = 8 % n_kv == 0 ? 8 / n_kv : 0;
+    xcds_per_kv = 8 % n_kv == 0 ? 8 / n_kv : 0;
     const int64_t items = static_cast<int64_t>(p.chunk_tiles) * p.chunk_split;
-    const int64_t groups = xcds_per_kv > 0 ? 8 * ceil_div(items, xcds_per_kv) : items * n_kv;
+    return xcds_per_kv > 0 ? 8 * ceil_div(items, xcds_per_kv) : items * n_kv;
+}
+
+template <bool WHOLE>
+int launch_chunk(const Step &step, const Plan &p, hipStream_t stream)
+{
+    const Step a = walking(step, p, true);
+    int32_t xcds_per_kv;
+    const int64_t groups = chunk_groups(p, a.c.n_kv_heads, xcds_per_kv);
     const int key_groups = p.chunk_two ? 2 : 1;
     if (groups * key_groups * 256 > kMaxThreads) return MQUANT_ERR_UNSUPPORTED;
-    auto kern = p.chunk_two ? chunk_kernel<2, P>() : chunk_kernel<1, P>();
+    auto kern = p.chunk_two ? paged_chunk_kernel<2> : paged_chunk_kernel<1>;
+    if constexpr (WHOLE) kern = p.chunk_two ? shared_whole_kernel<2> : shared_whole_kernel<1>;
     static LdsLimit limits[2];
     if (const int st = limits[p.chunk_two].raise(reinterpret_cast<const void *>(kern), key_groups * kChunkLds); st != MQUANT_OK) return st;
     MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(key_groups * 256), key_groups * kChunkLds, stream, a, xcds_per_kv);
+    if (const int st = launch_status(); st != MQUANT_OK || p.chunk_split == 1) return st;
+    MQ_LAUNCH(paged_combine_kernel<true>, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(a.T) * a.n_q, 4))), dim3(256), 0, stream, a);
     return launch_status();
 }
 
-template <Part P>
-int launch_few(Step a, const Plan &p, int64_t walked, hipStream_t stream)
+// Both parts: the prefixes with the sequences of few queries, then those of many, then the join.
+int launch_parts(Step step, const SharedPlan &p, hipStream_t stream)
 {
-    a.n_split = p.few_split;
-    a.piece = p.few_piece;
-    a.all = !p.chunk;
-    const int64_t groups = walked * a.c.n_kv_heads * p.few_split;
-    auto kern = p.few_nq == 1 ? few_kernel<1, P>() : p.few_nq == 2 ? few_kernel<2, P>() : few_kernel<3, P>();
-    static LdsLimit limits[3];
-    if (const int st = limits[p.few_nq - 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
-    MQ_LAUNCH(kern, dim3(static_cast<unsigned>(groups)), dim3(kFewWaves * 64), kFewLds, stream, a);
+    const int32_t n_kv = step.c.n_kv_heads;
+    step.in_prefix = pieces_by(p.pre);
+    step.in_suffix = pieces_by(p.suf);
+    const Step a = walking(step, p.pre, p.pre.chunk);
+    step.first_piece = p.pre_split;
+    const Step b = walking(step, p.suf, false);
+    int32_t xcds_per_kv = 0;
+    const int64_t first = p.pre.chunk ? chunk_groups(p.pre, n_kv, xcds_per_kv) : static_cast<int64_t>(step.n_groups) * n_kv * p.pre.few_split;
+    const int64_t all = first + (p.suf.few ? static_cast<int64_t>(step.c.n_seq) * n_kv * p.suf.few_split : 0);
+    if (all > kMaxThreads / 256) return MQUANT_ERR_UNSUPPORTED;
+    const int32_t nq_pre = p.pre.few ? p.pre.few_nq : 1, nq_suf = p.suf.few ? p.suf.few_nq : 1, nq = nq_pre > nq_suf ? nq_pre : nq_suf;
+    static LdsLimit limits[7];
+    if (p.pre.chunk) {
+        auto kern = nq == 1 ? shared_both_kernel<1> : nq == 2 ? shared_both_kernel<2> : shared_both_kernel<3>;
+        if (const int st = limits[nq - 1].raise(reinterpret_cast<const void *>(kern), kChunkLds); st != MQUANT_OK) return st;
+        MQ_LAUNCH(kern, dim3(static_cast<unsigned>(all)), dim3(256), kChunkLds, stream, a, b, static_cast<int32_t>(first), xcds_per_kv);
+    } else {
+        auto kern = nq == 1 ? shared_few_kernel<1> : nq == 2 ? shared_few_kernel<2> : shared_few_kernel<3>;
+        if (const int st = limits[2 + nq].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
+        MQ_LAUNCH(kern, dim3(static_cast<unsigned>(all)), dim3(kFewWaves * 64), kFewLds, stream, a, b, static_cast<int32_t>(first));
+    }
+    if (const int st = launch_status(); st != MQUANT_OK) return st;
+    if (p.suf.chunk) {
+        const int64_t groups = chunk_groups(p.suf, n_kv, xcds_per_kv);
+        if (groups * 256 > kMaxThreads) return MQUANT_ERR_UNSUPPORTED;
+        if (const int st = limits[6].raise(reinterpret_cast<const void *>(shared_suffix_kernel), kChunkLds); st != MQUANT_OK) return st;
+        MQ_LAUNCH(shared_suffix_kernel, dim3(static_cast<unsigned>(groups)), dim3(256), kChunkLds, stream, walking(step, p.suf, true), xcds_per_kv);
+        if (const int st = launch_status(); st != MQUANT_OK) return st;
+    }
+    MQ_LAUNCH(shared_combine_kernel, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(step.T) * step.n_q, 4))), dim3(256), 0, stream, step);
     return launch_status();
 }
 
@@ -1285,31 +1376,20 @@ extern "C" int mquant_paged_attention(const void *q, int64_t ldq, const mquant_p
 
     Step a = step_of(q, ldq, cache, row_start, pos, o, ldo, T, n_q_heads, workspace, p.few_part + p.chunk_part);
     a.few_stride = p.few_stride;
-    if (p.chunk) {
-        if (const int st = launch_chunk<Part::kAll>(a, p, stream); st != MQUANT_OK) return st;
-        if (p.chunk_split > 1) {
-            a.n_split = p.chunk_split;
-            a.piece = p.chunk_piece;
-            a.all = !p.few;
-            MQ_LAUNCH(paged_combine_kernel<true>, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * n_q_heads, 4))), dim3(256), 0,
-                      stream, a);
-            if (const int st = launch_status(); st != MQUANT_OK) return st;
-        }
-    }
-    if (p.few) {
-        a.part += p.chunk_part * kD;
-        a.part_ml += p.chunk_part;
-        if (const int st = launch_few<Part::kAll>(a, p, cache->n_seq, stream); st != MQUANT_OK) return st;
-        if (p.few_split > 1) {
-            a.n_split = p.few_split;
-            a.piece = p.few_piece;
-            a.all = !p.chunk;
-            const int64_t queries = static_cast<int64_t>(cache->n_seq) * n_kv * p.few_stride;
-            MQ_LAUNCH(paged_combine_kernel<false>, dim3(static_cast<unsigned>(ceil_div(queries, 4))), dim3(256), 0, stream, a);
-            return launch_status();
-        }
-    }
-    return MQUANT_OK;
+    if (p.chunk)
+        if (const int st = launch_chunk<false>(a, p, stream); st != MQUANT_OK) return st;
+    if (!p.few) return MQUANT_OK;
+    a.part += p.chunk_part * kD;
+    a.part_ml += p.chunk_part;
+    a = walking(a, p, false);
+    const int64_t units = static_cast<int64_t>(cache->n_seq) * n_kv;
+    auto kern = p.few_nq == 1 ? paged_few_kernel<1> : p.few_nq == 2 ? paged_few_kernel<2> : paged_few_kernel<3>;
+    static LdsLimit limits[3];
+    if (const int st = limits[p.few_nq - 1].raise(reinterpret_cast<const void *>(kern), kFewLds); st != MQUANT_OK) return st;
+    MQ_LAUNCH(kern, dim3(static_cast<unsigned>(units * p.few_split)), dim3(kFewWaves * 64), kFewLds, stream, a);
+    if (const int st = launch_status(); st != MQUANT_OK || p.few_split == 1) return st;
+    MQ_LAUNCH(paged_combine_kernel<false>, dim3(static_cast<unsigned>(ceil_div(units * p.few_stride, 4))), dim3(256), 0, stream, a);
+    return launch_status();
 }
 
 extern "C" int64_t mquant_paged_attention_shared_workspace_bytes(int32_t T, int32_t n_seq, int32_t n_groups, int32_t n_q_heads,
@@ -1318,6 +1398,7 @@ extern "C" int64_t mquant_paged_attention_shared_workspace_bytes(int32_t T, int3
 {
     if (const int st = check_sizes(T, n_seq, n_q_heads, n_kv_heads, head_dim, max_rows, max_suffix); st != MQUANT_OK) return st;
     if (const int st = check_sizes(T, n_groups, n_q_heads, n_kv_heads, head_dim, max_rows, max_prefix); st != MQUANT_OK) return st;
+    if (n_groups == 0) return make_plan(T, n_seq, n_q_heads, n_kv_heads, max_rows, max_suffix).bytes();
     return make_shared_plan(T, n_seq, n_groups, n_q_heads, n_kv_heads, max_rows, max_prefix, max_suffix).bytes();
 }
 
@@ -1331,9 +1412,11 @@ extern "C" int mquant_paged_attention_shared(const void *q, int64_t ldq, const m
     if (const int st = check_sizes(T, cache->n_seq, n_q_heads, n_kv, cache->head_dim, max_rows, max_suffix); st != MQUANT_OK) return st;
     if (const int st = check_sizes(T, n_groups, n_q_heads, n_kv, cache->head_dim, max_rows, max_prefix); st != MQUANT_OK) return st;
     if (T == 0 || cache->n_seq == 0) return MQUANT_OK;
+    if (n_groups == 0)
+        return mquant_paged_attention(q, ldq, cache, row_start, pos, o, ldo, T, n_q_heads, max_rows, max_suffix, workspace, workspace_bytes, stream_);
     if (const int st = check_rows(q, ldq, o, ldo, row_start, pos, n_q_heads); st != MQUANT_OK) return st;
-    if (n_groups > 0 && (!group_start || !prefix)) return MQUANT_ERR_NULL;
-    if (n_groups > 0 && (!aligned_to(group_start, 4) || !aligned_to(prefix, 4))) return MQUANT_ERR_ALIGNMENT;
+    if (!group_start || !prefix) return MQUANT_ERR_NULL;
+    if (!aligned_to(group_start, 4) || !aligned_to(prefix, 4)) return MQUANT_ERR_ALIGNMENT;
     const int32_t slots = cache->table_pages * cache->page_size;
     auto in_table = [&](int32_t bound) { return bound > 0 && bound < slots ? bound : slots; };
     SharedPlan p = make_shared_plan(T, cache->n_seq, n_groups, n_q_heads, n_kv, max_rows, in_table(max_prefix), in_table(max_suffix));
@@ -1342,23 +1425,12 @@ extern "C" int mquant_paged_attention_shared(const void *q, int64_t ldq, const m
         p = make_shared_plan(T, cache->n_seq, n_groups, n_q_heads, n_kv, max_rows, max_prefix > 0 ? max_prefix : slots,
                              max_suffix > 0 ? max_suffix : slots);
     const int64_t need = p.bytes();
-    if (!workspace || workspace_bytes < need) return MQUANT_ERR_WORKSPACE;
-    if (!aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
-    hipStream_t stream = static_cast<hipStream_t>(stream_);
-
+    if (need > 0 && (!workspace || workspace_bytes < need)) return MQUANT_ERR_WORKSPACE;
+    if (need > 0 && !aligned_to(workspace, 256)) return MQUANT_ERR_ALIGNMENT;
     Step a = step_of(q, ldq, cache, row_start, pos, o, ldo, T, n_q_heads, workspace, p.parts);
     a.group_start = group_start;
     a.prefix = prefix;
     a.n_groups = n_groups;
-    a.in_prefix = pieces_by(p.pre);
-    a.in_suffix = pieces_by(p.suf);
-    int st = MQUANT_OK;
-    if (p.pre.chunk) st = launch_chunk<Part::kPrefix>(a, p.pre, stream);
-    if (p.pre.few) st = launch_few<Part::kPrefix>(a, p.pre, n_groups, stream);
-    a.first_piece = p.pre_split;
-    if (st == MQUANT_OK && p.suf.chunk) st = launch_chunk<Part::kSuffix>(a, p.suf, stream);
-    if (st == MQUANT_OK && p.suf.few) st = launch_few<Part::kSuffix>(a, p.suf, cache->n_seq, stream);
-    if (st != MQUANT_OK) return st;
-    MQ_LAUNCH(shared_combine_kernel, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * n_q_heads, 4))), dim3(256), 0, stream, a);
-    return launch_status();
+    hipStream_t stream = static_cast<hipStream_t>(stream_);
+    return p.whole ? launch_chunk<true>(a, p.suf, stream) : launch_parts(a, p, stream);
 }

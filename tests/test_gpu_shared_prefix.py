@@ -59,6 +59,8 @@ STEPS = {                      # groups, query heads, kv heads, page
     "few_queries_each_part": ([(200, [(1, 230), (2, 260)])], 16, 16, 16),
     "drafts": ([(513, [(5, 600), (3, 520), (4, 517)])], 28, 4, 16),
     "questions": ([(700, [(150, 900), (33, 733), (60, 800)])], 28, 4, 16),
+    "long_questions": ([(3000, [(40, 3100), (35, 3050)])], 28, 4, 64),
+    "many_rows_each": ([(257, [(220, 480), (200, 460), (210, 900)]), (100, [(180, 300), (190, 290)])], 16, 16, 16),
     "mixed_lengths": ([(256, [(1, 300), (100, 400), (2, 258), (0, 256), (1, 2000)])], 7, 1, 32),
     "groups": ([(64, [(1, 70), (1, 90)]), (333, [(3, 400)]), (0, [(1, 30), (2, 5)]), (1000, [(1, 1001), (40, 1100), (1, 1003)])], 12, 2, 16),
     "inside_the_prefix": ([(500, [(1, 500), (3, 260), (1, 1), (2, 503), (40, 480)])], 28, 4, 16),
@@ -197,10 +199,14 @@ def test_seeded_sweep(mq):
 def test_routes(mq):
     """Which kernels the groups' rows and the bounds choose."""
     from kernel_trace import kernels
-    for name, want in (("decode", ["shared_few_kernel<2, true>", "shared_few_kernel<1, false>", "shared_combine_kernel"]),
-                       ("many", ["shared_chunk_kernel<2, true>", "shared_few_kernel<1, false>", "shared_combine_kernel"]),
-                       ("questions", ["shared_chunk_kernel<2, true>", "shared_chunk_kernel<2, false>", "shared_few_kernel<3, false>", "shared_combine_kernel"])):
+    for name, bounds, want in (("decode", True, ["shared_few_kernel<2>", "shared_combine_kernel"]),
+                               ("many", True, ["shared_both_kernel<1>", "shared_combine_kernel"]),
+                               ("drafts", True, ["shared_both_kernel<3>", "shared_combine_kernel"]),
+                               ("questions", True, ["shared_whole_kernel<2>"]),
+                               ("long_questions", True, ["shared_whole_kernel<2>", "paged_combine_kernel<true>"]),
+                               ("questions", False, ["shared_both_kernel<3>", "shared_suffix_kernel", "shared_combine_kernel"]),
+                               ("mixed_lengths", True, ["shared_both_kernel<3>", "shared_suffix_kernel", "shared_combine_kernel"])):
         st = make_shared(np.random.default_rng(10), *STEPS[name], poison=False)
         args = args_of(mq, st)
-        names = kernels(lambda: mq.paged_attention_shared(*args, *bounds_of(st)))
-        assert [n for n in names if n.startswith("shared")] == want, (name, names)
+        names = kernels(lambda: mq.paged_attention_shared(*args, *(bounds_of(st) if bounds else ())))
+        assert [n for n in names if n.startswith(("shared", "paged"))] == want, (name, names)
