@@ -760,8 +760,9 @@ int64_t mquant_sample_workspace_bytes(int32_t rows, int32_t V);
  * With S the kept weights' sum, the token is the first one in the order of the vocabulary up to which the kept weights add to more
  * than u * S.  Its log-probability is (l - m) / t - ln S.  Temperatures that are not above 0 take the first token of the ranking,
  * with log-probability 0.
- * Weights are computed in double and summed as whole multiples of 2^-43, so that results do not depend on how the work is split;
- * a token with a weight below 2^-44 is never drawn.
+ * Weights are computed in double, off by 2^-37 of themselves at most, and summed as whole numbers of 2^-43 of the largest weight of a
+ * part of the row, so that the order in which threads add cannot change a result; of tokens with weights of about 2^-43 and less, some can
+ * count as nothing.
  *   logits_dev      : fp16 or fp32 (type) [rows, V], ld >= V elements apart; aligned to the type.  -inf and NaN are tokens that
  *                     cannot be chosen; where +inf occurs, only such tokens can.  Up to 15 bytes before and behind a row are
  *                     read (within the 16-byte blocks that hold it) and not used.

@@ -1,9 +1,9 @@
 // The next token of every row of logits by temperature, top-k, top-p and min-p from a given random number, for gfx950.
 //
 // Token i has the weight w = 2^-x, x = (m - l) log2(e) / t >= 0; ranked by logit, the kept tokens are a front of the ranking, and
-// which token is drawn is a question of sums of weights.  Weights are formed in double (off by 2^-44 of themselves) and summed as whole
-// multiples of 2^-43: such sums do not depend on their order, so that atomics in LDS and any split of the work give the same
-// token.  2^20 tokens of weight 1 are 2^63.
+// which token is drawn is a question of sums of weights.  Weights are formed in double (off by 2^-38.7 of themselves) and summed as whole
+// multiples of 2^-43: such sums do not depend on their order, so that atomics in LDS give the same token every time.  2^20 tokens of
+// weight 1 are 2^63.  Parts of a row are summed against their own largest logit and put together by its weight.
 //
 // Nothing is sorted but a short list.  tile_kernel, a work-group to 16 KiB of a row, takes from every piece of 64 blocks of 16 bytes its
 // largest logit and, as the row's settings ask, the weight of every piece or the tokens and weights of the tile by bins of the logit.
@@ -24,14 +24,13 @@ using namespace mquant;
 
 namespace {
 
-
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxTokens = 1 << 20;
 constexpr int kBins = 1024;                // of walk_row
 constexpr int kCoarse = 256;               // bins of a tile: 1/4 of x wide, the last one has all that is left
 constexpr int kTileThreads = 256, kTileBlocks = 4, kTilePieces = kTileThreads / 64 * kTileBlocks;
 constexpr int kMaxPieces = ((kMaxTokens + 6) / 4 + kTileThreads * kTileBlocks - 1) / (kTileThreads * kTileBlocks) * kTilePieces;    // fp32, tiles filled up
-constexpr int kShort = kThreads / 16;      // tokens of a list up to which each is compared with all others, by 16 lanes
+constexpr int kShort = 256;                // tokens of a list up to which each is compared with all others
 constexpr int kList = 2048;                // tokens that are sorted at a time, two to a thread
 constexpr u64 kNone = ~0ull;
 constexpr int kIndexBits = 24;             // of a rank: logit, then number of the token
@@ -107,10 +106,14 @@ __device__ __forceinline__ Shared &lds()
 }
 
 // ---- a row's logits: the 16-byte blocks that hold it, from the aligned one in which it begins
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
 template <typename E>
 struct Row {
     static constexpr int kPer = 16 / sizeof(E);
-    const uint4 *block;
+    // in so many words memory: an address that went through a whole number is taken for one that may be in LDS, and a load from it
+    // waits for LDS too
+    const __attribute__((address_space(1))) v4u *block;
     int32_t skip, n_blocks, V;             // elements of the first block ahead of the row
     bool only_inf;                         // where +inf occurs, it counts as 0 and everything else as nothing
 
@@ -118,11 +121,11 @@ struct Row {
     {
         const uintptr_t p = reinterpret_cast<uintptr_t>(static_cast<const E *>(a.logits) + row * a.ld);
         skip = static_cast<int32_t>((p & 15) / sizeof(E));
-        block = reinterpret_cast<const uint4 *>(p & ~static_cast<uintptr_t>(15));
+        block = (const __attribute__((address_space(1))) v4u *)(p & ~static_cast<uintptr_t>(15));
         n_blocks = (skip + V + kPer - 1) / kPer;
     }
 
-    __device__ __forceinline__ uint4 load(int32_t b) const { return block[b < n_blocks ? b : n_blocks - 1]; }
+    __device__ __forceinline__ v4u load(int32_t b) const { return block[b < n_blocks ? b : n_blocks - 1]; }
 
     // Token number of element e of block b; outside [0, V): not of the row.
     __device__ __forceinline__ int32_t token(int32_t b, int e) const { return b * kPer + e - skip; }
@@ -130,13 +133,13 @@ struct Row {
     __device__ __forceinline__ float value(float l) const { return !only_inf ? l : l == INFINITY ? 0.0f : NAN; }
 
     // The logit of a token that is in reach already.
-    __device__ __forceinline__ float logit(int32_t token) const { return value(static_cast<float>(reinterpret_cast<const E *>(block)[token + skip])); }
+    __device__ __forceinline__ float logit(int32_t token) const { return value(static_cast<float>(((const __attribute__((address_space(1))) E *)block)[token + skip])); }
 
     // The logits of block b, NaN for what is not of the row.
-    __device__ __forceinline__ void read(const uint4 &raw, int32_t b, float (&l)[kPer]) const
+    __device__ __forceinline__ void read(const v4u &raw, int32_t b, float (&l)[kPer]) const
     {
         union {
-            uint4 u;
+            v4u u;
             E e[kPer];
         } x;
         x.u = raw;
@@ -312,7 +315,7 @@ __device__ __forceinline__ u64 target_of(float p, u64 sum)
 // What to do with the tokens of four blocks that `is` names by their logit: f(logit, token).  Found for all of them first, done one by one, so
 // that the code of f is there once.
 template <typename E, typename P, typename F>
-__device__ __forceinline__ void each_of(const Row<E> &row, const uint4 (&raw)[4], const int32_t (&b)[4], P is, F f)
+__device__ __forceinline__ void each_of(const Row<E> &row, const v4u (&raw)[4], const int32_t (&b)[4], P is, F f)
 {
     constexpr int kPer = Row<E>::kPer;
     uint32_t hits = 0;
@@ -338,7 +341,7 @@ __device__ __forceinline__ void each_token(const Row<E> &row, P is, F f)
 {
 #pragma unroll 1
     for (int32_t b0 = threadIdx.x; b0 < row.n_blocks; b0 += kThreads * 4) {
-        uint4 raw[4];
+        v4u raw[4];
         int32_t b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -373,7 +376,9 @@ __device__ __noinline__ void sort_list(int n)
     for (int k = 2; k <= size; k <<= 1)
 #pragma unroll 1
         for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
+            // up to a distance of 64 a wave's pairs are its own 128 numbers
+            if (j > 64 || (j == 64 && k > 128) || k == 2) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             const int t = threadIdx.x, i = ((t & ~(j - 1)) << 1) | (t & (j - 1));
             static_assert(kList == 2 * kThreads, "pairs of a thread");
             if (t < size >> 1) {
@@ -452,72 +457,131 @@ __device__ __forceinline__ u64 rescaled(u64 sum, float l, const Scale &sc)
     return static_cast<u64>(rint(static_cast<double>(sum) * sc.weight(l)));
 }
 
-// Sum over the 16 lanes of a row, for all of them: by pairs of a quad, then by mirrored halves of the row.
-__device__ __forceinline__ u64 row_sum(u64 x)
+// For each of the list's n <= kShort tokens the number of those that come ahead of it, by numbers of which every lane of a wave holds four
+// (the largest: takes no part): a wave compares 16 tokens with all, whose numbers its lanes 0 .. 15 hold in `mine`.
+template <typename N>
+__device__ __forceinline__ void count_ahead(const N (&held)[kShort / 64], N mine, int n, uint32_t *ahead)
 {
-    x += moved<0xb1, 0xf>(x, u64{0});
-    x += moved<0x4e, 0xf>(x, u64{0});
-    x += moved<0x141, 0xf>(x, u64{0});
-    x += moved<0x140, 0xf>(x, u64{0});
-    return x;
+    static_assert(kShort == kWaves * 16, "tokens of a wave");
+    const int t0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 16, lane = threadIdx.x & 63;
+    if (t0 >= n) return;
+    uint32_t count = 0;
+#pragma unroll 2
+    for (int j = 0; j < 16; ++j) {
+        const N target = from_lane(mine, j);
+        uint32_t c = 0;
+#pragma unroll
+        for (int g = 0; g < kShort / 64; ++g)
+            if (g * 64 < n) c += __builtin_popcountll(__ballot(held[g] < target));
+        count = lane == j ? c : count;
+    }
+    if (lane < 16 && t0 + lane < n) ahead[t0 + lane] = count;
 }
 
-// Which of the list's n <= kShort tokens is drawn: each is compared with all, by 16 lanes next to each other.  (256 tokens by 4 lanes each
-// took 29000 cycles for 220, which is the throughput of LDS; sorted they take half of that.)
+// Which of the list's n <= kShort tokens is drawn.  Their places in the ranking and then, of the kept ones, along the vocabulary are counted by all
+// waves, not sorted (220 tokens of 64 rows of 150001: 25 us for the kernel, sorted 32).  The rest is the first wave's, four tokens a lane,
+// without barriers: an instruction that all 16 waves run takes the work-group 16 cycles, one wave's 4.
 __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double min_w, float u, u64 all_mass, bool all_known, const Scale &sc)
 {
     Shared &s = lds();
-    constexpr u64 kTokenMask = (1u << kIndexBits) - 1;
-    const int tid = threadIdx.x, me = tid >> 4, part = tid & 15;
-    const bool mine = me < n;
-    const u64 rank = mine ? s.list.rank[me] : kNone;
-    const double w = mine ? sc.weight(logit_of(rank)) : 0.0;
-    const u64 weight = whole(w);
-    if (mine && part == 0) s.list.sum[me] = weight;
-    if (tid < 2) s.found[tid] = 0;
+    constexpr uint32_t kTokenMask = (1u << kIndexBits) - 1;
+    constexpr int kHeld = kShort / 64;
+    uint32_t *place = s.count, *kept_token = s.count + kShort;
+    static_assert(kBins >= 2 * kShort, "room for both");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int target = wave * 16 + (lane & 15);                // of this lane of 16, when the wave compares
+    u64 held[kHeld];
+    if (wave * 16 < n) {
+#pragma unroll
+        for (int g = 0; g < kHeld; ++g) held[g] = g * 64 + lane < n ? s.list.rank[g * 64 + lane] : kNone;
+        count_ahead(held, target < n ? s.list.rank[target] : kNone, n, place);
+    }
     __syncthreads();
-    u64 before = 0, ahead = 0;             // weight and number of the tokens ahead of mine
-    if (mine) {
-#pragma unroll 2
-        for (int j = part; j < n; j += 16) {
-            const u64 other = s.list.rank[j], sum = s.list.sum[j];
-            if (other < rank) {
-                ++ahead;
-                before += sum;
+    u64 sum = 0, weight[kHeld];
+    uint32_t n_kept = 0;
+    if (wave == 0) {
+        // ---- along the ranking: token lane + 64 g goes to its place, then a lane has four places next to each other
+        u64 *by_place = s.list.sum;
+#pragma unroll
+        for (int g = 0; g < kHeld; ++g) {
+            weight[g] = 0;
+            const int i = g * 64 + lane;
+            if (g * 64 < n && i < n) {
+                weight[g] = sc.weigh(logit_of(held[g]));
+                by_place[place[i]] = weight[g];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        u64 w[kHeld], here = 0;
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) here += w[e] = lane * kHeld + e < n ? by_place[lane * kHeld + e] : 0;
+        u64 ahead = wave_scan(here) - here;
+        if (k <= 0 || k > n) k = n;
+        u64 mass = kNone;                                      // a kept token has less ahead of it
+        if (p < 1.0f) {
+            u64 of_k = 0;
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e) of_k += lane * kHeld + e < k ? w[e] : 0;
+            mass = target_of(p, all_known ? all_mass : wave_sum(of_k));
+        }
+        u64 at = ahead;
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) {
+            n_kept += __builtin_popcountll(__ballot(lane * kHeld + e < k && at < mass));
+            at += w[e];
+        }
+        if (min_w > 0.0) {                                     // the kept ones are the ranking's first ones by weight too
+            uint32_t heavy = 0;
+#pragma unroll
+            for (int g = 0; g < kHeld; ++g)
+                if (g * 64 < n) heavy += __builtin_popcountll(__ballot(g * 64 + lane < n && sc.weight(logit_of(held[g])) >= min_w));
+            n_kept = heavy < n_kept ? heavy : n_kept;
+            n_kept = n_kept > 1 ? n_kept : 1;
+        }
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) sum += lane * kHeld + e < static_cast<int>(n_kept) ? w[e] : 0;
+        sum = wave_sum(sum);
+#pragma unroll
+        for (int g = 0; g < kHeld; ++g) {
+            const int i = g * 64 + lane;
+            if (g * 64 < n && i < n) {
+                const bool kept = place[i] < n_kept;
+                kept_token[i] = kept ? static_cast<uint32_t>(held[g]) & kTokenMask : ~0u;
             }
         }
     }
-    ahead = row_sum(ahead);
-    if (p < 1.0f) before = row_sum(before);
-    bool kept = mine && (k <= 0 || ahead < static_cast<u64>(k));
-    if (p < 1.0f) {
-        if (!all_known) {
-            if (kept && part == 0) atomicAdd(&s.found[0], weight);
-            __syncthreads();
-            all_mass = s.found[0];
-        }
-        kept = kept && before < target_of(p, all_mass);
-    }
-    kept = kept && (w >= min_w || ahead == 0);
     __syncthreads();
-    if (mine && part == 0) {
-        s.list.sum[me] = kept ? weight : 0;
-        if (kept) atomicAdd(&s.found[1], weight);
+    if (wave * 16 < n) {
+        uint32_t tokens[kHeld];
+#pragma unroll
+        for (int g = 0; g < kHeld; ++g) tokens[g] = g * 64 + lane < n ? kept_token[g * 64 + lane] : ~0u;
+        count_ahead(tokens, target < n ? kept_token[target] : ~0u, n, place);
     }
     __syncthreads();
-    const u64 sum = s.found[1];
-    const u64 pass = drawn_at(u, sum);
-    u64 at = 0;
-    if (kept) {
-#pragma unroll 2
-        for (int j = part; j < n; j += 16) {
-            const u64 other = s.list.rank[j], w_j = s.list.sum[j];
-            if ((other & kTokenMask) < (rank & kTokenMask)) at += w_j;
-        }
-    }
-    at = row_sum(at);
     Drawn d;
-    if (kept && part == 0 && at <= pass && at + weight > pass) d = {rank, sum};
+    if (wave != 0) return d;
+    // ---- the kept ones along the vocabulary, as above; the others come last
+    u64 *by_place = s.list.sum;
+    uint32_t *who = kept_token;
+#pragma unroll
+    for (int g = 0; g < kHeld; ++g) {
+        const int i = g * 64 + lane;
+        if (g * 64 < n && i < n && place[i] < n_kept) {        // the others come behind all kept ones
+            by_place[place[i]] = weight[g];
+            who[place[i]] = i;
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    u64 w[kHeld], here = 0;
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) here += w[e] = lane * kHeld + e < static_cast<int>(n_kept) ? by_place[lane * kHeld + e] : 0;
+    u64 at = wave_scan(here) - here;
+    const u64 pass = drawn_at(u, sum);
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) {
+        if (at <= pass && at + w[e] > pass) d = {s.list.rank[who[lane * kHeld + e]], sum};
+        at += w[e];
+    }
     return d;
 }
 
@@ -877,9 +941,9 @@ __global__ __launch_bounds__(kTileThreads) void tile_kernel(Args a)
     const int32_t piece0 = tile * kTilePieces + wave * kTileBlocks;
     auto block = [&](int j) {
         const int32_t b = (piece0 + j) * 64 + lane;
-        return row.block[b < row.n_blocks ? b : row.n_blocks - 1];
+        return row.load(b);
     };
-    uint4 b0 = block(0), b1 = block(1), b2 = block(2), b3 = block(3);
+    v4u b0 = block(0), b1 = block(1), b2 = block(2), b3 = block(3);
     const Settings set(a, r);
     const Ask ask = set.ask();
     mass[tid] = 0;
@@ -894,7 +958,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_kernel(Args a)
         top = wave_max(top);
         tile_top = fmaxf(tile_top, top);
         if (lane == 0) a.piece_max[r * a.pieces + piece0 + j] = top;
-        const uint4 next = b1;
+        const v4u next = b1;
         b1 = b2;
         b2 = b3;
         b3 = b0;
@@ -1102,7 +1166,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
             const int32_t n_todo = s.n_pieces;
 #pragma unroll 1
             for (int32_t i0 = wave; i0 < n_todo; i0 += kWaves * 4) {
-                uint4 raw[4];
+                v4u raw[4];
                 int32_t b[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
