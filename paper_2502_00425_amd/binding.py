@@ -807,8 +807,14 @@ class Rotary:
             for i, f in enumerate(freq):
                 self.struct.freq[i] = f
         self.struct.scale = scale
-        self.n_axes = self.struct.n_axes
-        self.fast = (self.address, self.n_axes)
+
+    @property
+    def n_axes(self) -> int:
+        return self.struct.n_axes
+
+    @property
+    def fast(self):
+        return self.address, self.struct.n_axes
 
 
 def _axes(pos, rot: Rotary, T: int, what: str) -> None:
@@ -943,6 +949,8 @@ def sample(logits, temperature, top_k, top_p, min_p, u, out=None, logprob=None, 
     kind = _FLOATS.get(logits.dtype)
     if kind is None:
         raise MQuantError(ERR_UNSUPPORTED, f"logits: expected float16 or float32, got {logits.dtype}")
+    if logits.dim() != 2:
+        raise MQuantError(ERR_BAD_SHAPE, f"logits: expected [rows, V], got {tuple(logits.shape)}")
     rows, V = logits.shape
     if out is None:
         out = torch.empty(rows, dtype=torch.int32, device=logits.device)

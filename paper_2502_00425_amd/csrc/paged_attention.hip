@@ -999,7 +999,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(Step a)
 __global__ __launch_bounds__(256) void shared_combine_kernel(Step a)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + uniform(threadIdx.x >> 6);
+    const int64_t item = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 4 + uniform(threadIdx.x >> 6);
     const int32_t row = static_cast<int32_t>(item / a.n_q), head = static_cast<int32_t>(item % a.n_q);
     if (row >= a.T) return;
     // The row's sequence, its group and what they have, from starts that are on their way together where a wave holds them.
@@ -1204,6 +1204,10 @@ SharedPlan make_shared_plan(int32_t T, int32_t n_seq, int32_t n_groups, int32_t 
 {
     SharedPlan p;
     if (T == 0 || n_seq == 0) return p;
+    // of longer ones a launch does not hold all pieces of both parts; what is behind its pieces the last one takes
+    constexpr int32_t kLongest = 1 << 27;
+    max_prefix = max_prefix < kLongest ? max_prefix : kLongest;
+    max_suffix = max_suffix < kLongest ? max_suffix : kLongest;
     const int64_t G = n_q / n_kv, queries = T * G, tiles = ceil_div(queries, kChunkQ);
     // As a whole where sequences of about equal rows fill their work-groups nearly as well as their group would: 12 sequences of 29 to 150 rows x
     // 28 heads behind 6001 slots 152 us in parts.
@@ -1211,8 +1215,7 @@ SharedPlan make_shared_plan(int32_t T, int32_t n_seq, int32_t n_groups, int32_t 
     p.whole = max_rows > 0 && max_rows * G <= 2 * each && n_seq * ceil_div(each, kChunkQ) * 4 <= tiles * 5;
     if (p.whole) {
         p.suf.chunk = true;
-        const int64_t kv = static_cast<int64_t>(max_prefix) + max_suffix;
-        plan_pieces(p.suf, T, n_seq, n_q, n_kv, T, kv < 0x7fffffc0 ? static_cast<int32_t>(kv) : 0x7fffffc0);
+        plan_pieces(p.suf, T, n_seq, n_q, n_kv, T, max_prefix + max_suffix);
         // that counts a tile more for every sequence: two key groups also where the tiles of equal rows leave a compute unit to each
         // (252 work-groups, 103 tiles: 148 us with one group, which then has nobody beside it)
         if (p.suf.chunk_split == 1 && n_seq * ceil_div(each, kChunkQ) * n_kv * 21 <= kNumCU * 20) p.suf.chunk_two = true;
@@ -1290,7 +1293,9 @@ int launch_parts(Step step, const SharedPlan &p, hipStream_t stream)
     int32_t xcds_per_kv = 0;
     const int64_t first = p.pre.chunk ? chunk_groups(p.pre, n_kv, xcds_per_kv) : static_cast<int64_t>(step.n_groups) * n_kv * p.pre.few_split;
     const int64_t all = first + (p.suf.few ? static_cast<int64_t>(step.c.n_seq) * n_kv * p.suf.few_split : 0);
-    if (all > kMaxThreads / 256) return MQUANT_ERR_UNSUPPORTED;
+    int32_t suf_xcds_per_kv = 0;
+    const int64_t longer = p.suf.chunk ? chunk_groups(p.suf, n_kv, suf_xcds_per_kv) : 0;
+    if (all > kMaxThreads / 256 || longer > kMaxThreads / 256) return MQUANT_ERR_UNSUPPORTED;
     const int32_t nq_pre = p.pre.few ? p.pre.few_nq : 1, nq_suf = p.suf.few ? p.suf.few_nq : 1, nq = nq_pre > nq_suf ? nq_pre : nq_suf;
     static LdsLimit limits[7];
     if (p.pre.chunk) {
@@ -1304,13 +1309,15 @@ int launch_parts(Step step, const SharedPlan &p, hipStream_t stream)
     }
     if (const int st = launch_status(); st != MQUANT_OK) return st;
     if (p.suf.chunk) {
-        const int64_t groups = chunk_groups(p.suf, n_kv, xcds_per_kv);
-        if (groups * 256 > kMaxThreads) return MQUANT_ERR_UNSUPPORTED;
         if (const int st = limits[6].raise(reinterpret_cast<const void *>(shared_suffix_kernel), kChunkLds); st != MQUANT_OK) return st;
-        MQ_LAUNCH(shared_suffix_kernel, dim3(static_cast<unsigned>(groups)), dim3(256), kChunkLds, stream, walking(step, p.suf, true), xcds_per_kv);
+        MQ_LAUNCH(shared_suffix_kernel, dim3(static_cast<unsigned>(longer)), dim3(256), kChunkLds, stream, walking(step, p.suf, true), suf_xcds_per_kv);
         if (const int st = launch_status(); st != MQUANT_OK) return st;
     }
-    MQ_LAUNCH(shared_combine_kernel, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(step.T) * step.n_q, 4))), dim3(256), 0, stream, step);
+    // all rows of all heads may be more threads than a dimension of a launch has
+    constexpr int64_t kAcross = kMaxThreads / 256 / 2;
+    const int64_t joins = ceil_div(static_cast<int64_t>(step.T) * step.n_q, 4);
+    MQ_LAUNCH(shared_combine_kernel, dim3(static_cast<unsigned>(joins < kAcross ? joins : kAcross), static_cast<unsigned>(ceil_div(joins, kAcross))),
+              dim3(256), 0, stream, step);
     return launch_status();
 }
 
