@@ -627,7 +627,8 @@ int mquant_lora_apply(const void *x_dev, int64_t ldx, const int32_t *perm_dev, c
 /*
  * DEVICE.  The bookkeeping of a step: which rows the sequences get, their pages, positions and slots, all from arrays in
  * device memory, so that a captured loop needs no host.  A sequence with rows[s] < 0 has ended: its pages behind the first
- * shared[s] go to the end of the free pages, and its length becomes 0.  Then, in the order of the sequences,
+ * shared[s] go to the end of the free pages, and its length becomes 0 (one that is to begin behind its shared pages again gets their length
+ * from the program).  Then, in the order of the sequences,
  *     r[s]    = rows[s], or 0 where rows[s] <= 0 or length[s] + rows[s] is more than the table holds
  *     need[s] = ceil((length[s] + r[s]) / page_size) - ceil(length[s] / page_size)
  * and a sequence is served while r[0] + .. + r[s] <= T and need[0] + .. + need[s] <= the free pages there are (those given back in

@@ -207,3 +207,68 @@ def test_replays_and_streams(mq):
             want = call()
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_lists_of_every_length(mq, dtype):
+    """As many kept tokens as a way of drawing takes at most, one less and one more: by their number, by their weight and as equals."""
+    rng = np.random.default_rng(11)
+    V = 9000
+    lengths = [1, 2, 15, 16, 17, 63, 64, 65, 127, 129, 255, 256, 257, 511, 513, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4097]
+    for kind in ("steps", "equal ahead", "near"):
+        x = np.full((len(lengths), V), -12.0)
+        for r, n in enumerate(lengths):
+            ahead = rng.permutation(V)[:n]
+            x[r, ahead] = {"steps": 4 - 0.002 * np.arange(n), "equal ahead": np.full(n, 2.0), "near": rng.uniform(1.9, 2.1, n)}[kind]
+            x[r] += {"steps": 1, "equal ahead": 0, "near": 0}[kind] * rng.uniform(0, 1e-3, V)
+        x = x.astype(np.float16 if dtype == torch.float16 else np.float32)
+        n, u = np.array(lengths), rng.random(len(lengths), dtype=np.float32)
+        check(mq, x, 1.0, n, 1.0, 0.0, u, dtype, kind)
+        check(mq, x, 1.0, n, 0.9, 0.0, u, dtype, kind + " top-p")
+        check(mq, x, 1.0, n + 5, 1.0, 0.01, u, dtype, kind + " min-p")
+        check(mq, x, 1.0, 0, 1.0, 0.0001, u, dtype, kind + " min-p alone")
+        check(mq, x, 0.5, 0, 0.97, 0.0, u, dtype, kind + " top-p alone")
+        check(mq, x, 0.5, 0, 0.99, 0.2, u, dtype, kind + " top-p and min-p")
+        check(mq, x, 1.0, n, 0.99, 0.0, NEXT, dtype, kind + " the last")
+
+
+def test_kept_tokens_without_weight(mq):
+    """Top-k keeps tokens whose weight is nothing beside the first ones: they hold no part of the interval, wherever they lie."""
+    x = np.full((8, 700), -60000.0, dtype=np.float16)
+    x[:, 300], x[:, 500], x[:, 20] = 5.0, 4.0, 4.5
+    u = np.array([0, 0.1, 0.3, 0.4, 0.5, 0.9, 0.99, NEXT], dtype=np.float32)
+    for k in (2, 3, 4, 50, 200, 600):
+        check(mq, x, 1.0, k, 1.0, 0.0, u)
+        check(mq, x, 1.0, k, 0.9999, 0.0, u)
+
+
+def test_scratch_of_a_larger_call_with_anything_in_it(mq):
+    rng = np.random.default_rng(12)
+    n = len(SETTINGS)
+    ws = torch.empty(mq.sample_workspace_bytes(64, 70000), dtype=torch.uint8, device="cuda")
+    cols = [dev(np.asarray(c, d)) for c, d in zip(zip(*SETTINGS), (np.float32, np.int32, np.float32, np.float32))]
+    for V in (5, 3000, 50000):
+        x, u = dev(logits_of(rng, n, V, torch.float32)), dev(rng.random(n, dtype=np.float32))
+        want = mq.sample(x, *cols, u)
+        for fill in (0, 0x7f, 0xff):
+            ws.fill_(fill)
+            got = mq.sample(x, *cols, u, workspace=ws)
+            assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_rows_beyond_32_bits(mq):
+    """2100 rows of 2^20 logits: the last ones are drawn as they are alone; what is behind them is no row."""
+    rng = np.random.default_rng(13)
+    V, rows = 1 << 20, 2100
+    x = torch.zeros((rows, V), dtype=torch.float16, device="cuda")
+    some = dev(logits_of(rng, 3, V, torch.float16))
+    x[-3:] = some
+    u = dev(rng.random(rows, dtype=np.float32))
+    for args in ((None, None, None, None), (None, 50, None, None), (None, None, 0.6, None)):
+        full = lambda c, d, n: None if c is None else torch.full((n,), c, dtype=d, device="cuda")
+        cols = lambda n: [full(c, d, n) for c, d in zip(args, (torch.float32, torch.int32, torch.float32, torch.float32))]
+        token, logprob = mq.sample(x, *cols(rows), u)
+        alone = mq.sample(some, *cols(3), u[-3:].contiguous())
+        assert torch.equal(token[-3:], alone[0]) and torch.equal(logprob[-3:], alone[1])
+        if args[1] is None and args[2] is None:
+            assert token[:-3].cpu().numpy().tolist() == np.floor(u[:-3].cpu().numpy().astype(np.float64) * V).astype(int).tolist()

@@ -210,3 +210,21 @@ def test_routes(mq):
         args = args_of(mq, st)
         names = kernels(lambda: mq.paged_attention_shared(*args, *(bounds_of(st) if bounds else ())))
         assert [n for n in names if n.startswith(("shared", "paged"))] == want, (name, names)
+
+
+@pytest.mark.parametrize("name", ["decode_in_a_page", "questions", "many_rows_each"])
+def test_pages_beyond_32_bits(mq, name):
+    """The same step with its pages at the end of a pool of more than 2^31 values each: the same bits."""
+    st = make_shared(np.random.default_rng(21), *STEPS[name])
+    args, bounds = args_of(mq, st), bounds_of(st)
+    want = mq.paged_attention_shared(*args, *bounds)
+    _, hkv, page, _ = st["kp"].shape
+    far = (1 << 31) // (hkv * page * D) + 1
+    pools = []
+    for a in ("kp", "vp"):
+        pool = torch.empty((far + len(st[a]), hkv, page, D), dtype=torch.float16, device="cuda")
+        pool[far:] = dev(st[a])
+        pools.append(pool)
+    table = np.where(st["table"] >= 0, st["table"] + far, st["table"]).astype(np.int32)
+    cache = mq.PagedCache(*pools, dev(table))
+    assert torch.equal(mq.paged_attention_shared(args[0], cache, *args[2:], *bounds), want)
