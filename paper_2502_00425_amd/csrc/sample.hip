@@ -135,8 +135,8 @@ struct Row {
     // The logit of a token that is in reach already.
     __device__ __forceinline__ float logit(int32_t token) const { return value(static_cast<float>(((const __attribute__((address_space(1))) E *)block)[token + skip])); }
 
-    // The logits of block b, NaN for what is not of the row.
-    __device__ __forceinline__ void read(const v4u &raw, int32_t b, float (&l)[kPer]) const
+    // The logits of a block that is all of the row's.
+    __device__ __forceinline__ void read(const v4u &raw, float (&l)[kPer]) const
     {
         union {
             v4u u;
@@ -145,6 +145,26 @@ struct Row {
         x.u = raw;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) l[e] = value(static_cast<float>(x.e[e]));
+    }
+
+    // Block b with NaN for what is not of the row.
+    __device__ __forceinline__ v4u blank(const v4u &raw, int32_t b) const
+    {
+        union {
+            v4u u;
+            E e[kPer];
+        } x;
+        x.u = raw;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (static_cast<uint32_t>(token(b, e)) >= static_cast<uint32_t>(V)) x.e[e] = static_cast<E>(NAN);
+        return x.u;
+    }
+
+    // The logits of block b, NaN for what is not of the row.
+    __device__ __forceinline__ void read(const v4u &raw, int32_t b, float (&l)[kPer]) const
+    {
+        read(raw, l);
         if (b == 0 || b >= n_blocks - 1) {
 #pragma unroll
             for (int e = 0; e < kPer; ++e)
@@ -194,6 +214,24 @@ __device__ __forceinline__ float wave_max(float x)
     with(moved<0x142, 0xa>(o, 0u));
     with(moved<0x143, 0xc>(o, 0u));
     return float_of(__builtin_amdgcn_readlane(o, 63));
+}
+
+// The same of four logits a lane at once: the largest of number i in the lanes 16 i .. 16 i + 15.
+__device__ __forceinline__ float four_max(float x0, float x1, float x2, float x3)
+{
+    auto swapped = [](float a, float b, auto swap) {           // exchanges parts of a wave, then the larger of both
+        const auto r = swap(__float_as_uint(a), __float_as_uint(b));
+        return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    };
+    auto halves = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane32_swap(a, b, false, false); };
+    auto rows = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane16_swap(a, b, false, false); };
+    uint32_t o = order_of(fmaxf(swapped(swapped(x0, x2, halves), swapped(x1, x3, halves), rows), -INFINITY));
+    auto with = [&](uint32_t y) { o = o > y ? o : y; };
+    with(moved<0xb1, 0xf>(o, 0u));                             // of a pair, a quad, by mirrored halves and rows
+    with(moved<0x4e, 0xf>(o, 0u));
+    with(moved<0x141, 0xf>(o, 0u));
+    with(moved<0x140, 0xf>(o, 0u));
+    return float_of(o);
 }
 
 __device__ __forceinline__ u64 rank_of(float l, int32_t token)
@@ -934,7 +972,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_kernel(Args a)
     __shared__ float tops[kTileThreads / 64];
     constexpr int kPer = Row<E>::kPer;
     static_assert(kTileBlocks == 4, "blocks of a lane, by name");
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t r = blockIdx.x / a.tiles;
     const int32_t tile = blockIdx.x % a.tiles;
     const Row<E> row(a, r);
@@ -948,35 +986,41 @@ __global__ __launch_bounds__(kTileThreads) void tile_kernel(Args a)
     const Ask ask = set.ask();
     mass[tid] = 0;
     count[tid] = 0;
-    float tile_top = -INFINITY;
+    if (piece0 == 0 || (piece0 + kTileBlocks) * 64 >= row.n_blocks) {          // the row's first and last blocks
 #pragma unroll 1
-    for (int j = 0; j < kTileBlocks; ++j) {
+        for (int j = 0; j < kTileBlocks; ++j) {
+            const v4u now = row.blank(b0, (piece0 + j) * 64 + lane);
+            b0 = b1;
+            b1 = b2;
+            b2 = b3;
+            b3 = now;
+        }
+    }
+    auto largest = [&](const v4u &raw) {
         float l[kPer], top = -INFINITY;
-        row.read(b0, (piece0 + j) * 64 + lane, l);
+        row.read(raw, l);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) top = fmaxf(top, l[e]);
-        top = wave_max(top);
-        tile_top = fmaxf(tile_top, top);
-        if (lane == 0) a.piece_max[r * a.pieces + piece0 + j] = top;
-        const v4u next = b1;
-        b1 = b2;
-        b2 = b3;
-        b3 = b0;
-        b0 = next;
-    }
+        return top;
+    };
+    const float tops4 = four_max(largest(b0), largest(b1), largest(b2), largest(b3));
+    if ((lane & 15) == 0) a.piece_max[r * a.pieces + piece0 + (lane >> 4)] = tops4;
+    float tile_top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kTileBlocks; ++j) tile_top = fmaxf(tile_top, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(tops4), j * 16)));
     if (ask == Ask::kNothing) return;
     if (ask == Ask::kSums) {               // of the wave's four pieces together
         const Scale sc(set.t, tile_top);
         double w = 0.0;
 #pragma unroll 1
-        for (int j = 0; j < kTileBlocks; ++j) {
-            float l[kPer];
-            row.read(b0, (piece0 + j) * 64 + lane, l);
+        for (int j = 0; j < kTileBlocks; j += 2) {
+            float l[kPer], k[kPer];
+            row.read(b0, l);
+            row.read(b1, k);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) w += sc.weight(l[e]);
-            b0 = b1;
-            b1 = b2;
-            b2 = b3;
+            for (int e = 0; e < kPer; ++e) w += sc.weight(l[e]) + sc.weight(k[e]);
+            b0 = b2;
+            b1 = b3;
         }
         const u64 all = wave_sum(whole(w));
         if (lane == 0) {
@@ -994,7 +1038,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_kernel(Args a)
 #pragma unroll 1
     for (int j = 0; j < kTileBlocks; ++j) {
         float l[kPer];
-        row.read(b0, (piece0 + j) * 64 + lane, l);
+        row.read(b0, l);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             if (!there(l[e])) continue;
