@@ -283,6 +283,16 @@ struct Scale {
         return float_of(lo);
     }
 
+    // The same by a wave at once, 64 floats around where the bins' border is but for what is rounded.
+    __device__ __forceinline__ float least_near(int bin) const
+    {
+        const float near = static_cast<float>(bin + 1) / (-0.25f * bin_of);
+        const float l = float_of(order_of(fminf(fmaxf(near, -1e38f), 1e38f)) + (threadIdx.x & 63) - 32);
+        const uint64_t in = __ballot(coarse(l) <= bin);        // of the lanes from some one on
+        const int from = in != 0 ? __builtin_ctzll(in) : 0;
+        return from > 0 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), from)) : least(bin);
+    }
+
     __device__ double x(float l) const { return (static_cast<double>(m) - static_cast<double>(l)) * x_of; }
     // Falls with l, like the rank, whatever is rounded; the last bin has all that is left.
     __device__ int bin(float l) const { return static_cast<int>(fminf((m - l) * bin_of, static_cast<float>(kBins - 1))); }
@@ -390,9 +400,43 @@ __device__ __forceinline__ void each_token(const Row<E> &row, P is, F f)
     }
 }
 
+// What a row's work-group knows when its way is one of the functions below.  Those write the row's result themselves and get what they need through
+// memory: what is passed or kept around a call would be held in scratch memory by every call, also of rows that go another way.
+struct Known {
+    Settings set;
+    Scale sc;
+    float top;
+    double min_w;
+    int32_t k;
+    int base, end;                         // first coarse bin, and the one of the cut
+    u64 target;                            // of top-p alone
+    u64 all_mass;                          // weight of all tokens that can be chosen, 0: not known
+};
+
+__device__ __forceinline__ Known &known()
+{
+    __shared__ u64 room[(sizeof(Known) + 7) / 8];
+    return *reinterpret_cast<Known *>(room);
+}
+
+// The row's token and its log-probability.
+__device__ __forceinline__ void put_result(const Args &a, int64_t r, int32_t token, double logprob)
+{
+    a.token[r] = token;
+    if (a.logprob) a.logprob[r] = static_cast<float>(logprob);
+}
+
 // A thread's answer: the token that is drawn, by its rank, among kept ones of this weight; kNone: another thread has it.
 struct Drawn {
     u64 rank = kNone, sum = 0;
+
+    __device__ __forceinline__ void write(const Args &a, int64_t r, const Scale &sc) const
+    {
+        if (rank == kNone) return;
+        // the log-probability of a token among kept ones of this weight
+        put_result(a, r, static_cast<int32_t>(rank & ((1u << kIndexBits) - 1)),
+                -sc.x(logit_of(rank)) * 0.69314718055994530942 - log(static_cast<double>(sum) * 0x1p-43));
+    }
 };
 
 // ---- lists
@@ -495,49 +539,43 @@ __device__ __forceinline__ u64 rescaled(u64 sum, float l, const Scale &sc)
     return static_cast<u64>(rint(static_cast<double>(sum) * sc.weight(l)));
 }
 
-// For each of the list's n <= kShort tokens the number of those that come ahead of it, by numbers of which every lane of a wave holds four
-// (the largest: takes no part): a wave compares 16 tokens with all, whose numbers its lanes 0 .. 15 hold in `mine`.
+// For each of n <= kShort numbers in LDS, how many are less: `ahead`, zeros before (rows of 0 count none).  A lane holds one, and all waves have a share
+// of those that it is compared with, which every lane reads at once.
 template <typename N>
-__device__ __forceinline__ void count_ahead(const N (&held)[kShort / 64], N mine, int n, uint32_t *ahead)
+__device__ __forceinline__ void count_ahead(const N *v, int n, uint32_t *ahead)
 {
-    static_assert(kShort == kWaves * 16, "tokens of a wave");
-    const int t0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 16, lane = threadIdx.x & 63;
-    if (t0 >= n) return;
+    static_assert(kShort == 4 * 64 && kWaves == 16, "shares of a wave");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int log2 = n <= 64 ? 0 : n <= 128 ? 1 : 2, group = wave & ((1 << log2) - 1), part = wave >> log2;
+    const int t = group * 64 + lane, per = (n + (kWaves >> log2) - 1) >> (4 - log2), from = part * per, to = from + per < n ? from + per : n;
+    const N mine = t < n ? v[t] : 0;
     uint32_t count = 0;
-#pragma unroll 2
-    for (int j = 0; j < 16; ++j) {
-        const N target = from_lane(mine, j);
-        uint32_t c = 0;
-#pragma unroll
-        for (int g = 0; g < kShort / 64; ++g)
-            if (g * 64 < n) c += __builtin_popcountll(__ballot(held[g] < target));
-        count = lane == j ? c : count;
-    }
-    if (lane < 16 && t0 + lane < n) ahead[t0 + lane] = count;
+#pragma unroll 4
+    for (int j = from; j < to; ++j) count += v[j] < mine ? 1 : 0;
+    if (count > 0) atomicAdd(&ahead[t], count);
 }
 
 // Which of the list's n <= kShort tokens is drawn.  Their places in the ranking and then, of the kept ones, along the vocabulary are counted by all
-// waves, not sorted (220 tokens of 64 rows of 150001: 25 us for the kernel, sorted 32).  The rest is the first wave's, four tokens a lane,
+// waves, not sorted (220 tokens of 64 rows of 150001: 22 us for the kernel, sorted 32).  The rest is the first wave's, four tokens a lane,
 // without barriers: an instruction that all 16 waves run takes the work-group 16 cycles, one wave's 4.
 __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double min_w, float u, u64 all_mass, bool all_known, const Scale &sc)
 {
     Shared &s = lds();
     constexpr uint32_t kTokenMask = (1u << kIndexBits) - 1;
     constexpr int kHeld = kShort / 64;
-    uint32_t *place = s.count, *kept_token = s.count + kShort;
-    static_assert(kBins >= 2 * kShort, "room for both");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int target = wave * 16 + (lane & 15);                // of this lane of 16, when the wave compares
-    u64 held[kHeld];
-    if (wave * 16 < n) {
-#pragma unroll
-        for (int g = 0; g < kHeld; ++g) held[g] = g * 64 + lane < n ? s.list.rank[g * 64 + lane] : kNone;
-        count_ahead(held, target < n ? s.list.rank[target] : kNone, n, place);
-    }
+    uint32_t *place = s.coarse_count, *kept_place = s.count, *kept_token = s.count + kShort;
+    static_assert(kBins >= 2 * kShort && kCoarse >= kShort, "room for them");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (tid < kShort) place[tid] = kept_place[tid] = 0;
     __syncthreads();
+    count_ahead(s.list.rank, n, place);
+    __syncthreads();
+    u64 held[kHeld];
     u64 sum = 0, weight[kHeld];
     uint32_t n_kept = 0;
     if (wave == 0) {
+#pragma unroll
+        for (int g = 0; g < kHeld; ++g) held[g] = g * 64 + lane < n ? s.list.rank[g * 64 + lane] : kNone;
         // ---- along the ranking: token lane + 64 g goes to its place, then a lane has four places next to each other
         u64 *by_place = s.list.sum;
 #pragma unroll
@@ -589,12 +627,7 @@ __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double mi
         }
     }
     __syncthreads();
-    if (wave * 16 < n) {
-        uint32_t tokens[kHeld];
-#pragma unroll
-        for (int g = 0; g < kHeld; ++g) tokens[g] = g * 64 + lane < n ? kept_token[g * 64 + lane] : ~0u;
-        count_ahead(tokens, target < n ? kept_token[target] : ~0u, n, place);
-    }
+    count_ahead(kept_token, n, kept_place);
     __syncthreads();
     Drawn d;
     if (wave != 0) return d;
@@ -605,8 +638,8 @@ __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double mi
     for (int g = 0; g < kHeld; ++g) {
         const int i = g * 64 + lane;
         if (g * 64 < n && i < n && place[i] < n_kept) {        // the others come behind all kept ones
-            by_place[place[i]] = weight[g];
-            who[place[i]] = i;
+            by_place[kept_place[i]] = weight[g];
+            who[kept_place[i]] = i;
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -624,9 +657,16 @@ __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double mi
 }
 
 // The same for more tokens: sorted by rank, then the kept ones by their number.
-__device__ __noinline__ Drawn draw_sorted(int n, int32_t k, float p, double min_w, float u, u64 all_mass, bool all_known, Scale sc)
+__device__ __noinline__ void draw_sorted(const Args *args, int64_t r, int n)
 {
     Shared &s = lds();
+    const Known w = known();
+    const Scale &sc = w.sc;
+    const float p = w.set.p, u = w.set.u;
+    const double min_w = w.min_w;
+    const u64 all_mass = w.all_mass;
+    const bool all_known = all_mass > 0;
+    int32_t k = w.k;
     constexpr u64 kTokenMask = (1u << kIndexBits) - 1;
     const int i = threadIdx.x * 2;
     sort_list(n);
@@ -660,7 +700,7 @@ __device__ __noinline__ Drawn draw_sorted(int n, int32_t k, float p, double min_
     Drawn d;
     if (place == i) d = {r0, sum};
     if (place == i + 1) d = {r1, sum};
-    return d;
+    d.write(*args, r, sc);
 }
 
 // The piece in which the sum passes u's share of it, of `pieces` sums in s.piece, and the sum ahead of it, for all threads: s.found32[0],
@@ -700,17 +740,6 @@ __device__ __forceinline__ u64 pick_token(const Row<E> &row, int32_t b, const fl
 }
 
 // ---- long lists
-// What a row's work-group knows when it comes to them.
-struct Known {
-    Settings set;
-    Scale sc;
-    float top;
-    double min_w;
-    int32_t k;
-    int base, end;                         // first coarse bin, and the one of the cut
-    u64 target;                            // of top-p alone
-};
-
 // The rank of the last token that a cut keeps of the n tokens that `of` names by their logit, a run of the ranking: by rank the first `count` of them
 // (at least 1, at most all), and only those with less than `mass` of their weight before them (the first one has).  kept_mass: the weight of
 // those kept.
@@ -833,9 +862,11 @@ __device__ __forceinline__ u64 last_by_weight(const Scale &sc, double min_w)
 // Many tokens are kept, and the tiles have their weights by coarse bins: the last kept token, in the bin of the cut, then the tile in which the
 // sum passes u S, which is looked at token by token.
 template <typename E>
-__device__ __noinline__ Drawn draw_long(Args a, int64_t r, Known w)
+__device__ __noinline__ void draw_long(const Args *args, int64_t r)
 {
     Shared &s = lds();
+    const Args a = *args;
+    const Known w = known();
     const Row<E> row(a, r);
     const Scale &sc = w.sc;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -911,15 +942,17 @@ __device__ __noinline__ Drawn draw_long(Args a, int64_t r, Known w)
     pass = static_cast<u64>(static_cast<double>(pass - ahead) * (static_cast<double>(all) / static_cast<double>(s.piece[tile])));
     if (pass >= all) pass = all - 1;
     d = {pick_token(row, b, l, weight, at, pass), sum};
-    return d;
+    d.write(a, r, sc);
 }
 
 // The others (+inf among the logits, more tokens than a list holds by top-k or min-p alone), without the tiles' help: the last kept token
 // by parts of the whole row, then the kept weights along the vocabulary.
 template <typename E>
-__device__ __noinline__ Drawn draw_whole(Args a, int64_t r, Known w)
+__device__ __noinline__ void draw_whole(const Args *args, int64_t r)
 {
     Shared &s = lds();
+    const Args a = *args;
+    const Known w = known();
     Row<E> row(a, r);
     row.only_inf = w.top == INFINITY;
     const Scale &sc = w.sc;
@@ -952,7 +985,7 @@ __device__ __noinline__ Drawn draw_whole(Args a, int64_t r, Known w)
     Drawn d;
     u64 pass;
     const u64 sum = find_piece(pieces, w.set.u, pass);
-    if (tid >= 64) return d;
+    if (tid >= 64) return;
     const int32_t b = s.found32[0] * 64 + lane;
     float l[Row<E>::kPer];
     row.read(row.load(b), b, l);
@@ -960,7 +993,7 @@ __device__ __noinline__ Drawn draw_whole(Args a, int64_t r, Known w)
 #pragma unroll
     for (int e = 0; e < Row<E>::kPer; ++e) here += weight[e] = kept(l[e], row.token(b, e));
     d = {pick_token(row, b, l, weight, s.found[0] + wave_scan(here) - here, pass), sum};
-    return d;
+    d.write(a, r, sc);
 }
 
 // ---- what the tiles of a row find out
@@ -1062,16 +1095,10 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
 {
     Shared &s = lds();
     constexpr int kPer = Row<E>::kPer;
-    constexpr int32_t kTokenMask = (1 << kIndexBits) - 1;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t r = blockIdx.x;
     const Row<E> row(a, r);
     const float *piece_max = a.piece_max + r * a.pieces;
-    auto result = [&](int32_t token, double logprob) {
-        a.token[r] = token;
-        if (a.logprob) a.logprob[r] = static_cast<float>(logprob);
-    };
-
     // ---- what the tiles found out, on its way at once: to another L2 a trip takes more than a microsecond
     constexpr int kEarly = 4;
     const int32_t n_bins = a.tiles * kCoarse;
@@ -1092,7 +1119,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
     const Settings set(a, r);
     top = wave_max(top);
     if (top == -INFINITY) {
-        if (tid == 0) result(-1, -INFINITY);
+        if (tid == 0) put_result(a, r, -1, -INFINITY);
         return;
     }
     if (set.first()) {
@@ -1107,16 +1134,16 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
 #pragma unroll
         for (int i = kPer - 1; i >= 0; --i)
             if (l[i] == top) e = i;
-        if (lane == __builtin_ctzll(__ballot(e < kPer))) result(row.token(b, e), 0.0);
+        if (lane == __builtin_ctzll(__ballot(e < kPer))) put_result(a, r, row.token(b, e), 0.0);
         return;
     }
     const Ask ask = set.ask();
     const float p = set.p;
     Known w = {set, Scale(set.t, top == INFINITY ? 0.0f : top), top, set.min_p > 0.0f ? static_cast<double>(set.min_p) : 0.0, set.k, 0,
-               kCoarse - 1, 0};
+               kCoarse - 1, 0, 0};
     const Scale &sc = w.sc;
     const bool by_weight = w.min_w > 0.0 && !(p < 1.0f);       // min-p says by itself which tokens can be kept
-    Drawn d;
+    const Args *args = reinterpret_cast<const Args *>((const void *)__builtin_amdgcn_kernarg_segment_ptr());   // a, where it is
     if (ask == Ask::kSums && top < INFINITY) {
         // ---- the weights of four pieces each, then of the four pieces' tokens, against their own largest logit as the tile summed them: a
         // wave to a piece
@@ -1148,7 +1175,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
         }
         pass = static_cast<u64>(static_cast<double>(pass - s.found[0]) * (static_cast<double>(all) / static_cast<double>(s.piece[four])));
         if (pass >= all) pass = all - 1;
-        d = {pick_token(row, b, l, weight, ahead + up - here, pass), sum};
+        Drawn{pick_token(row, b, l, weight, ahead + up - here, pass), sum}.write(a, r, sc);
     } else if (top < INFINITY && (ask != Ask::kNothing || by_weight)) {
         // ---- tokens and weight by the row's coarse bins; the bin in which the ranking is cut
         const bool counted = ask == Ask::kCount || ask == Ask::kBoth, weighed = ask == Ask::kMass || ask == Ask::kBoth;
@@ -1187,18 +1214,13 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
                 w.end = bin_in(s.coarse_mass, [&](u64 all) { return w.target = target_of(p, all_mass = all); }, ahead);
             }
         }
-        // ---- the tokens up to there, where they are few: those up to this many quarters, the last float ahead of the next bin
-        float most = INFINITY;
-        if (w.end < kCoarse - 1 && w.base + w.end < 1 << 29) { // there coarse() stops
-            most = static_cast<float>(w.base + w.end + 1);
-            if (static_cast<int>(most) > w.base + w.end) most = most == 0.0f ? -0x1p-149f : __uint_as_float(__float_as_uint(most) + (most > 0.0f ? -1 : 1));
-        }
-        float least = -FLT_MAX;
+        // ---- the tokens up to there, where they are few: those with at least this logit
+        float least = w.end < kCoarse - 1 ? sc.least_near(w.base + w.end) : -FLT_MAX;
         if (by_weight) {                                       // what is rounded here lets a few more in
             const double x = fmax(-log2(static_cast<double>(set.min_p)), 0.0) * (1.0 + 0x1p-20) + 0x1p-20;
             least = fmaxf(least, static_cast<float>(static_cast<double>(top) - x / sc.x_of - fabs(static_cast<double>(top)) * 0x1p-22));
         }
-        auto can = [&](float l) { return l >= least && sc.quarters(l) <= most; };
+        auto can = [&](float l) { return l >= least; };
         uint32_t n = kList + 1;
         if (!counted || up_to_end <= kList || by_weight) {
             // the pieces that can have such a token, then a wave every 16th of them, four at a time
@@ -1224,17 +1246,21 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
             n = s.n;
             __syncthreads();
         }
-        if (n <= kShort) d = draw_short(n, w.k, p, w.min_w, set.u, all_mass, ask == Ask::kMass, sc);
-        else if (n <= kList) d = draw_sorted(n, w.k, p, w.min_w, set.u, all_mass, ask == Ask::kMass, sc);
-        else if (weighed) d = draw_long<E>(a, r, w);
-        else d = draw_whole<E>(a, r, w);
+        if (n <= kShort) {
+            draw_short(n, w.k, p, w.min_w, set.u, all_mass, ask == Ask::kMass, sc).write(a, r, sc);
+            return;
+        }
+        w.all_mass = all_mass;
+        if (tid == 0) known() = w;
+        __syncthreads();
+        if (n <= kList) draw_sorted(args, r, n);
+        else if (weighed) draw_long<E>(args, r);
+        else draw_whole<E>(args, r);
     } else {
-        d = draw_whole<E>(a, r, w);
+        if (tid == 0) known() = w;
+        __syncthreads();
+        draw_whole<E>(args, r);
     }
-    // the log-probability of a token among kept ones of this weight
-    if (d.rank != kNone)
-        result(static_cast<int32_t>(d.rank & kTokenMask),
-               -sc.x(logit_of(d.rank)) * 0.69314718055994530942 - log(static_cast<double>(d.sum) * 0x1p-43));
 }
 
 // Tiles of a row whose logits take `bytes` each, wherever in a block it begins.
