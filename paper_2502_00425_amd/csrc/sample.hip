@@ -32,6 +32,7 @@ constexpr int kTileThreads = 256, kTileBlocks = 4, kTilePieces = kTileThreads / 
 constexpr int kMaxPieces = ((kMaxTokens + 6) / 4 + kTileThreads * kTileBlocks - 1) / (kTileThreads * kTileBlocks) * kTilePieces;    // fp32, tiles filled up
 constexpr int kShort = 256;                // tokens of a list up to which each is compared with all others
 constexpr int kList = 2048;                // tokens that are sorted at a time, two to a thread
+constexpr int kBin = 8192;                 // tokens of the cut's bin that are held, where more than kList are kept
 constexpr u64 kNone = ~0ull;
 constexpr int kIndexBits = 24;             // of a rank: logit, then number of the token
 
@@ -93,10 +94,11 @@ struct Shared {
             uint32_t count[256];
         } digit;
     };
+    u64 bin[kBin];                         // tokens of the cut's bin, by their rank
     u64 room[kWaves];
     u64 found[2];
     uint32_t found32[2];
-    uint32_t n, n_pieces;
+    uint32_t n, n_pieces, n_bin, at_least;
 };
 
 __device__ __forceinline__ Shared &lds()
@@ -366,6 +368,8 @@ template <typename E, typename P, typename F>
 __device__ __forceinline__ void each_of(const Row<E> &row, const v4u (&raw)[4], const int32_t (&b)[4], P is, F f)
 {
     constexpr int kPer = Row<E>::kPer;
+    // by name: an array that the program indexes is given 16 KiB of LDS or scratch memory (50 best of 256 rows of 128000: 49 us, 37 by name)
+    const int32_t b0 = b[0], b1 = b[1], b2 = b[2], b3 = b[3];
     uint32_t hits = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -378,27 +382,52 @@ __device__ __forceinline__ void each_of(const Row<E> &row, const v4u (&raw)[4], 
     while (hits != 0) {
         const int h = __builtin_ctz(hits), i = h / kPer;
         hits &= hits - 1;
-        const int32_t token = row.token(i < 2 ? (i == 0 ? b[0] : b[1]) : i == 2 ? b[2] : b[3], h % kPer);
+        int32_t block = b0;
+        block = i == 1 ? b1 : block;
+        block = i == 2 ? b2 : block;
+        block = i == 3 ? b3 : block;
+        const int32_t token = row.token(block, h % kPer);
         f(row.logit(token), token);
     }
 }
 
 // The same for the whole row.
-template <typename E, typename P, typename F>
-__device__ __forceinline__ void each_token(const Row<E> &row, P is, F f)
-{
+template <typename E>
+struct InRow {
+    const Row<E> &row;
+
+    template <typename P, typename F>
+    __device__ __forceinline__ void each(P is, F f) const
+    {
 #pragma unroll 1
-    for (int32_t b0 = threadIdx.x; b0 < row.n_blocks; b0 += kThreads * 4) {
-        v4u raw[4];
-        int32_t b[4];
+        for (int32_t b0 = threadIdx.x; b0 < row.n_blocks; b0 += kThreads * 4) {
+            v4u raw[4];
+            int32_t b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            b[i] = b0 + i * kThreads;
-            raw[i] = row.load(b[i]);
+            for (int i = 0; i < 4; ++i) {
+                b[i] = b0 + i * kThreads;
+                raw[i] = row.load(b[i]);
+            }
+            each_of(row, raw, b, is, f);
         }
-        each_of(row, raw, b, is, f);
     }
-}
+};
+
+// And for the n tokens that LDS holds of the cut's bin.
+struct InBin {
+    int n;
+
+    template <typename P, typename F>
+    __device__ __forceinline__ void each(P is, F f) const
+    {
+        const u64 *rank = lds().bin;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const float l = logit_of(rank[i]);
+            if (is(l)) f(l, static_cast<int32_t>(rank[i] & ((1u << kIndexBits) - 1)));
+        }
+    }
+};
 
 // What a row's work-group knows when its way is one of the functions below.  Those write the row's result themselves and get what they need through
 // memory: what is passed or kept around a call would be held in scratch memory by every call, also of rows that go another way.
@@ -743,8 +772,8 @@ __device__ __forceinline__ u64 pick_token(const Row<E> &row, int32_t b, const fl
 // The rank of the last token that a cut keeps of the n tokens that `of` names by their logit, a run of the ranking: by rank the first `count` of them
 // (at least 1, at most all), and only those with less than `mass` of their weight before them (the first one has).  kept_mass: the weight of
 // those kept.
-template <typename E, typename F>
-__device__ __forceinline__ u64 cut_run(const Row<E> &row, const Scale &sc, F of, u64 n, u64 count, u64 mass, u64 &kept_mass)
+template <typename S, typename F>
+__device__ __forceinline__ u64 cut_run(const S &tokens, const Scale &sc, F of, u64 n, u64 count, u64 mass, u64 &kept_mass)
 {
     Shared &s = lds();
     const int tid = threadIdx.x;
@@ -759,7 +788,7 @@ __device__ __forceinline__ u64 cut_run(const Row<E> &row, const Scale &sc, F of,
             s.digit.count[tid] = 0;
         }
         __syncthreads();
-        each_token(row, of, [&](float l, int32_t token) {
+        tokens.each(of, [&](float l, int32_t token) {
             const u64 r = rank_of(l, token);
             if (r >> low >> 8 != prefix) return;
             atomicAdd(&s.digit.mass[r >> low & 255], sc.weigh(l));
@@ -794,7 +823,7 @@ __device__ __forceinline__ u64 cut_run(const Row<E> &row, const Scale &sc, F of,
     __syncthreads();
     if (tid == 0) s.n = 0;
     __syncthreads();
-    each_token(row, of, [&](float l, int32_t token) {
+    tokens.each(of, [&](float l, int32_t token) {
         if (rank_of(l, token) >> low == prefix) put(l, token);
     });
     __syncthreads();
@@ -810,8 +839,8 @@ __device__ __forceinline__ u64 cut_run(const Row<E> &row, const Scale &sc, F of,
 }
 
 // The same of a run that may be long: counted by kBins parts first, and the part of the cut is then the run.
-template <typename E, typename F, typename B>
-__device__ __forceinline__ u64 cut_by_parts(const Row<E> &row, const Scale &sc, F of, B part_of, u64 count, u64 mass, u64 &kept_mass)
+template <typename S, typename F, typename B>
+__device__ __forceinline__ u64 cut_by_parts(const S &tokens, const Scale &sc, F of, B part_of, u64 count, u64 mass, u64 &kept_mass)
 {
     Shared &s = lds();
     const int tid = threadIdx.x;
@@ -820,7 +849,7 @@ __device__ __forceinline__ u64 cut_by_parts(const Row<E> &row, const Scale &sc, 
     s.count[tid] = 0;
     if (tid == 0) s.found32[0] = 0;
     __syncthreads();
-    each_token(row, of, [&](float l, int32_t) {
+    tokens.each(of, [&](float l, int32_t) {
         const int at = part_of(l);
         atomicAdd(&s.count[at], 1u);
         atomicAdd(&s.mass[at], sc.weigh(l));
@@ -841,7 +870,7 @@ __device__ __forceinline__ u64 cut_by_parts(const Row<E> &row, const Scale &sc, 
     __syncthreads();
     const u64 c0 = s.found[0], w0 = s.found[1], n = s.found32[1];
     __syncthreads();
-    const u64 last = cut_run(row, sc, [&](float l) { return of(l) && part_of(l) == part; }, n, count - c0, mass > w0 ? mass - w0 : 0, kept_mass);
+    const u64 last = cut_run(tokens, sc, [&](float l) { return of(l) && part_of(l) == part; }, n, count - c0, mass > w0 ? mass - w0 : 0, kept_mass);
     kept_mass += w0;
     return last;
 }
@@ -869,7 +898,7 @@ __device__ __noinline__ void draw_long(const Args *args, int64_t r)
     const Known w = known();
     const Row<E> row(a, r);
     const Scale &sc = w.sc;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float p = w.set.p;
     const u64 *tile_mass = w.k > 0 ? a.tile_mass : a.tile_bins;
     __syncthreads();
@@ -882,14 +911,27 @@ __device__ __noinline__ void draw_long(const Args *args, int64_t r)
     }
     __syncthreads();
     u64 last = kNone, in_bin, target = w.target;
-    int bin = w.end;
+    int bin = w.end, held = -1;
+    uint32_t n_held = 0;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {                     // top-k, then top-p of the weight of its tokens
         if (pass == 0 ? w.k <= 0 : !(p < 1.0f)) continue;
         const u64 c0 = bin > 0 ? s.coarse_count[bin - 1] : 0, m0 = bin > 0 ? s.coarse_mass[bin - 1] : 0;
-        const float from = bin < kCoarse - 1 ? sc.least(w.base + bin) : -FLT_MAX, to = bin > 0 ? sc.least(w.base + bin - 1) : INFINITY;
-        const u64 by = cut_by_parts(row, sc, [&](float l) { return l >= from && l < to; }, [&](float l) { return sc.fine(l, w.base + bin); },
-                                    pass == 0 ? w.k - c0 : kNone, pass == 0 ? kNone : target - m0, in_bin);
+        const float from = bin < kCoarse - 1 ? sc.least_near(w.base + bin) : -FLT_MAX, to = bin > 0 ? sc.least_near(w.base + bin - 1) : INFINITY;
+        auto in = [&](float l) { return l >= from && l < to; };
+        if (tid == 0) s.n_bin = 0;
+        __syncthreads();
+        InRow<E>{row}.each(in, [&](float l, int32_t token) {
+            const uint32_t at = atomicAdd(&s.n_bin, 1u);
+            if (at < kBin) s.bin[at] = rank_of(l, token);
+        });
+        __syncthreads();
+        held = bin;
+        n_held = s.n_bin;
+        auto part = [&](float l) { return sc.fine(l, w.base + bin); };
+        const u64 count = pass == 0 ? w.k - c0 : kNone, mass = pass == 0 ? kNone : target - m0;
+        const u64 by = n_held <= kBin ? cut_by_parts(InBin{static_cast<int>(n_held)}, sc, in, part, count, mass, in_bin)
+                                      : cut_by_parts(InRow<E>{row}, sc, in, part, count, mass, in_bin);
         last = by < last ? by : last;
         if (pass == 0 && p < 1.0f) {
             target = target_of(p, m0 + in_bin);
@@ -909,19 +951,24 @@ __device__ __noinline__ void draw_long(const Args *args, int64_t r)
     const float lo_kept = logit_of(last);
     const int cut_at = sc.coarse(lo_kept) - w.base;
     bin = cut_at < kCoarse - 1 ? cut_at : kCoarse - 1;
-    const float above = bin > 0 ? sc.least(w.base + bin - 1) : INFINITY;
-    for (int32_t i = tid; i < a.tiles; i += kThreads) s.piece[i] = 0;
-    __syncthreads();
+    const float above = bin > 0 ? sc.least_near(w.base + bin - 1) : INFINITY;
+    static_assert(kCoarse == 4 * 64, "bins of a lane");
 #pragma unroll 1
-    for (int32_t i = tid; i < a.tiles * kCoarse; i += kThreads) {              // a wave: 64 bins of a tile
-        const float tile_top = a.tile_max[r * a.tiles + i / kCoarse];
-        const u64 m = tile_mass[r * a.tiles * kCoarse + i];
-        const u64 sum = wave_sum(m > 0 && i % kCoarse + sc.coarse(tile_top) - w.base < bin ? rescaled(m, tile_top, sc) : 0);
-        if (lane == 0 && sum > 0) atomicAdd(&s.piece[i / kCoarse], sum);
+    for (int32_t i = wave; i < a.tiles; i += kWaves) {         // a wave: a tile
+        const float tile_top = a.tile_max[r * a.tiles + i];
+        const int behind = bin - (sc.coarse(tile_top) - w.base) - lane * 4;
+        const u64 *m = tile_mass + (r * a.tiles + i) * kCoarse + lane * 4;
+        const u64 m0 = m[0], m1 = m[1], m2 = m[2], m3 = m[3];
+        const u64 sum = wave_sum((behind > 0 ? m0 : 0) + (behind > 1 ? m1 : 0) + (behind > 2 ? m2 : 0) + (behind > 3 ? m3 : 0));
+        if (lane == 0) s.piece[i] = sum > 0 ? rescaled(sum, tile_top, sc) : 0;
     }
-    each_token(row, [&](float l) { return l >= lo_kept && l < above; }, [&](float l, int32_t token) {
+    __syncthreads();
+    auto rest = [&](float l) { return l >= lo_kept && l < above; };
+    auto add = [&](float l, int32_t token) {
         if (rank_of(l, token) <= last) atomicAdd(&s.piece[(token + row.skip) / (Row<E>::kPer * kTileThreads * kTileBlocks)], sc.weigh(l));
-    });
+    };
+    if (held == bin && n_held <= kBin) InBin{static_cast<int>(n_held)}.each(rest, add);
+    else InRow<E>{row}.each(rest, add);
     __syncthreads();
     Drawn d;
     u64 pass;
@@ -964,7 +1011,7 @@ __device__ __noinline__ void draw_whole(const Args *args, int64_t r)
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {                     // top-k (or all tokens, for their weight), then top-p
         if (pass == 0 ? w.k <= 0 && !(w.set.p < 1.0f) : !(w.set.p < 1.0f)) continue;
-        const u64 by = cut_by_parts(row, sc, all_tokens, part, pass == 0 && w.k > 0 ? w.k : kNone, pass == 0 ? kNone : target_of(w.set.p, of_k),
+        const u64 by = cut_by_parts(InRow<E>{row}, sc, all_tokens, part, pass == 0 && w.k > 0 ? w.k : kNone, pass == 0 ? kNone : target_of(w.set.p, of_k),
                                     pass == 0 ? of_k : none);
         last = by < last ? by : last;
     }
@@ -1189,7 +1236,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
             else atomicAdd(&s.coarse_mass[bin], rescaled(n, tile_top, sc));
             if (ask == Ask::kBoth) atomicAdd(&s.coarse_mass[bin], rescaled(a.tile_mass[r * n_bins + i], tile_top, sc));
         };
-        if (tid == 0) s.n = s.n_pieces = 0;
+        if (tid == 0) s.n = s.n_pieces = s.at_least = 0;
         if (tid < kCoarse) {
             s.coarse_mass[tid] = 0;
             s.coarse_count[tid] = 0;
@@ -1226,10 +1273,16 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
             // the pieces that can have such a token, then a wave every 16th of them, four at a time
             uint16_t *todo = reinterpret_cast<uint16_t *>(s.mass);
             static_assert(kMaxPieces <= 0xffff && kMaxPieces * 2 <= sizeof(s.mass) + sizeof(s.count), "pieces by their number");
+            // by weight alone: a token of bin b weighs 2^-((b - 1) / 4) at most, so there are at least this many (of the further bins the
+            // weights' rounding to 2^-43 would be most)
+            if (!counted && weighed && tid <= w.end && tid <= kCoarse / 2) {
+                const double n_here = static_cast<double>(s.coarse_mass[tid]) * 0x1p-43 * static_cast<double>(exp2f(0.25f * static_cast<float>(tid - 1)));
+                atomicAdd(&s.at_least, static_cast<uint32_t>(n_here < 0x1p21 ? n_here : 0x1p21));
+            }
             for (int32_t i = tid; i < a.pieces; i += kThreads)
                 if (can(piece_max[i])) todo[atomicAdd(&s.n_pieces, 1u)] = static_cast<uint16_t>(i);
             __syncthreads();
-            const int32_t n_todo = s.n_pieces;
+            const int32_t n_todo = s.at_least <= kList + kCoarse ? s.n_pieces : 0;
 #pragma unroll 1
             for (int32_t i0 = wave; i0 < n_todo; i0 += kWaves * 4) {
                 v4u raw[4];
@@ -1243,7 +1296,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
                 each_of(row, raw, b, can, put);
             }
             __syncthreads();
-            n = s.n;
+            n = s.at_least <= kList + kCoarse ? s.n : kList + 1;
             __syncthreads();
         }
         if (n <= kShort) {

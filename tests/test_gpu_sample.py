@@ -272,3 +272,20 @@ def test_rows_beyond_32_bits(mq):
         assert torch.equal(token[-3:], alone[0]) and torch.equal(logprob[-3:], alone[1])
         if args[1] is None and args[2] is None:
             assert token[:-3].cpu().numpy().tolist() == np.floor(u[:-3].cpu().numpy().astype(np.float64) * V).astype(int).tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_bins_of_every_length(mq, dtype):
+    """As many tokens in the bin that top-p cuts as are held there, one less and one more, among long lists."""
+    rng = np.random.default_rng(14)
+    V = 60000
+    for n in (2000, 8191, 8192, 8193, 20000):
+        x = rng.uniform(-9.0, -4.0, (5, V))
+        for r in range(5):
+            x[r, rng.permutation(V)[:n]] = -0.01 * rng.random(n) if r < 3 else 0.25
+        x = x.astype(np.float16 if dtype == torch.float16 else np.float32)
+        u = np.array([0.0, 0.3, 0.7, NEXT, 0.5], dtype=np.float32)
+        for p in (0.3, 0.6, 0.9, 0.99):
+            check(mq, x, 1.0, 0, p, 0.0, u, dtype, f"{n} {p}")
+        check(mq, x, 1.0, n - 100, 0.9, 0.0, u, dtype, f"{n} by both")
+        check(mq, x, 1.0, n + 100, 0.999, 1e-3, u, dtype, f"{n} and by weight")
