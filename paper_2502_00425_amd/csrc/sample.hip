@@ -5,16 +5,20 @@
 // multiples of 2^-43: such sums do not depend on their order, so that atomics in LDS give the same token every time.  2^20 tokens of
 // weight 1 are 2^63.  Parts of a row are summed against their own largest logit and put together by its weight.
 //
-// Nothing is sorted but a short list.  tile_kernel, a work-group to 16 KiB of a row, takes from every piece of 64 blocks of 16 bytes its
-// largest logit and, as the row's settings ask, the weight of every piece or the tokens and weights of the tile by bins of the logit.
+// Nothing is sorted but short runs of the ranking.  tile_kernel, a work-group to 16 KiB of a row, takes from every piece of 64 blocks of 16 bytes
+// its largest logit and, as the row's settings ask, the weight of four pieces or the tokens or weights of the tile by bins of the logit.
 // pick_kernel, a work-group to a row, puts them together:
-//   rows without filters: the piece in which the sum passes u S, and the token in it;
-//   what top-k, top-p and min-p can keep is a short list, by the bins: it is gathered from the pieces whose largest logit can be in it, and
-//   everything is decided among its tokens;
-//   many tokens are kept: the tokens of the bin in which the ranking is cut are gathered (narrowed by finer bins, then digit by digit of their
-//   rank, where they are more than the list holds); with the rank of the last kept token the tiles' bins give the tile in which the
-//   sum passes u S, which is looked at token by token;
-//   the rest (+inf among the logits, long lists by top-k or min-p alone): bins of the whole row and a walk over it by the one work-group.
+//   rows without filters: the four pieces in which the sum passes u S, and the token in them;
+//   what top-k, top-p and min-p can keep is, by the bins, a list of up to kList tokens: they are gathered from the pieces whose largest logit
+//   can be among them, and everything is decided there, by comparing each with all (up to kShort) or by parts of the ranking and the vocabulary;
+//   more tokens are kept: those of the bin in which the ranking is cut are gathered (or narrowed in the row itself, by finer bins and then digit by
+//   digit of their rank, where LDS does not hold them); with the rank of the last kept token the tiles' bins give the tile in
+//   which the sum passes u S, which is looked at token by token;
+//   the rest (+inf among the logits, more than kList tokens by top-k or min-p alone): bins of the whole row and a walk over it by the one
+//   work-group.
+// What bounds them, in us a launch: tile_kernel the weights' arithmetic (256 rows of 128000 fp32 33 drawn from all, 4 TB/s; greedy 20, 6.5 TB/s from the
+// last cache; 64 rows of 150001 fp16 10 and 4) or the atomics of the bins (17 by top-p); pick_kernel trips to what other L2s wrote, the gather
+// and the code's own way through a cold cache (one row's 50 best of 32000 9.5, 64 rows' of 150001 12).
 #include <cfloat>
 #include <cmath>
 
@@ -26,13 +30,13 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxTokens = 1 << 20;
-constexpr int kBins = 1024;                // of walk_row
+constexpr int kBins = 1024;                // parts of a ranking or of the vocabulary, one to a thread
 constexpr int kCoarse = 256;               // bins of a tile: 1/4 of x wide, the last one has all that is left
 constexpr int kTileThreads = 256, kTileBlocks = 4, kTilePieces = kTileThreads / 64 * kTileBlocks;
 constexpr int kMaxPieces = ((kMaxTokens + 6) / 4 + kTileThreads * kTileBlocks - 1) / (kTileThreads * kTileBlocks) * kTilePieces;    // fp32, tiles filled up
 constexpr int kShort = 256;                // tokens of a list up to which each is compared with all others
 constexpr int kList = 2048;                // tokens that are sorted at a time, two to a thread
-constexpr int kBin = 8192;                 // tokens of the cut's bin that are held, where more than kList are kept
+constexpr int kHold = 8192;                // tokens that are held in LDS: a list, or those of one bin
 constexpr u64 kNone = ~0ull;
 constexpr int kIndexBits = 24;             // of a rank: logit, then number of the token
 
@@ -94,11 +98,11 @@ struct Shared {
             uint32_t count[256];
         } digit;
     };
-    u64 bin[kBin];                         // tokens of the cut's bin, by their rank
+    u64 held[kHold];                       // tokens by their rank, as they came
     u64 room[kWaves];
     u64 found[2];
     uint32_t found32[2];
-    uint32_t n, n_pieces, n_bin, at_least;
+    uint32_t n, n_pieces, n_held, at_least;
 };
 
 __device__ __forceinline__ Shared &lds()
@@ -391,6 +395,58 @@ __device__ __forceinline__ void each_of(const Row<E> &row, const v4u (&raw)[4], 
     }
 }
 
+__device__ __forceinline__ void put_held(float l, int32_t token)
+{
+    const uint32_t at = atomicAdd(&lds().n, 1u);
+    if (at < kHold) lds().held[at] = rank_of(l, token);
+}
+
+// Takes the tokens of four blocks into the held ones, as far as there is room; n counts them.  A wave asks for its places once.
+template <typename E, typename P>
+__device__ __forceinline__ void hold_blocks(const Row<E> &row, const v4u (&raw)[4], const int32_t (&b)[4], P is, uint32_t &n)
+{
+    constexpr int kPer = Row<E>::kPer, kMany = 256;
+    uint32_t hits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float l[kPer];
+        row.read(raw[i], b[i], l);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) hits |= is(l[e]) && b[i] < row.n_blocks ? 1u << (i * kPer + e) : 0u;
+    }
+    const uint32_t mine = __builtin_popcount(hits), up = wave_scan(mine), total = from_lane(up, 63);
+    if (total == 0) return;
+    uint32_t at = 0;
+    if ((threadIdx.x & 63) == 0) at = atomicAdd(&n, total);
+    at = __builtin_amdgcn_readfirstlane(at) + up - mine;
+    u64 *to = lds().held;
+    if (total > kMany) {                   // one by one, each of a lane's would be waited for
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float l[kPer];
+            row.read(raw[i], b[i], l);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (hits >> (i * kPer + e) & 1) {
+                    if (at < kHold) to[at] = rank_of(l[e], row.token(b[i], e));
+                    ++at;
+                }
+        }
+        return;
+    }
+    const int32_t b0 = b[0], b1 = b[1], b2 = b[2], b3 = b[3];
+#pragma unroll 1
+    for (; hits != 0; hits &= hits - 1, ++at) {
+        const int h = __builtin_ctz(hits), i = h / kPer;
+        int32_t block = b0;
+        block = i == 1 ? b1 : block;
+        block = i == 2 ? b2 : block;
+        block = i == 3 ? b3 : block;
+        const int32_t token = row.token(block, h % kPer);
+        if (at < kHold) to[at] = rank_of(row.logit(token), token);
+    }
+}
+
 // The same for the whole row.
 template <typename E>
 struct InRow {
@@ -411,16 +467,32 @@ struct InRow {
             each_of(row, raw, b, is, f);
         }
     }
+
+    template <typename P>
+    __device__ __forceinline__ void hold(P is, uint32_t &n) const
+    {
+#pragma unroll 1
+        for (int32_t b0 = threadIdx.x; b0 - static_cast<int32_t>(threadIdx.x & 63) < row.n_blocks; b0 += kThreads * 4) {       // whole waves
+            v4u raw[4];
+            int32_t b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                b[i] = b0 + i * kThreads;
+                raw[i] = row.load(b[i]);
+            }
+            hold_blocks(row, raw, b, is, n);
+        }
+    }
 };
 
-// And for the n tokens that LDS holds of the cut's bin.
-struct InBin {
+// And for the n tokens that LDS holds.
+struct Held {
     int n;
 
     template <typename P, typename F>
     __device__ __forceinline__ void each(P is, F f) const
     {
-        const u64 *rank = lds().bin;
+        const u64 *rank = lds().held;
 #pragma unroll 1
         for (int i = threadIdx.x; i < n; i += kThreads) {
             const float l = logit_of(rank[i]);
@@ -440,6 +512,7 @@ struct Known {
     int base, end;                         // first coarse bin, and the one of the cut
     u64 target;                            // of top-p alone
     u64 all_mass;                          // weight of all tokens that can be chosen, 0: not known
+    float least;                           // the smallest logit of a list
 };
 
 __device__ __forceinline__ Known &known()
@@ -476,7 +549,7 @@ __device__ __forceinline__ void put(float l, int32_t token)
 }
 
 // Sorts the n <= kList numbers of the list, rising; all threads.
-__device__ __noinline__ void sort_list(int n)
+__device__ __forceinline__ void sort_list(int n)
 {
     u64 *v = lds().list.rank;
     int size = 2;
@@ -597,14 +670,14 @@ __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double mi
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid < kShort) place[tid] = kept_place[tid] = 0;
     __syncthreads();
-    count_ahead(s.list.rank, n, place);
+    count_ahead(s.held, n, place);
     __syncthreads();
     u64 held[kHeld];
     u64 sum = 0, weight[kHeld];
     uint32_t n_kept = 0;
     if (wave == 0) {
 #pragma unroll
-        for (int g = 0; g < kHeld; ++g) held[g] = g * 64 + lane < n ? s.list.rank[g * 64 + lane] : kNone;
+        for (int g = 0; g < kHeld; ++g) held[g] = g * 64 + lane < n ? s.held[g * 64 + lane] : kNone;
         // ---- along the ranking: token lane + 64 g goes to its place, then a lane has four places next to each other
         u64 *by_place = s.list.sum;
 #pragma unroll
@@ -679,57 +752,10 @@ __device__ __forceinline__ Drawn draw_short(int n, int32_t k, float p, double mi
     const u64 pass = drawn_at(u, sum);
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) {
-        if (at <= pass && at + w[e] > pass) d = {s.list.rank[who[lane * kHeld + e]], sum};
+        if (at <= pass && at + w[e] > pass) d = {s.held[who[lane * kHeld + e]], sum};
         at += w[e];
     }
     return d;
-}
-
-// The same for more tokens: sorted by rank, then the kept ones by their number.
-__device__ __noinline__ void draw_sorted(const Args *args, int64_t r, int n)
-{
-    Shared &s = lds();
-    const Known w = known();
-    const Scale &sc = w.sc;
-    const float p = w.set.p, u = w.set.u;
-    const double min_w = w.min_w;
-    const u64 all_mass = w.all_mass;
-    const bool all_known = all_mass > 0;
-    int32_t k = w.k;
-    constexpr u64 kTokenMask = (1u << kIndexBits) - 1;
-    const int i = threadIdx.x * 2;
-    sort_list(n);
-    sum_list(n, sc);
-    if (k <= 0 || k > n) k = n;
-    int kept = cut_list(n, k, p < 1.0f ? target_of(p, all_known ? all_mass : s.list.sum[k - 1]) : kNone);
-    if (min_w > 0.0) {
-        auto heavy = [&](int i) { return i < kept && sc.weight(logit_of(s.list.rank[i])) >= min_w; };
-        const int n_heavy = count_all(heavy(i), heavy(i + 1));
-        kept = n_heavy > 1 ? n_heavy : 1;
-    }
-    const u64 sum = s.list.sum[kept - 1], pass = drawn_at(u, sum);
-    const u64 r0 = i < kept ? s.list.rank[i] : kNone, r1 = i + 1 < kept ? s.list.rank[i + 1] : kNone;
-    __syncthreads();
-    // sorted by the token's number, with the place in the ranking behind it
-    if (i < kept) s.list.rank[i] = (r0 & kTokenMask) << 12 | static_cast<u64>(i);
-    if (i + 1 < kept) s.list.rank[i + 1] = (r1 & kTokenMask) << 12 | static_cast<u64>(i + 1);
-    __syncthreads();
-    sort_list(kept);
-    auto weight_at = [&](int at) {
-        const int place = static_cast<int>(s.list.rank[at] & 0xfff);
-        return s.list.sum[place] - (place > 0 ? s.list.sum[place - 1] : 0);
-    };
-    const u64 x = i < kept ? weight_at(i) : 0, y = i + 1 < kept ? weight_at(i + 1) : 0;
-    u64 total;
-    const u64 up = scan(x + y, s.room, total);
-    if (up - x - y <= pass && up - y > pass) s.found32[0] = static_cast<uint32_t>(s.list.rank[i] & 0xfff);
-    if (up - y <= pass && up > pass) s.found32[0] = static_cast<uint32_t>(s.list.rank[i + 1] & 0xfff);
-    __syncthreads();
-    const int place = s.found32[0];                            // a place has its logit in the thread that held it
-    Drawn d;
-    if (place == i) d = {r0, sum};
-    if (place == i + 1) d = {r1, sum};
-    d.write(*args, r, sc);
 }
 
 // The piece in which the sum passes u's share of it, of `pieces` sums in s.piece, and the sum ahead of it, for all threads: s.found32[0],
@@ -829,6 +855,32 @@ __device__ __forceinline__ u64 cut_run(const S &tokens, const Scale &sc, F of, u
     __syncthreads();
     const int m = s.n;
     __syncthreads();
+    if (m <= 64) {                         // by one wave, each compared with all
+        if (tid < 64) {
+            const u64 mine = tid < m ? s.list.rank[tid] : kNone, weight = tid < m ? sc.weigh(logit_of(mine)) : 0;
+            s.list.sum[tid] = weight;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            u64 ahead = 0;
+            uint32_t before = 0;
+#pragma unroll 2
+            for (int j = 0; j < m; ++j) {
+                const bool less = s.list.rank[j] < mine;
+                before += less ? 1 : 0;
+                ahead += less ? s.list.sum[j] : 0;
+            }
+            const bool kept = tid < m && (before == 0 || (before < count && ahead < mass));
+            const u64 sum = wave_sum(kept ? weight : 0);
+            if (kept && before + 1 == __builtin_popcountll(__ballot(kept))) {
+                s.found[0] = mine;
+                s.found[1] = sum;
+            }
+        }
+        __syncthreads();
+        const u64 last = s.found[0];
+        kept_mass = passed + s.found[1];
+        __syncthreads();
+        return last;
+    }
     sort_list(m);
     sum_list(m, sc);
     const int k = cut_list(m, count, mass);
@@ -888,6 +940,60 @@ __device__ __forceinline__ u64 last_by_weight(const Scale &sc, double min_w)
     return rank_of(float_of(lo), (1 << kIndexBits) - 1);
 }
 
+// Which of the n <= kHold tokens held is drawn: the last kept one by parts of the ranking, then the weights of the kept ones by parts of the
+// vocabulary, and of the part in which the sum passes u S a thread has one token.  (Sorted by rank and then by their number, 1900 tokens took
+// 45 us.)
+__device__ __noinline__ void draw_list(const Args *args, int64_t r, int n)
+{
+    Shared &s = lds();
+    const Known w = known();
+    const Scale &sc = w.sc;
+    const int tid = threadIdx.x;
+    const Held tokens = {n};
+    const float p = w.set.p, scale = fmaxf((kBins - 0.5f) / (sc.m - w.least), sc.bin_of);
+    auto any = [](float) { return true; };
+    auto part_of = [&](float l) { return static_cast<int>(fminf((sc.m - l) * scale, kBins - 1.0f)); };
+    u64 last = kNone, of_k = w.all_mass, none;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {                     // top-k (or all tokens, for their weight), then top-p
+        if (pass == 0 ? (w.k <= 0 || w.k >= n) && (of_k > 0 || !(p < 1.0f)) : !(p < 1.0f)) continue;
+        const u64 by = cut_by_parts(tokens, sc, any, part_of, pass == 0 && w.k > 0 ? w.k : kNone, pass == 0 ? kNone : target_of(p, of_k),
+                                    pass == 0 ? of_k : none);
+        last = by < last ? by : last;
+    }
+    auto kept = [&](float l, int32_t token) { return rank_of(l, token) <= last && (!(w.min_w > 0.0) || sc.weight(l) >= w.min_w); };
+    int shift = 0;
+    while ((args->V - 1) >> shift >= kBins) ++shift;
+    static_assert(kMaxTokens <= kBins * kThreads && kThreads <= kList, "tokens of a part");
+    __syncthreads();
+    s.mass[tid] = 0;
+    s.list.sum[tid] = 0;
+    __syncthreads();
+    tokens.each(any, [&](float l, int32_t token) {
+        if (kept(l, token)) atomicAdd(&s.mass[token >> shift], sc.weigh(l));
+    });
+    __syncthreads();
+    const u64 here = s.mass[tid];
+    u64 sum;
+    const u64 up = scan(here, s.room, sum), pass = drawn_at(w.set.u, sum);
+    if (up > pass && up - here <= pass) {
+        s.found32[0] = tid;
+        s.found[0] = up - here;
+    }
+    __syncthreads();
+    const int part = s.found32[0];
+    tokens.each(any, [&](float l, int32_t token) {
+        if (token >> shift != part || !kept(l, token)) return;
+        s.list.sum[token & ((1 << shift) - 1)] = sc.weigh(l);
+        s.list.rank[token & ((1 << shift) - 1)] = rank_of(l, token);
+    });
+    __syncthreads();
+    const u64 mine = s.list.sum[tid];
+    u64 all;
+    const u64 at = s.found[0] + scan(mine, s.room, all);
+    if (at > pass && at - mine <= pass) Drawn{s.list.rank[tid], sum}.write(*args, r, sc);
+}
+
 // Many tokens are kept, and the tiles have their weights by coarse bins: the last kept token, in the bin of the cut, then the tile in which the
 // sum passes u S, which is looked at token by token.
 template <typename E>
@@ -919,18 +1025,15 @@ __device__ __noinline__ void draw_long(const Args *args, int64_t r)
         const u64 c0 = bin > 0 ? s.coarse_count[bin - 1] : 0, m0 = bin > 0 ? s.coarse_mass[bin - 1] : 0;
         const float from = bin < kCoarse - 1 ? sc.least_near(w.base + bin) : -FLT_MAX, to = bin > 0 ? sc.least_near(w.base + bin - 1) : INFINITY;
         auto in = [&](float l) { return l >= from && l < to; };
-        if (tid == 0) s.n_bin = 0;
+        if (tid == 0) s.n_held = 0;
         __syncthreads();
-        InRow<E>{row}.each(in, [&](float l, int32_t token) {
-            const uint32_t at = atomicAdd(&s.n_bin, 1u);
-            if (at < kBin) s.bin[at] = rank_of(l, token);
-        });
+        InRow<E>{row}.hold(in, s.n_held);
         __syncthreads();
         held = bin;
-        n_held = s.n_bin;
+        n_held = s.n_held;
         auto part = [&](float l) { return sc.fine(l, w.base + bin); };
         const u64 count = pass == 0 ? w.k - c0 : kNone, mass = pass == 0 ? kNone : target - m0;
-        const u64 by = n_held <= kBin ? cut_by_parts(InBin{static_cast<int>(n_held)}, sc, in, part, count, mass, in_bin)
+        const u64 by = n_held <= kHold ? cut_by_parts(Held{static_cast<int>(n_held)}, sc, in, part, count, mass, in_bin)
                                       : cut_by_parts(InRow<E>{row}, sc, in, part, count, mass, in_bin);
         last = by < last ? by : last;
         if (pass == 0 && p < 1.0f) {
@@ -967,7 +1070,7 @@ __device__ __noinline__ void draw_long(const Args *args, int64_t r)
     auto add = [&](float l, int32_t token) {
         if (rank_of(l, token) <= last) atomicAdd(&s.piece[(token + row.skip) / (Row<E>::kPer * kTileThreads * kTileBlocks)], sc.weigh(l));
     };
-    if (held == bin && n_held <= kBin) InBin{static_cast<int>(n_held)}.each(rest, add);
+    if (held == bin && n_held <= kHold) Held{static_cast<int>(n_held)}.each(rest, add);
     else InRow<E>{row}.each(rest, add);
     __syncthreads();
     Drawn d;
@@ -1187,7 +1290,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
     const Ask ask = set.ask();
     const float p = set.p;
     Known w = {set, Scale(set.t, top == INFINITY ? 0.0f : top), top, set.min_p > 0.0f ? static_cast<double>(set.min_p) : 0.0, set.k, 0,
-               kCoarse - 1, 0, 0};
+               kCoarse - 1, 0, 0, 0.0f};
     const Scale &sc = w.sc;
     const bool by_weight = w.min_w > 0.0 && !(p < 1.0f);       // min-p says by itself which tokens can be kept
     const Args *args = reinterpret_cast<const Args *>((const void *)__builtin_amdgcn_kernarg_segment_ptr());   // a, where it is
@@ -1268,6 +1371,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
             least = fmaxf(least, static_cast<float>(static_cast<double>(top) - x / sc.x_of - fabs(static_cast<double>(top)) * 0x1p-22));
         }
         auto can = [&](float l) { return l >= least; };
+        w.all_mass = ask == Ask::kMass ? all_mass : 0;
+        w.least = least;
+        if (tid == 0) known() = w;                             // for a way that may follow, so that registers need not keep it
         uint32_t n = kList + 1;
         if (!counted || up_to_end <= kList || by_weight) {
             // the pieces that can have such a token, then a wave every 16th of them, four at a time
@@ -1293,20 +1399,19 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Args a)
                     b[j] = i < n_todo ? todo[i] * 64 + lane : row.n_blocks;
                     raw[j] = row.load(b[j]);
                 }
-                each_of(row, raw, b, can, put);
+                each_of(row, raw, b, can, put_held);
             }
             __syncthreads();
             n = s.at_least <= kList + kCoarse ? s.n : kList + 1;
             __syncthreads();
         }
         if (n <= kShort) {
-            draw_short(n, w.k, p, w.min_w, set.u, all_mass, ask == Ask::kMass, sc).write(a, r, sc);
+            const Known &w = known();
+            draw_short(n, w.k, w.set.p, w.min_w, w.set.u, w.all_mass, w.all_mass > 0, w.sc).write(*args, r, w.sc);
             return;
         }
-        w.all_mass = all_mass;
-        if (tid == 0) known() = w;
         __syncthreads();
-        if (n <= kList) draw_sorted(args, r, n);
+        if (n <= kList) draw_list(args, r, n);
         else if (weighed) draw_long<E>(args, r);
         else draw_whole<E>(args, r);
     } else {
