@@ -87,7 +87,9 @@ __device__ __forceinline__ void write_row(const Plan &a, int32_t i, int32_t s, i
     if (a.slot) a.slot[i] = at;
 }
 
-// Bound by trips to memory, one behind another: lengths and requests, the free pages, the table, and a barrier between them.
+// Bound by trips to memory, one behind another: lengths and requests, the free pages, the table, and a barrier between them.  us of a call in a
+// graph: one sequence and row 3.7, 256 generating sequences of up to 16384 tokens with 29 ended ones, whose pages go back, 13.2, 700 sequences that get
+// 134302 rows 11.8 with plan_rows_kernel; an empty launch is 1.6.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void plan_kernel(Plan a, int32_t write_rows)
 {
