@@ -735,7 +735,8 @@ int64_t mquant_paged_attention_shared_workspace_bytes(int32_t T, int32_t n_seq, 
  *                     not share it
  * Pages that lie wholly inside a prefix are looked up in the first sequence's table only; where a prefix ends inside a
  * page, that page is each sequence's own and holds the prefix's last tokens in each.
- * n_groups may be 0.  Errors: as mquant_paged_attention; ERR_BAD_SHAPE (n_groups < 0), ERR_NULL (the groups' arrays).
+ * n_groups may be 0.  Errors: as mquant_paged_attention; ERR_BAD_SHAPE (n_groups < 0), ERR_NULL (the groups' arrays),
+ * ERR_UNSUPPORTED (groups and a table beyond 2^30 slots).
  */
 int mquant_paged_attention_shared(const void *q_dev, int64_t ldq, const mquant_paged_cache_t *cache, const int32_t *row_start_dev,
                                   const int32_t *pos_dev, const int32_t *group_start_dev, const int32_t *prefix_dev,

@@ -1428,6 +1428,7 @@ extern "C" int mquant_paged_attention_shared(const void *q, int64_t ldq, const m
     if (!group_start || !prefix) return MQUANT_ERR_NULL;
     if (!aligned_to(group_start, 4) || !aligned_to(prefix, 4)) return MQUANT_ERR_ALIGNMENT;
     const int32_t slots = cache->table_pages * cache->page_size;
+    if (slots > 1 << 30) return MQUANT_ERR_UNSUPPORTED;        // where a piece begins, behind a prefix, has to fit 32 bits
     auto in_table = [&](int32_t bound) { return bound > 0 && bound < slots ? bound : slots; };
     SharedPlan p = make_shared_plan(T, cache->n_seq, n_groups, n_q_heads, n_kv, max_rows, in_table(max_prefix), in_table(max_suffix));
     // scratch that was asked for with bounds beyond the table may be another size: then those bounds' pieces are taken

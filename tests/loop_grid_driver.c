@@ -26,7 +26,7 @@ int main(int argc, char **argv)
     LOAD(mquant_paged_attention_shared); LOAD(mquant_paged_attention_shared_workspace_bytes);
     LOAD(mquant_step_plan); LOAD(mquant_sample); LOAD(mquant_sample_workspace_bytes);
     void *P = (void *)0x10000, *Q = (void *)0x20000;
-    const int32_t seqs[] = {1, 2, 31, 200, 2000}, rows[] = {1, 2, 5, 13, 100, 700}, tables[] = {1, 513, 33554431}, groups[] = {0, 1, 3, 200, 3000},
+    const int32_t seqs[] = {1, 2, 31, 200, 2000}, rows[] = {1, 2, 5, 13, 100, 700}, tables[] = {1, 513, 16777216}, groups[] = {0, 1, 3, 200, 3000},
                   bounds[] = {0, 1, 129, 8200, 131072, 0x40000000, 0x7fffff81, 0x7fffffff};
     int failed = 0;
     for (int h = 0; h < 3; ++h)

@@ -140,6 +140,9 @@ def test_shared_attention_refusals():
         assert call(n_groups=n_groups, c=cache(k=None, v=None, table=None, n_seq=0), q=None) == mq.OK
         assert call(n_groups=n_groups, T=1 << 30, hq=4) == mq.ERR_UNSUPPORTED
     assert call(groups=None) == call(prefix=None) == mq.ERR_NULL
+    for page, table_pages in ((16, (1 << 26) + 1), (64, 33554431), (4096, (1 << 18) + 1)):
+        assert call(c=cache(page=page, table_pages=table_pages), ws=None) == mq.ERR_UNSUPPORTED
+        assert call(c=cache(page=page, table_pages=table_pages - 1), ws=None) == (mq.ERR_UNSUPPORTED if page == 64 else mq.ERR_WORKSPACE)
     assert call(groups=P + 2) == call(prefix=P + 1) == mq.ERR_ALIGNMENT
     big = dict(T=2, rows=1, longest=100000, behind=100, c=cache(page=64, table_pages=2000, n_pages=4000))
     need = size(2, 2, 1, 28, 4, 128, 1, 100000, 100)
