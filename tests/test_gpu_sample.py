@@ -289,3 +289,33 @@ def test_bins_of_every_length(mq, dtype):
             check(mq, x, 1.0, 0, p, 0.0, u, dtype, f"{n} {p}")
         check(mq, x, 1.0, n - 100, 0.9, 0.0, u, dtype, f"{n} by both")
         check(mq, x, 1.0, n + 100, 0.999, 1e-3, u, dtype, f"{n} and by weight")
+
+
+def test_two_graphs_that_share_a_workspace_and_two_streams_at_once(mq):
+    """Steps of other sizes and settings in turn on the same scratch; then both at once on two streams, each with its own: the same bits."""
+    rng = np.random.default_rng(15)
+    ws = torch.full((mq.sample_workspace_bytes(70, 60000),), 255, dtype=torch.uint8, device="cuda")
+    steps = []
+    for rows, V, dtype, kind in ((70, 9001, torch.float16, "model"), (25, 60000, torch.float32, "normal")):
+        x, u = dev(logits_of(rng, rows, V, dtype, kind)), dev(rng.random(rows, dtype=np.float32))
+        cols = [dev(np.resize(np.asarray(c, d), rows)) for c, d in zip(zip(*SETTINGS), (np.float32, np.int32, np.float32, np.float32))]
+        out, lp = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.float32, device="cuda")
+        want = mq.sample(x, *cols, u)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            mq.sample(x, *cols, u, out, lp, ws)
+        steps.append((graph, (x, *cols, u), out, lp, want))
+    for _ in range(3):
+        for graph, _, out, lp, want in steps:
+            out.fill_(-5), lp.fill_(5.0)
+            graph.replay()
+            assert torch.equal(out, want[0]) and torch.equal(lp, want[1])
+    streams = [torch.cuda.Stream() for _ in steps]
+    torch.cuda.synchronize()
+    got = []
+    for stream, (_, args, _, _, _) in zip(streams, steps):
+        with torch.cuda.stream(stream):
+            got.append([mq.sample(*args) for _ in range(20)])
+    torch.cuda.synchronize()
+    for results, (_, _, _, _, want) in zip(got, steps):
+        assert all(torch.equal(a, want[0]) and torch.equal(b, want[1]) for a, b in results)
