@@ -18,7 +18,7 @@
 //   work-group.
 // What bounds them, in us a launch: tile_kernel the weights' arithmetic (256 rows of 128000 fp32 33 drawn from all, 4 TB/s; greedy 20, 6.5 TB/s from the
 // last cache; 64 rows of 150001 fp16 10 and 4) or the atomics of the bins (17 by top-p); pick_kernel trips to what other L2s wrote, the gather
-// and the code's own way through a cold cache (one row's 50 best of 32000 9.5, 64 rows' of 150001 12).
+// and the code's own way through a cold cache (one row's 50 best of 32000 9, 64 rows' of 150001 11).
 #include <cfloat>
 #include <cmath>
 
@@ -371,16 +371,28 @@ __device__ __forceinline__ u64 target_of(float p, u64 sum)
 template <typename E, typename P, typename F>
 __device__ __forceinline__ void each_of(const Row<E> &row, const v4u (&raw)[4], const int32_t (&b)[4], P is, F f)
 {
-    constexpr int kPer = Row<E>::kPer;
+    // eight tokens a block: one block at a time, since code that runs once is waited for (four at a time 1 us more, one row of 32000 15.2 us); of
+    // four tokens that is no longer so (12.7 us, 13.0 by one)
+    constexpr int kPer = Row<E>::kPer, kUnroll = kPer == 8 ? 1 : 4;
     // by name: an array that the program indexes is given 16 KiB of LDS or scratch memory (50 best of 256 rows of 128000: 49 us, 37 by name)
     const int32_t b0 = b[0], b1 = b[1], b2 = b[2], b3 = b[3];
     uint32_t hits = 0;
-#pragma unroll
+    v4u r0 = raw[0], r1 = raw[1], r2 = raw[2], r3 = raw[3];
+    int32_t c0 = b0, c1 = b1, c2 = b2, c3 = b3;
+#pragma unroll kUnroll
     for (int i = 0; i < 4; ++i) {
         float l[kPer];
-        row.read(raw[i], b[i], l);
+        row.read(r0, c0, l);
+        const bool in = c0 < row.n_blocks;
+        hits >>= kPer;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) hits |= is(l[e]) && b[i] < row.n_blocks ? 1u << (i * kPer + e) : 0u;
+        for (int e = 0; e < kPer; ++e) hits |= is(l[e]) && in ? 1u << (3 * kPer + e) : 0u;
+        r0 = r1;
+        r1 = r2;
+        r2 = r3;
+        c0 = c1;
+        c1 = c2;
+        c2 = c3;
     }
 #pragma unroll 1
     while (hits != 0) {
