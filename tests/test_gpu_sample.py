@@ -37,7 +37,7 @@ def check(mq, logits, t, k, p, m, u, dtype=torch.float16, what=""):
         if want < 0:
             assert logprob[r] == -np.inf
         else:
-            assert abs(logprob[r] - lp) <= 2.0 ** -24 * abs(lp) + V * 2.0 ** -44 + 2.0 ** -37, f"{what} row {r}: {logprob[r]} {lp}"
+            assert abs(float(logprob[r]) - lp) <= 2.0 ** -24 * abs(lp) + V * 2.0 ** -44 + 2.0 ** -37, f"{what} row {r}: {logprob[r]} {lp}"
 
 
 def logits_of(rng, rows, V, dtype, kind="model"):
